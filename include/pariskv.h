@@ -431,6 +431,139 @@ int pariskv_offload_rows(const void* K_src, const void* V_src, int64_t src_capac
                          void* K_dst, void* V_dst, int64_t dst_capacity, int64_t dst_row, int64_t t,
                          int32_t batch, int32_t n_kv_heads, void* stream);
 
+/* ------------------------------------------------- quantised K/V cache */
+
+/* A K/V cache held in 8- or 4-bit codes, for the rows that a decode step
+ * retrieves (half to a quarter of the bytes that cross HBM or the host link).
+ *   rec  uint8 [batch][Hkv][capacity][pariskv_quant_record_bytes(k_bits, v_bits)],
+ *        16-byte aligned, device memory (host_mapped == 0) or pinned host memory
+ *        that kernels reach over the host link (host_mapped == 1).
+ * A row of 128 float16 values is 4 blocks of 32 dims.  A block has a scale 2^s
+ * and stands for code values times 2^s, the codes e4m3 (8 bits: 4 exponent and
+ * 3 mantissa bits, bias 7, largest value M = 448) or e2m1 (4 bits: 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives, M = 6):
+ *   s     the smallest integer >= s_min with max |x| <= M 2^s; s_min = -15 (8
+ *         bits), -23 (4 bits)
+ *   code  the code value nearest to x 2^-s, ties to the even code, of those
+ *         whose value times 2^s stays within float16's 65504.
+ * Every stored value is then a float16 value, and a value of that set is kept
+ * as it is.  Blocks with infinities or NaNs hold unspecified values (no fault;
+ * other blocks are as they would be).
+ * One record, the K codes in order of their dims (4-bit codes two a byte, the
+ * even dim in the low bits), the V codes, the 4 bytes s + 127 of K's blocks,
+ * the 4 of V's, 8 zero bytes: 272 bytes with 8-bit codes, 208 with 8 and 4
+ * bits, 144 with 4-bit codes. */
+typedef struct pariskv_quant_cache {
+    uint8_t* rec;
+    int64_t capacity;    /* rows per (sequence, KV head), 1..2^30-1 */
+    int32_t k_bits;      /* 8 or 4 */
+    int32_t v_bits;      /* 8 or 4 */
+    int32_t host_mapped; /* 0 or 1 */
+} pariskv_quant_cache;
+
+/* Bytes of one record; 0 for other numbers of bits.  Host only. */
+size_t pariskv_quant_record_bytes(int32_t k_bits, int32_t v_bits);
+
+/* Quantise K/V rows as they are written: rows [src_row, src_row + t) of K and V
+ * (device float16 [batch][Hkv][src_capacity][D]) into t rows of the cache, from
+ * `row` on, or, with rows (device int32 [batch]) non-NULL, from rows[b] on in
+ * sequence b; then rows that fall outside [0, capacity) are not written.
+ * Errors: INVALID, CAPACITY (row + t > capacity, rows NULL), HIP. */
+int pariskv_quantize_rows(const pariskv_config* cfg, const pariskv_quant_cache* cache, const void* K,
+                          const void* V, int64_t src_capacity, int64_t src_row, int64_t row,
+                          const int32_t* rows, int64_t t, int32_t batch, void* stream);
+
+/* The values of t cache rows, from `row` or rows[b] on, as float16 into rows
+ * [dst_row, dst_row + t) of K and V (device float16 [batch][Hkv][dst_capacity][D]).
+ * With rows, destination rows whose cache row falls outside [0, capacity) are
+ * left as they were.
+ * Errors: INVALID, CAPACITY (row + t > capacity, rows NULL), HIP. */
+int pariskv_dequantize_rows(const pariskv_config* cfg, const pariskv_quant_cache* cache, int64_t row,
+                            const int32_t* rows, int64_t t, void* K, void* V, int64_t dst_capacity,
+                            int64_t dst_row, int32_t batch, void* stream);
+
+/* pariskv_sparse_attend over the rows of a quantised cache: the attention over
+ * the float16 values the records stand for, in float32.  Entries of idx outside
+ * [0, capacity) are skipped; out is zero when no entry is left.
+ * Errors: INVALID, UNSUPPORTED (k > 4096), HIP. */
+int pariskv_quant_attend(const pariskv_config* cfg, const void* q, const pariskv_quant_cache* cache,
+                         const int32_t* idx, int32_t k, int32_t batch, float scale, float* out, void* stream);
+
+/* pariskv_tiered_attend with the retrieval rows in a quantised cache (entry j
+ * attends its row win->retr_begin + idx[j]) and Sink + Local + Update Buffer
+ * rows in the float16 window cache K_win, V_win.
+ * Errors: those of pariskv_tiered_attend. */
+int pariskv_quant_tiered_attend(const pariskv_config* cfg, const void* q, const void* K_win, const void* V_win,
+                                int64_t win_capacity, const pariskv_quant_cache* cache, const int32_t* idx,
+                                int32_t k, const pariskv_window* win, int32_t batch, float scale, float* out,
+                                void* stream);
+
+/* ------------------------------------------------- several new tokens at a time */
+
+#define PARISKV_MAX_TREE 64 /* largest number of drafted tokens of a sequence */
+
+/* Bytes of the workspace that pariskv_tree_attend and pariskv_quant_tree_attend
+ * need for these sizes (at least 256; 0 on invalid input). */
+size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t n, int32_t t);
+
+/* Verification of drafted tokens (t of every sequence, 1 = a dense decode step):
+ * token i attends the sequence's cached rows and the drafted tokens that its
+ * mask names, its ancestors in the tree of drafts and itself,
+ *   o_i = sum_j softmax_j(scale <k_j, q_i>) v_j.
+ *   q       device float16 [batch][Hq][t][D]
+ *   K, V    device float16 [batch][Hkv][kv_capacity][D], the cached rows
+ *   n       cached rows of every sequence, 0..kv_capacity; with lens (device
+ *           int32 [batch], or NULL) sequence b has min(max(lens[b], 0), n)
+ *   K_tree, V_tree  device float16 [batch][Hkv][t][D], the drafts' own rows
+ *           (not in the cache: which of them stay is known after verification)
+ *   mask    device int64 [batch][t]: bit j of word i lets token i attend draft
+ *           j (bits from t on are ignored); NULL: a chain, drafts j <= i.
+ *           Drafts that no token of their sequence attends may hold anything.
+ *   out     device float [batch][Hq][t][D]; zero where a token attends nothing
+ *   workspace  device, >= pariskv_tree_workspace(...) bytes, 256-byte aligned;
+ *           overwritten, so calls that overlap need one each
+ * t = 0 does nothing.
+ * Errors: INVALID, UNSUPPORTED (t > PARISKV_MAX_TREE), WORKSPACE, HIP. */
+int pariskv_tree_attend(const pariskv_config* cfg, const void* q, const void* K, const void* V,
+                        int64_t kv_capacity, const void* K_tree, const void* V_tree, const int64_t* mask,
+                        int64_t n, const int32_t* lens, int32_t t, int32_t batch, float scale, float* out,
+                        void* workspace, size_t ws_bytes, void* stream);
+
+/* pariskv_tree_attend over a quantised cache in device memory.
+ * Errors: those of pariskv_tree_attend; UNSUPPORTED for a host-mapped cache. */
+int pariskv_quant_tree_attend(const pariskv_config* cfg, const void* q, const pariskv_quant_cache* cache,
+                              const void* K_tree, const void* V_tree, const int64_t* mask, int64_t n,
+                              const int32_t* lens, int32_t t, int32_t batch, float scale, float* out,
+                              void* workspace, size_t ws_bytes, void* stream);
+
+/* Bytes of the workspace that pariskv_sink_window_attend needs for these sizes
+ * (at least 256; 0 on invalid input). */
+size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, int64_t pos, int64_t t,
+                                     int64_t sink, int64_t window);
+
+/* Attention of t new tokens per sequence -- a prompt, a chunk of one, or a
+ * single token -- over a sliding window and the first tokens, which stay
+ * visible: the token at position p attends the cache rows j <= p with j < sink
+ * or j > p - window (window >= pos + t: plain causal attention).
+ *   q       device float16 [batch][Hq][t][D]
+ *   K, V    device float16 [batch][Hkv][kv_capacity][D]: row j holds position j,
+ *           the new tokens' rows among them
+ *   pos     position of the first new token; with starts (device int32 [batch],
+ *           or NULL) that of sequence b is min(max(starts[b], 0), pos)
+ *   counts  device int32 [batch] or NULL: sequence b has min(max(counts[b], 0),
+ *           t) new tokens, the rest of its q is padding, whose rows of out are
+ *           left as they were; cache rows behind its last token are never used
+ *   out     device float16 [batch][Hq][t][D]
+ *   workspace  device, >= pariskv_sink_window_workspace(...) bytes, 256-byte
+ *           aligned; overwritten, so calls that overlap need one each
+ * t = 0 does nothing.
+ * Errors: INVALID (also pos + t > kv_capacity, window < 1), UNSUPPORTED (more
+ * than 2^31-1 blocks), WORKSPACE, HIP. */
+int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const void* K, const void* V,
+                               int64_t kv_capacity, int64_t pos, const int32_t* starts, int64_t t,
+                               const int32_t* counts, int64_t sink, int64_t window, int32_t batch, float scale,
+                               void* out, void* workspace, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------- without a caller workspace */
 
 /* Bytes of the static scratch array pariskv_retrieve_attend_noalloc keeps its

@@ -27,10 +27,11 @@ attention   Exact and candidate-restricted softmax attention
 window      The four decode-time KV regions (Sink, Retrieval, Local, Update
             Buffer) replayed token by token from Sec. "Buffer Update", and
             attention over Sink + retrieved + Local + Buffer rows.
+quant       Block-scaled 8- and 4-bit codes of K/V rows and their records.
 
 Parity status: every function is pinned by a ``-m "not gpu"`` test against
 something other than itself (worked examples, closed forms, brute force,
 hand-computed fixtures or distributional facts).  None is "parity unpinned".
 """
 
-from . import quantizer, rotation, encode, retrieve, attention, window  # noqa: F401
+from . import quantizer, rotation, encode, retrieve, attention, window, quant  # noqa: F401

@@ -22,7 +22,9 @@ __all__ = [
     "retrieve", "retrieve_workspace_size", "workspace_layout", "sparse_attend", "retrieve_attend",
     "retrieve_attend_noalloc", "NOALLOC_SCRATCH_BYTES",
     "window_regions", "window_attend", "retrieve_window_attend", "tiered_attend", "retrieve_tiered_attend",
-    "offload_rows", "window_slot", "group_attend", "quantizer_table", "rotation_signs",
+    "offload_rows", "window_slot", "group_attend", "QuantCache", "quantize_rows", "dequantize_rows",
+    "quant_attend", "quant_tiered_attend", "tree_attend", "quant_tree_attend", "tree_workspace_size",
+    "sink_window_attend", "sink_window_workspace_size", "MAX_TREE", "quantizer_table", "rotation_signs",
     "profile_enable", "profile_reset", "profile_read", "stream_copy", "stream_read",
 ]
 
@@ -33,6 +35,7 @@ ABI_VERSION = 4
 OK, ERR_INVALID, ERR_CAPACITY, ERR_WORKSPACE, ERR_HIP, ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 HEAD_DIM, SUBSPACES, CENTROIDS, REC_BYTES = 128, 16, 256, 128
 MAX_ATTEND_ROWS = 4096
+MAX_TREE = 64
 # Ablation variants (Sec. "Ablation Studies"): Config.flags, Budget.flags.
 NO_ROTATION, NO_ALPHA_CORRECTION = 1, 2
 BINARY_COLLISIONS = 1
@@ -67,6 +70,11 @@ class _Budget(ctypes.Structure):
 class _Window(ctypes.Structure):
     _fields_ = [("sink_len", ctypes.c_int64), ("retr_begin", ctypes.c_int64),
                 ("dense_begin", ctypes.c_int64), ("dense_end", ctypes.c_int64)]
+
+
+class _QuantCache(ctypes.Structure):
+    _fields_ = [("rec", ctypes.c_void_p), ("capacity", ctypes.c_int64), ("k_bits", ctypes.c_int32),
+                ("v_bits", ctypes.c_int32), ("host_mapped", ctypes.c_int32)]
 
 
 class _Layout(ctypes.Structure):
@@ -126,6 +134,24 @@ def lib():
         L.pariskv_group_attend.argtypes = [P(_Config), VP, VP, VP, I32, I64, VP, I32, I32, ctypes.c_float, VP,
                                            VP, VP]
         L.pariskv_offload_rows.argtypes = [VP, VP, I64, I64, VP, VP, I64, I64, I64, I32, I32, VP]
+        F = ctypes.c_float
+        L.pariskv_quant_record_bytes.argtypes = [I32, I32]
+        L.pariskv_quant_record_bytes.restype = SZ
+        L.pariskv_quantize_rows.argtypes = [P(_Config), P(_QuantCache), VP, VP, I64, I64, I64, VP, I64, I32, VP]
+        L.pariskv_dequantize_rows.argtypes = [P(_Config), P(_QuantCache), I64, VP, I64, VP, VP, I64, I64, I32, VP]
+        L.pariskv_quant_attend.argtypes = [P(_Config), VP, P(_QuantCache), VP, I32, I32, F, VP, VP]
+        L.pariskv_quant_tiered_attend.argtypes = [P(_Config), VP, VP, VP, I64, P(_QuantCache), VP, I32, P(_Window),
+                                                  I32, F, VP, VP]
+        L.pariskv_tree_workspace.argtypes = [P(_Config), I32, I64, I32]
+        L.pariskv_tree_workspace.restype = SZ
+        L.pariskv_tree_attend.argtypes = [P(_Config), VP, VP, VP, I64, VP, VP, VP, I64, VP, I32, I32, F, VP, VP, SZ,
+                                          VP]
+        L.pariskv_quant_tree_attend.argtypes = [P(_Config), VP, P(_QuantCache), VP, VP, VP, I64, VP, I32, I32, F, VP,
+                                                VP, SZ, VP]
+        L.pariskv_sink_window_workspace.argtypes = [P(_Config), I32, I64, I64, I64, I64]
+        L.pariskv_sink_window_workspace.restype = SZ
+        L.pariskv_sink_window_attend.argtypes = [P(_Config), VP, VP, VP, I64, I64, VP, I64, VP, I64, I64, I32, F, VP,
+                                                 VP, SZ, VP]
         L.pariskv_stream_copy.argtypes = [VP, VP, SZ, VP]
         L.pariskv_stream_read.argtypes = [VP, SZ, ctypes.c_uint32, VP, VP]
         L.pariskv_quantizer_table.argtypes = [I32, P(ctypes.c_double), P(ctypes.c_double)]
@@ -594,6 +620,247 @@ def offload_rows(K_src, V_src, src_row, K_dst, V_dst, dst_row, t, stream=None):
             raise ValueError(f"{nm} must be device or pinned host memory")
     _check(lib().pariskv_offload_rows(ps[0], ps[1], src_cap, int(src_row), ps[2], ps[3], dst_cap, int(dst_row),
                                       int(t), b, hkv, _stream(stream)))
+
+
+# ---- quantised K/V cache, several new tokens at a time
+
+
+def _require_here(stream, *tensors):
+    """The library launches on the current device: every GPU tensor and the stream must be there."""
+    torch = _torch()
+    here = None
+    for t in tensors:
+        if t is not None and t.is_cuda:
+            if here is None:
+                here = torch.cuda.current_device()
+            if t.device.index != here:
+                raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+    if stream is not None and here is not None and stream.device.index != here:
+        raise ValueError(f"stream on {stream.device}, but the current device is cuda:{here}")
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor the call writes on `stream`, owned by that stream: its memory is not reused before the work there."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class QuantCache:
+    """K/V rows in 8- or 4-bit codes (see ``pariskv_quant_cache``): rec uint8 [batch][Hkv][capacity][record bytes]
+    on the GPU, or in pinned host memory with host_mapped."""
+
+    def __init__(self, rec, k_bits=8, v_bits=8, host_mapped=False):
+        self.rec, self.k_bits, self.v_bits, self.host_mapped = rec, int(k_bits), int(v_bits), bool(host_mapped)
+
+    @staticmethod
+    def record_bytes(k_bits, v_bits):
+        n = int(lib().pariskv_quant_record_bytes(int(k_bits), int(v_bits)))
+        if n == 0:
+            raise ValueError(f"k_bits and v_bits must each be 8 or 4, got {k_bits} and {v_bits}")
+        return n
+
+    @classmethod
+    def empty(cls, cfg, batch, capacity, k_bits=8, v_bits=8, device="cuda", host_mapped=False):
+        torch = _torch()
+        shape = (batch, cfg.n_kv_heads, capacity, cls.record_bytes(k_bits, v_bits))
+        rec = (torch.empty(shape, dtype=torch.uint8, pin_memory=True) if host_mapped else
+               torch.empty(shape, dtype=torch.uint8, device=device))
+        return cls(rec, k_bits, v_bits, host_mapped)
+
+    @property
+    def capacity(self):
+        return int(self.rec.shape[2])
+
+    def c(self, cfg, batch, dev):
+        torch = _torch()
+        bytes_ = self.record_bytes(self.k_bits, self.v_bits)
+        ptr = _arg(self.rec, "cache.rec", torch.uint8, (batch, cfg.n_kv_heads, _rows(self.rec), bytes_),
+                   None if self.host_mapped else dev)
+        if self.host_mapped and (self.rec.is_cuda or not self.rec.is_pinned()):
+            raise ValueError("cache.rec must be pinned host memory when host_mapped")
+        self._c = _QuantCache(ptr, self.capacity, self.k_bits, self.v_bits, int(self.host_mapped))
+        return ctypes.byref(self._c)
+
+
+def _cache_arg(cfg, cache, batch, dev):
+    if not isinstance(cache, QuantCache):
+        raise TypeError("cache must be a QuantCache")
+    return cache.c(cfg, batch, dev)
+
+
+def _row_arg(row, batch, dev):
+    """(row, pointer or None, tensor or None) of a first row: a number, or an int32 GPU tensor [batch]."""
+    torch = _torch()
+    if isinstance(row, torch.Tensor):
+        return 0, _arg(row, "row", torch.int32, (batch,), dev), row
+    return int(row), None, None
+
+
+def _quant_rows(cfg, cache, K, V, row, dev):
+    half = _torch().float16
+    if not isinstance(K, _torch().Tensor) or K.dim() != 4:
+        raise ValueError("K must be a [batch][Hkv][capacity][D] float16 tensor")
+    batch = int(K.shape[0])
+    kp = _arg(K, "K", half, (batch, cfg.n_kv_heads, K.shape[2], HEAD_DIM), dev)
+    vp = _arg(V, "V", half, (batch, cfg.n_kv_heads, K.shape[2], HEAD_DIM), dev)
+    cp = _cache_arg(cfg, cache, batch, dev)
+    return batch, kp, vp, cp, _row_arg(row, batch, dev)
+
+
+def quantize_rows(cfg, cache, K, V, src_row, row, t, stream=None):
+    """Write rows [src_row, src_row + t) of K, V [batch][Hkv][capacity][D] float16 into the quantised cache from row
+    `row` on: a number, or an int32 GPU tensor [batch] with each sequence's (rows outside the cache are skipped)."""
+    dev = []
+    batch, kp, vp, cp, (r, rp, rt) = _quant_rows(cfg, cache, K, V, row, dev)
+    _require_device(dev)
+    _require_here(stream, K, V, cache.rec, rt)
+    _check(lib().pariskv_quantize_rows(cfg.c(), cp, kp, vp, int(K.shape[2]), int(src_row), r, rp, int(t), batch,
+                                       _stream(stream)))
+
+
+def dequantize_rows(cfg, cache, row, t, K, V, dst_row=0, stream=None):
+    """The float16 values of t cache rows from `row` on (as in quantize_rows) into rows [dst_row, dst_row + t) of K, V
+    [batch][Hkv][capacity][D]."""
+    dev = []
+    batch, kp, vp, cp, (r, rp, rt) = _quant_rows(cfg, cache, K, V, row, dev)
+    _require_device(dev)
+    _require_here(stream, K, V, cache.rec, rt)
+    _check(lib().pariskv_dequantize_rows(cfg.c(), cp, r, rp, int(t), kp, vp, int(K.shape[2]), int(dst_row), batch,
+                                         _stream(stream)))
+
+
+def quant_attend(cfg, q, cache, idx, scale, out=None, stream=None):
+    """sparse_attend over the rows idx of a quantised cache; returns out [batch][Hq][D] float32."""
+    torch = _torch()
+    dev = []
+    qp, batch = _q_arg(cfg, q, dev)
+    cp = _cache_arg(cfg, cache, batch, dev)
+    xp, k = _idx_arg(cfg, idx, batch, dev)
+    if out is None:
+        out = _new((batch, cfg.n_q_heads, HEAD_DIM), torch.float32, q.device, stream)
+    out, op = _out_arg(cfg, out, batch, q.device, dev)
+    _require_device(dev)
+    _require_here(stream, q, cache.rec, idx, out)
+    _check(lib().pariskv_quant_attend(cfg.c(), qp, cp, xp, k, batch, float(scale), op, _stream(stream)))
+    return out
+
+
+def quant_tiered_attend(cfg, q, K_win, V_win, cache, idx, win, scale, out=None, stream=None):
+    """tiered_attend with the retrieved rows in a quantised cache."""
+    torch = _torch()
+    dev = []
+    qp, batch = _q_arg(cfg, q, dev)
+    kwp, vwp, wcap = _kv_args(cfg, batch, K_win, V_win, False, dev, ("K_win", "V_win"))
+    cp = _cache_arg(cfg, cache, batch, dev)
+    xp, k = _idx_arg(cfg, idx, batch, dev)
+    if out is None:
+        out = _new((batch, cfg.n_q_heads, HEAD_DIM), torch.float32, q.device, stream)
+    out, op = _out_arg(cfg, out, batch, q.device, dev)
+    _require_device(dev)
+    _require_here(stream, q, K_win, V_win, cache.rec, idx, out)
+    _check(lib().pariskv_quant_tiered_attend(cfg.c(), qp, kwp, vwp, wcap, cp, xp, k, win.c(), batch, float(scale), op,
+                                             _stream(stream)))
+    return out
+
+
+def _tokens_arg(cfg, q, dev):
+    torch = _torch()
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a [batch][Hq][t][D] tensor")
+    batch, t = int(q.shape[0]), int(q.shape[2])
+    return _arg(q, "q", torch.float16, (batch, cfg.n_q_heads, t, HEAD_DIM), dev), batch, t
+
+
+def _tokens_out(q, dtype, out, dev, stream):
+    if out is None:
+        out = _new(tuple(q.shape), dtype, q.device, stream)
+    return out, _arg(out, "out", dtype, tuple(q.shape), dev)
+
+
+def _workspace_arg(workspace, size, q, dev, stream):
+    torch = _torch()
+    if workspace is None:
+        workspace = _new((max(256, size),), torch.uint8, q.device, stream)
+    shape = workspace.shape if isinstance(workspace, torch.Tensor) and workspace.dim() == 1 else (None,)
+    return workspace, _arg(workspace, "workspace", torch.uint8, shape, dev)
+
+
+def tree_workspace_size(cfg, batch, n, t):
+    """Bytes of the workspace of tree_attend and quant_tree_attend (0 on invalid sizes)."""
+    return int(lib().pariskv_tree_workspace(cfg.c(), int(batch), int(n), int(t)))
+
+
+def _tree_args(cfg, q, K_tree, V_tree, n, mask, lens, out, workspace, dev, stream):
+    torch = _torch()
+    qp, batch, t = _tokens_arg(cfg, q, dev)
+    rows = (batch, cfg.n_kv_heads, t, HEAD_DIM)
+    ktp, vtp = _arg(K_tree, "K_tree", torch.float16, rows, dev), _arg(V_tree, "V_tree", torch.float16, rows, dev)
+    mp = _arg(mask, "mask", torch.int64, (batch, t), dev, optional=True)
+    lp = _arg(lens, "lens", torch.int32, (batch,), dev, optional=True)
+    out, op = _tokens_out(q, torch.float32, out, dev, stream)
+    workspace, wp = _workspace_arg(workspace, 0 if workspace is not None else tree_workspace_size(cfg, batch, n, t), q,
+                                   dev, stream)
+    return (qp, ktp, vtp, mp, lp, op, wp), batch, t, out, workspace
+
+
+def tree_attend(cfg, q, K, V, K_tree, V_tree, n, scale, mask=None, lens=None, out=None, workspace=None, stream=None):
+    """Attention of t <= 64 drafted tokens per sequence, q [batch][Hq][t][D], over the n cached rows of K, V
+    [batch][Hkv][kv_capacity][D] (or lens[b] of them, int32 [batch]) and the drafts' own rows K_tree, V_tree
+    [batch][Hkv][t][D]: token i attends draft j when bit j of mask[b, i] (int64 [batch][t]) is set, without a mask when
+    j <= i.  Returns out [batch][Hq][t][D] float32."""
+    dev = []
+    (qp, ktp, vtp, mp, lp, op, wp), batch, t, out, workspace = _tree_args(cfg, q, K_tree, V_tree, n, mask, lens, out,
+                                                                          workspace, dev, stream)
+    kp, vp, cap = _kv_args(cfg, batch, K, V, False, dev)
+    _require_device(dev)
+    _require_here(stream, q, K, V, K_tree, V_tree, mask, lens, out, workspace)
+    _check(lib().pariskv_tree_attend(cfg.c(), qp, kp, vp, cap, ktp, vtp, mp, int(n), lp, t, batch, float(scale), op,
+                                     wp, workspace.numel(), _stream(stream)))
+    return out
+
+
+def quant_tree_attend(cfg, q, cache, K_tree, V_tree, n, scale, mask=None, lens=None, out=None, workspace=None,
+                      stream=None):
+    """tree_attend over the rows of a quantised cache on the GPU."""
+    dev = []
+    (qp, ktp, vtp, mp, lp, op, wp), batch, t, out, workspace = _tree_args(cfg, q, K_tree, V_tree, n, mask, lens, out,
+                                                                          workspace, dev, stream)
+    cp = _cache_arg(cfg, cache, batch, dev)
+    _require_device(dev)
+    _require_here(stream, q, cache.rec, K_tree, V_tree, mask, lens, out, workspace)
+    _check(lib().pariskv_quant_tree_attend(cfg.c(), qp, cp, ktp, vtp, mp, int(n), lp, t, batch, float(scale), op, wp,
+                                           workspace.numel(), _stream(stream)))
+    return out
+
+
+def sink_window_workspace_size(cfg, batch, pos, t, sink, window):
+    """Bytes of the workspace of sink_window_attend (0 on invalid sizes)."""
+    return int(lib().pariskv_sink_window_workspace(cfg.c(), int(batch), int(pos), int(t), int(sink), int(window)))
+
+
+def sink_window_attend(cfg, q, K, V, pos, sink, window, scale, starts=None, counts=None, out=None, workspace=None,
+                       stream=None):
+    """Attention of t new tokens per sequence, q [batch][Hq][t][D] at positions pos .. pos + t - 1, over the cache rows
+    (row = position) of K, V [batch][Hkv][kv_capacity][D] that each sees: j <= p with j < sink or j > p - window.
+    starts (int32 [batch], at most pos) gives each sequence's first position, counts (int32 [batch]) how many of its t
+    tokens there are; rows of out behind them are left as they were.  Returns out [batch][Hq][t][D] float16."""
+    torch = _torch()
+    dev = []
+    qp, batch, t = _tokens_arg(cfg, q, dev)
+    kp, vp, cap = _kv_args(cfg, batch, K, V, False, dev)
+    sp = _arg(starts, "starts", torch.int32, (batch,), dev, optional=True)
+    np_ = _arg(counts, "counts", torch.int32, (batch,), dev, optional=True)
+    out, op = _tokens_out(q, torch.float16, out, dev, stream)
+    size = 0 if workspace is not None else sink_window_workspace_size(cfg, batch, pos, t, sink, window)
+    workspace, wp = _workspace_arg(workspace, size, q, dev, stream)
+    _require_device(dev)
+    _require_here(stream, q, K, V, starts, counts, out, workspace)
+    _check(lib().pariskv_sink_window_attend(cfg.c(), qp, kp, vp, cap, int(pos), sp, t, np_, int(sink), int(window), batch,
+                                            float(scale), op, wp, workspace.numel(), _stream(stream)))
+    return out
 
 
 def stream_copy(dst, src, stream=None):

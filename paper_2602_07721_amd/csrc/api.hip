@@ -14,7 +14,9 @@
 #include <vector>
 
 #include "../../include/pariskv.h"
+#include "chunk_attend.hpp"
 #include "internal.hpp"
+#include "quant.hpp"
 
 namespace pariskv {
 
@@ -835,6 +837,312 @@ int pariskv_offload_rows(const void* K_src, const void* V_src, int64_t src_capac
         if (e != hipSuccess) return hip_fail(e, "hipMemcpy2DAsync");
     }
     return PARISKV_OK;
+}
+
+// ---- quantised cache
+
+size_t pariskv_quant_record_bytes(int32_t k_bits, int32_t v_bits) {
+    if ((k_bits != 8 && k_bits != 4) || (v_bits != 8 && v_bits != 4)) return 0;
+    return (size_t)quant_record_bytes(k_bits, v_bits);
+}
+
+// Checks a quantised cache and gives its records' device address.
+static int check_quant_cache(const pariskv_config* cfg, const pariskv_quant_cache* c, int32_t batch) {
+    if (!c) return fail(PARISKV_ERR_INVALID, "cache is NULL");
+    const size_t bytes = pariskv_quant_record_bytes(c->k_bits, c->v_bits);
+    if (bytes == 0) return fail(PARISKV_ERR_INVALID, "k_bits %d, v_bits %d: each must be 8 or 4", c->k_bits, c->v_bits);
+    if (!c->rec || !aligned16(c->rec)) return fail(PARISKV_ERR_INVALID, "rec must be non-NULL and 16-byte aligned");
+    if (c->capacity < 1 || c->capacity > kMaxKvRows)
+        return fail(PARISKV_ERR_INVALID, "cache capacity %lld outside 1..2^30-1", (long long)c->capacity);
+    if (c->host_mapped != 0 && c->host_mapped != 1) return fail(PARISKV_ERR_INVALID, "host_mapped must be 0 or 1");
+    int64_t n;
+    if (!mul_ok((int64_t)batch * cfg->n_kv_heads, c->capacity, &n) || !mul_ok(n, (int64_t)bytes, &n))
+        return fail(PARISKV_ERR_INVALID, "batch * n_kv_heads * cache capacity overflows");
+    return PARISKV_OK;
+}
+
+static int quant_device_rec(const pariskv_quant_cache* c, uint8_t** rec) {
+    *rec = c->rec;
+    if (!c->host_mapped) return PARISKV_OK;
+    void* p = nullptr;
+    const hipError_t e = hipHostGetDevicePointer(&p, c->rec, 0);
+    if (e != hipSuccess) return hip_fail(e, "hipHostGetDevicePointer(rec)");
+    *rec = static_cast<uint8_t*>(p);
+    return PARISKV_OK;
+}
+
+// The checks that both directions share: t rows of a float16 cache pair from `at` on, t rows of
+// the quantised cache from `row` (rows NULL) on.
+static int check_quant_rows(const pariskv_config* cfg, const pariskv_quant_cache* cache, const void* K, const void* V,
+                            int64_t kv_capacity, int64_t at, int64_t row, const int32_t* rows, int64_t t,
+                            int32_t batch) {
+    int rc = check_config(cfg, batch);
+    if (rc) return rc;
+    if ((rc = check_quant_cache(cfg, cache, batch)) != PARISKV_OK) return rc;
+    if (!K || !V || !aligned16(K) || !aligned16(V))
+        return fail(PARISKV_ERR_INVALID, "K and V must be non-NULL and 16-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(rows) & 3u) != 0) return fail(PARISKV_ERR_INVALID, "rows must be 4-byte aligned");
+    if (kv_capacity < 1 || kv_capacity > INT32_MAX)
+        return fail(PARISKV_ERR_INVALID, "K/V capacity %lld outside 1..2^31-1", (long long)kv_capacity);
+    if (t < 0 || at < 0 || at > kv_capacity - t)
+        return fail(PARISKV_ERR_INVALID, "K/V rows [%lld, %lld + %lld) outside [0, %lld)", (long long)at, (long long)at,
+                    (long long)t, (long long)kv_capacity);
+    if (!rows && row < 0) return fail(PARISKV_ERR_INVALID, "row %lld < 0", (long long)row);
+    if (!rows && row > cache->capacity - t)
+        return fail(PARISKV_ERR_CAPACITY, "rows [%lld, %lld + %lld) exceed cache capacity %lld", (long long)row,
+                    (long long)row, (long long)t, (long long)cache->capacity);
+    return PARISKV_OK;
+}
+
+int pariskv_quantize_rows(const pariskv_config* cfg, const pariskv_quant_cache* cache, const void* K, const void* V,
+                          int64_t src_capacity, int64_t src_row, int64_t row, const int32_t* rows, int64_t t,
+                          int32_t batch, void* stream) {
+    prof_chain_start();
+    int rc = check_quant_rows(cfg, cache, K, V, src_capacity, src_row, row, rows, t, batch);
+    if (rc || t == 0) return rc;
+    uint8_t* rec;
+    if ((rc = quant_device_rec(cache, &rec)) != PARISKV_OK) return rc;
+    const hipError_t e = launch_quantize_rows(
+        static_cast<const char*>(K) + src_row * kD * 2, static_cast<const char*>(V) + src_row * kD * 2, src_capacity, rec,
+        cache->capacity, cache->k_bits, cache->v_bits, row, rows, t, batch, cfg->n_kv_heads,
+        static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "quantize_rows launch");
+}
+
+int pariskv_dequantize_rows(const pariskv_config* cfg, const pariskv_quant_cache* cache, int64_t row,
+                            const int32_t* rows, int64_t t, void* K, void* V, int64_t dst_capacity, int64_t dst_row,
+                            int32_t batch, void* stream) {
+    prof_chain_start();
+    int rc = check_quant_rows(cfg, cache, K, V, dst_capacity, dst_row, row, rows, t, batch);
+    if (rc || t == 0) return rc;
+    uint8_t* rec;
+    if ((rc = quant_device_rec(cache, &rec)) != PARISKV_OK) return rc;
+    const hipError_t e = launch_dequantize_rows(
+        rec, cache->capacity, cache->k_bits, cache->v_bits, row, rows, t, batch, cfg->n_kv_heads,
+        static_cast<char*>(K) + dst_row * kD * 2, static_cast<char*>(V) + dst_row * kD * 2, dst_capacity,
+        static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "dequantize_rows launch");
+}
+
+static int quant_attend_impl(const pariskv_config* cfg, const void* q, const pariskv_quant_cache* cache,
+                             const int32_t* idx, int32_t k, const pariskv_window* win, int32_t batch, float scale,
+                             float* out, const void* Kw, const void* Vw, int64_t win_capacity, void* stream) {
+    prof_chain_start();
+    int rc = check_config(cfg, batch);
+    if (rc) return rc;
+    if ((rc = check_quant_cache(cfg, cache, batch)) != PARISKV_OK) return rc;
+    if (!q || !idx || !out) return fail(PARISKV_ERR_INVALID, "q, idx and out must be non-NULL");
+    if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(idx) & 3u) != 0)
+        return fail(PARISKV_ERR_INVALID, "q and out must be 16-byte aligned, idx 4-byte aligned");
+    if (k < 1) return fail(PARISKV_ERR_INVALID, "k %d < 1", k);
+    if (k > kMaxAttendRows) return fail(PARISKV_ERR_UNSUPPORTED, "k %d above %d", k, kMaxAttendRows);
+    if (!std::isfinite(scale)) return fail(PARISKV_ERR_INVALID, "scale is not finite");
+    AttendWindow aw;
+    if ((rc = check_window(win, cache->capacity, k, -1, win_capacity, &aw)) != PARISKV_OK) return rc;
+    uint8_t* rec;
+    if ((rc = quant_device_rec(cache, &rec)) != PARISKV_OK) return rc;
+    const hipError_t e = launch_quant_attend(q, rec, cache->capacity, cache->k_bits, cache->v_bits, idx, k, batch,
+                                             cfg->n_kv_heads, cfg->q_per_kv, scale, out, aw, Kw, Vw,
+                                             static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "quant_attend launch");
+}
+
+int pariskv_quant_attend(const pariskv_config* cfg, const void* q, const pariskv_quant_cache* cache,
+                         const int32_t* idx, int32_t k, int32_t batch, float scale, float* out, void* stream) {
+    return quant_attend_impl(cfg, q, cache, idx, k, nullptr, batch, scale, out, nullptr, nullptr, 0, stream);
+}
+
+int pariskv_quant_tiered_attend(const pariskv_config* cfg, const void* q, const void* K_win, const void* V_win,
+                                int64_t win_capacity, const pariskv_quant_cache* cache, const int32_t* idx, int32_t k,
+                                const pariskv_window* win, int32_t batch, float scale, float* out, void* stream) {
+    if (!win) return fail(PARISKV_ERR_INVALID, "win must be non-NULL");
+    const int rc = check_window_cache(K_win, V_win, win_capacity);
+    if (rc) return rc;
+    return quant_attend_impl(cfg, q, cache, idx, k, win, batch, scale, out, K_win, V_win, win_capacity, stream);
+}
+
+// ---- several new tokens at a time
+
+static int check_tree_sizes(const pariskv_config* cfg, int32_t batch, int64_t n, int32_t t) {
+    const int rc = check_config(cfg, batch);
+    if (rc) return rc;
+    if (n < 0 || n > kMaxKvRows) return fail(PARISKV_ERR_INVALID, "n %lld outside 0..2^30-1", (long long)n);
+    if (t < 0) return fail(PARISKV_ERR_INVALID, "t %d < 0", t);
+    if (t > PARISKV_MAX_TREE)
+        return fail(PARISKV_ERR_UNSUPPORTED, "%d drafted tokens, above %d", t, PARISKV_MAX_TREE);
+    return PARISKV_OK;
+}
+
+// Bytes of a few-token call's workspace and its number of shares.
+static size_t chunk_workspace(const ChunkArgs& a, int32_t* splits) {
+    const int64_t groups = (int64_t)a.batch * a.hkv, rows = (int64_t)a.g * a.t;
+    *splits = chunk_splits(groups, rows, chunk_keys(a.n, a.t, a.sink, a.window));
+    const size_t bytes = chunk_part_bytes(groups, rows, *splits);
+    return bytes < 256 ? 256 : (bytes + 255) / 256 * 256;
+}
+
+static int check_workspace(const void* workspace, size_t ws_bytes, size_t need) {
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+        return fail(PARISKV_ERR_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
+    if (ws_bytes < need) return fail(PARISKV_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);
+    return PARISKV_OK;
+}
+
+size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t n, int32_t t) {
+    if (check_tree_sizes(cfg, batch, n, t) != PARISKV_OK) return 0;
+    if (t == 0) return 256;
+    ChunkArgs a{};
+    a.batch = batch;
+    a.hkv = cfg->n_kv_heads;
+    a.g = cfg->q_per_kv;
+    a.t = t;
+    a.n = n;
+    return chunk_workspace(a, &a.splits);
+}
+
+static int tree_impl(const pariskv_config* cfg, const void* q, const void* K, const void* V,
+                     const pariskv_quant_cache* cache, int64_t kv_capacity, const void* K_tree, const void* V_tree,
+                     const int64_t* mask, int64_t n, const int32_t* lens, int32_t t, int32_t batch, float scale,
+                     float* out, void* workspace, size_t ws_bytes, void* stream) {
+    prof_chain_start();
+    int rc = check_tree_sizes(cfg, batch, n, t);
+    if (rc) return rc;
+    if (cache) {
+        if ((rc = check_quant_cache(cfg, cache, batch)) != PARISKV_OK) return rc;
+        if (cache->host_mapped)
+            return fail(PARISKV_ERR_UNSUPPORTED, "every row is read: the cache must be in device memory");
+        kv_capacity = cache->capacity;
+    } else {
+        if (!K || !V || !aligned16(K) || !aligned16(V))
+            return fail(PARISKV_ERR_INVALID, "K and V must be non-NULL and 16-byte aligned");
+        if (kv_capacity < 1 || kv_capacity > kMaxKvRows)
+            return fail(PARISKV_ERR_INVALID, "kv_capacity %lld outside 1..2^30-1", (long long)kv_capacity);
+    }
+    if (n > kv_capacity)
+        return fail(PARISKV_ERR_INVALID, "n %lld exceeds capacity %lld", (long long)n, (long long)kv_capacity);
+    if (!std::isfinite(scale)) return fail(PARISKV_ERR_INVALID, "scale is not finite");
+    if (t == 0) return PARISKV_OK;
+    if (!q || !K_tree || !V_tree || !out)
+        return fail(PARISKV_ERR_INVALID, "q, K_tree, V_tree and out must be non-NULL");
+    if (!aligned16(q) || !aligned16(K_tree) || !aligned16(V_tree) || !aligned16(out) ||
+        (reinterpret_cast<uintptr_t>(mask) & 7u) != 0 || (reinterpret_cast<uintptr_t>(lens) & 3u) != 0)
+        return fail(PARISKV_ERR_INVALID,
+                    "q, K_tree, V_tree and out must be 16-byte aligned, mask 8-byte, lens 4-byte");
+    ChunkArgs a{};
+    a.q = q;
+    a.K = K;
+    a.V = V;
+    if (cache) {
+        a.rec = cache->rec;
+        a.k_bits = cache->k_bits;
+        a.v_bits = cache->v_bits;
+    }
+    a.capacity = kv_capacity;
+    a.Kt = K_tree;
+    a.Vt = V_tree;
+    a.mask = mask;
+    a.lens = lens;
+    a.n = n;
+    a.batch = batch;
+    a.hkv = cfg->n_kv_heads;
+    a.g = cfg->q_per_kv;
+    a.t = t;
+    a.scale = scale;
+    a.out = out;
+    const size_t need = chunk_workspace(a, &a.splits);
+    if ((rc = check_workspace(workspace, ws_bytes, need)) != PARISKV_OK) return rc;
+    a.part = static_cast<float*>(workspace);
+    const hipError_t e = launch_chunk_attend(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "tree_attend launch");
+}
+
+int pariskv_tree_attend(const pariskv_config* cfg, const void* q, const void* K, const void* V, int64_t kv_capacity,
+                        const void* K_tree, const void* V_tree, const int64_t* mask, int64_t n, const int32_t* lens,
+                        int32_t t, int32_t batch, float scale, float* out, void* workspace, size_t ws_bytes,
+                        void* stream) {
+    return tree_impl(cfg, q, K, V, nullptr, kv_capacity, K_tree, V_tree, mask, n, lens, t, batch, scale, out, workspace,
+                     ws_bytes, stream);
+}
+
+int pariskv_quant_tree_attend(const pariskv_config* cfg, const void* q, const pariskv_quant_cache* cache,
+                              const void* K_tree, const void* V_tree, const int64_t* mask, int64_t n,
+                              const int32_t* lens, int32_t t, int32_t batch, float scale, float* out, void* workspace,
+                              size_t ws_bytes, void* stream) {
+    if (!cache) return fail(PARISKV_ERR_INVALID, "cache is NULL");
+    return tree_impl(cfg, q, nullptr, nullptr, cache, 0, K_tree, V_tree, mask, n, lens, t, batch, scale, out, workspace,
+                     ws_bytes, stream);
+}
+
+static int check_sink_window_sizes(const pariskv_config* cfg, int32_t batch, int64_t pos, int64_t t, int64_t sink,
+                                   int64_t window) {
+    const int rc = check_config(cfg, batch);
+    if (rc) return rc;
+    if (pos < 0 || t < 0 || pos > kMaxKvRows || t > kMaxKvRows - pos)
+        return fail(PARISKV_ERR_INVALID, "positions [%lld, %lld + %lld) outside [0, 2^30-1)", (long long)pos,
+                    (long long)pos, (long long)t);
+    if (sink < 0 || window < 1)
+        return fail(PARISKV_ERR_INVALID, "sink %lld < 0 or window %lld < 1", (long long)sink, (long long)window);
+    const int64_t heads = (int64_t)batch * cfg->n_kv_heads * cfg->q_per_kv;
+    if (heads * ((t + 127) / 128) > INT32_MAX)
+        return fail(PARISKV_ERR_UNSUPPORTED, "%lld query heads x %lld tokens", (long long)heads, (long long)t);
+    return PARISKV_OK;
+}
+
+static void sink_window_shape(const pariskv_config* cfg, int32_t batch, int64_t pos, int64_t t, int64_t sink,
+                              int64_t window, ChunkArgs* a) {
+    a->batch = batch;
+    a->hkv = cfg->n_kv_heads;
+    a->g = cfg->q_per_kv;
+    a->t = (int32_t)t;
+    a->n = pos;
+    // Rows beyond every position are beyond every sink and window alike.
+    a->sink = sink < kMaxKvRows ? sink : kMaxKvRows;
+    a->window = window < kMaxKvRows ? window : kMaxKvRows;
+}
+
+size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, int64_t pos, int64_t t, int64_t sink,
+                                     int64_t window) {
+    if (check_sink_window_sizes(cfg, batch, pos, t, sink, window) != PARISKV_OK) return 0;
+    ChunkArgs a{};
+    sink_window_shape(cfg, batch, pos, t, sink, window, &a);
+    return t > 0 && few_tokens(a) ? chunk_workspace(a, &a.splits) : 256;
+}
+
+int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const void* K, const void* V,
+                               int64_t kv_capacity, int64_t pos, const int32_t* starts, int64_t t,
+                               const int32_t* counts, int64_t sink, int64_t window, int32_t batch, float scale,
+                               void* out, void* workspace, size_t ws_bytes, void* stream) {
+    prof_chain_start();
+    int rc = check_sink_window_sizes(cfg, batch, pos, t, sink, window);
+    if (rc) return rc;
+    if (kv_capacity < 1 || kv_capacity > kMaxKvRows)
+        return fail(PARISKV_ERR_INVALID, "kv_capacity %lld outside 1..2^30-1", (long long)kv_capacity);
+    if (pos + t > kv_capacity)
+        return fail(PARISKV_ERR_INVALID, "positions [%lld, %lld) exceed kv_capacity %lld", (long long)pos,
+                    (long long)(pos + t), (long long)kv_capacity);
+    if (!std::isfinite(scale)) return fail(PARISKV_ERR_INVALID, "scale is not finite");
+    if (t == 0) return PARISKV_OK;
+    if (!q || !K || !V || !out) return fail(PARISKV_ERR_INVALID, "q, K, V and out must be non-NULL");
+    if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out) ||
+        (reinterpret_cast<uintptr_t>(starts) & 3u) != 0 || (reinterpret_cast<uintptr_t>(counts) & 3u) != 0)
+        return fail(PARISKV_ERR_INVALID, "q, K, V and out must be 16-byte aligned, starts and counts 4-byte");
+    ChunkArgs a{};
+    sink_window_shape(cfg, batch, pos, t, sink, window, &a);
+    a.q = q;
+    a.K = K;
+    a.V = V;
+    a.capacity = kv_capacity;
+    a.lens = starts;
+    a.counts = counts;
+    a.scale = scale;
+    a.out = out;
+    const bool few = few_tokens(a);
+    const size_t need = few ? chunk_workspace(a, &a.splits) : 256;
+    if ((rc = check_workspace(workspace, ws_bytes, need)) != PARISKV_OK) return rc;
+    a.part = static_cast<float*>(workspace);
+    const hipError_t e = few ? launch_chunk_attend(a, static_cast<hipStream_t>(stream))
+                             : launch_prompt_attend(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "sink_window_attend launch");
 }
 
 int pariskv_stream_copy(void* dst, const void* src, size_t bytes, void* stream) {

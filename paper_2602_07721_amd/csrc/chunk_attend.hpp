@@ -1,0 +1,59 @@
+// Attention of a few new tokens per sequence over its cache: drafted tokens with the tree they
+// form (tree_attend), and the few-token form of the sliding window with sinks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "internal.hpp"
+
+namespace pariskv {
+
+// One call.  The t new tokens of a sequence and the g query heads of a KV head are g t rows that
+// read the same keys: row r is head r / t, token r % t.  The keys of a sequence, in order:
+//   rows [0, sink_end) and [lo, hi) of its cache, then the drafts' own rows (Kt, Vt).
+// Tree (window == 0): sink_end = lo = 0, hi = lens[seq] or n; every row sees all of them, and
+// the drafts its mask names.  Sliding window: new token i stands at p = start + i, start =
+// lens[seq] or n; it sees cache rows j <= p with j < sink or j > p - window; no drafts.
+struct ChunkArgs {
+    const void* q;        // float16 [batch][hkv g][t][D]
+    const void* K;        // float16 [batch][hkv][capacity][D], or null with rec
+    const void* V;
+    const uint8_t* rec;   // quantised records [batch][hkv][capacity], or null
+    int32_t k_bits, v_bits;
+    int64_t capacity;
+    const void* Kt;       // float16 [batch][hkv][t][D] (tree)
+    const void* Vt;
+    const int64_t* mask;  // [batch][t] or null: drafts j <= i
+    const int32_t* lens;  // [batch] or null
+    const int32_t* counts;  // new tokens of each sequence [batch] or null: t (sliding window)
+    int64_t n;
+    int64_t sink, window;
+    int32_t batch, hkv, g, t;
+    float scale;
+    void* out;            // [batch][hkv g][t][D], float32 (tree) or float16 (sliding window)
+    float* part;          // chunk_part_bytes
+    int32_t splits;
+};
+
+// Most keys a sequence of the call can have (its size, before any device-side length).
+inline int64_t chunk_keys(int64_t n, int64_t t, int64_t sink, int64_t window) {
+    if (window == 0) return n;
+    const int64_t all = n + t;  // and no more than the sinks and t windows that overlap
+    const int64_t near = window >= all ? all : window + t - 1;
+    return near >= all || sink >= all - near ? all : near + sink;
+}
+// Blocks that share the keys of one (sequence, KV head).
+int32_t chunk_splits(int64_t groups, int64_t rows, int64_t keys);
+size_t chunk_part_bytes(int64_t groups, int64_t rows, int32_t splits);
+hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s);
+
+// Whether the sliding window takes the few-token form: blocks of it share a sequence's keys,
+// blocks of the prompt form hold 128 tokens of a head.
+inline bool few_tokens(const ChunkArgs& a) { return a.t <= 16; }
+
+// The prompt form of the sliding window (many new tokens): the same arguments, float16 out.
+hipError_t launch_prompt_attend(const ChunkArgs& a, hipStream_t s);
+
+}  // namespace pariskv

@@ -353,6 +353,17 @@ hipError_t launch_group_attend(const void* q, const void* K, const void* V, int6
 int32_t group_splits(int64_t groups, int64_t per, int64_t n);
 size_t group_part_bytes(int64_t groups, int32_t splits);
 
+// Rows into and out of a quantised cache (quant.hpp), attention over its records.
+hipError_t launch_quantize_rows(const void* K, const void* V, int64_t src_capacity, uint8_t* rec, int64_t capacity,
+                                int32_t k_bits, int32_t v_bits, int64_t row, const int32_t* rows, int64_t t,
+                                int32_t batch, int32_t hkv, hipStream_t s);
+hipError_t launch_dequantize_rows(const uint8_t* rec, int64_t capacity, int32_t k_bits, int32_t v_bits, int64_t row,
+                                  const int32_t* rows, int64_t t, int32_t batch, int32_t hkv, void* K, void* V,
+                                  int64_t dst_capacity, hipStream_t s);
+hipError_t launch_quant_attend(const void* q, const uint8_t* rec, int64_t capacity, int32_t k_bits, int32_t v_bits,
+                               const int32_t* idx, int32_t k, int32_t batch, int32_t hkv, int32_t g, float scale,
+                               float* out, const AttendWindow& win, const void* Kw, const void* Vw, hipStream_t s);
+
 // Reference streaming kernels (measurement only): a copy and a read of `bytes`.
 hipError_t launch_stream_copy(void* dst, const void* src, size_t bytes, hipStream_t s);
 hipError_t launch_stream_read(const void* src, size_t bytes, uint32_t key, uint32_t* sink, hipStream_t s);

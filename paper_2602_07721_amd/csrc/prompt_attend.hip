@@ -1,0 +1,213 @@
+// Attention of a prompt, or of a long chunk of one, over a sliding window and the first tokens
+// that stay visible: token p sees the rows j <= p with j < sink or j > p - window.
+//
+// A block holds 128 tokens of one query head, 32 a wave, and walks the rows that any of them
+// sees -- the sinks before the windows, then the stretch from the first token's window to the
+// last token -- in tiles of 64 through LDS, two buffers deep.  Per wave and tile:
+//   S^T = K Q^T    matrix instructions of 32 x 32: a lane holds 32 keys' scores of one token, so
+//                  a row's maximum needs one exchange and its sum none until the end,
+//   O^T += V^T P^T the scores' own registers are the second operand (the sum over keys may run in
+//                  any order that both operands agree on); V^T by transposing LDS reads.
+// Tiles inside every token's window take no masks.  Bound by the matrix and vector units
+// together: 4 D flops a visible pair, and an exponential, a maximum, a sum and a rounding.
+
+#include <hip/hip_fp16.h>
+
+#include "chunk_attend_device.hpp"
+
+namespace pariskv {
+
+namespace {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr int kPaThreads = 256;
+constexpr int kPaTokens = 128;  // tokens of a block
+constexpr int kPaKeys = 64;     // keys of a tile
+constexpr float kPaUp = 8.f;    // P is held scaled by 2^8, and grows by up to 2^7 before the
+constexpr float kPaSlack = 7.f; // running maximum is raised: below 2^16, and small P lose nothing
+
+__global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs a, int qtiles) {
+    __shared__ u4v sk[2][kPaKeys * 16];
+    __shared__ u4v sv[2][kPaKeys * 16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+
+    // The tiles with the most keys first (the last tokens of a prompt see the most), and the
+    // heads of one KV head on one XCD, whose L2 then holds their keys.
+    const int64_t groups = (int64_t)a.batch * a.hkv;
+    int64_t id = blockIdx.x;
+    const int64_t per = (int64_t)qtiles * a.g;  // blocks of one (sequence, KV head)
+    int64_t grp, in;
+    const int64_t full = groups / 8 * 8 * per;
+    if (id < full) {
+        grp = id / (8 * per) * 8 + id % 8;
+        in = id / 8 % per;
+    } else {
+        id -= full;
+        grp = full / per + id / per;
+        in = id % per;
+    }
+    const int qt = qtiles - 1 - (int)(in / a.g);
+    const int seq = (int)(grp / a.hkv);
+    const KeySpan whole = key_span(a, seq);
+    const int i0 = qt * kPaTokens;
+    if (i0 >= whole.tokens) return;  // before any barrier, the whole block
+    const int i1 = min(i0 + kPaTokens, whole.tokens);
+    const int64_t p0 = whole.start + i0, hi = whole.start + i1;
+    const int64_t lo = p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
+    const int64_t sink_end = a.sink < lo ? a.sink : lo;
+    const int64_t keys = sink_end + hi - lo;
+    const int tiles = (int)((keys + kPaKeys - 1) / kPaKeys);
+
+    const int64_t head = grp * a.g + in % a.g;  // (seq, query head)
+    const float c2 = score_factor(a.scale);
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    const int tok = min(i0 + 32 * wave + col, i1 - 1);
+    const int64_t p = whole.start + tok;
+    const int64_t wave_first = whole.start + min(i0 + 32 * wave, i1 - 1);
+    const int64_t wave_last = whole.start + min(i0 + 32 * wave + 31, i1 - 1);
+    const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) + (head * a.t + tok) * kD);
+    h8v qf[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) qf[c] = query_part(qr[2 * c + half], flip);
+
+    float nm = __builtin_huge_valf(), sum = 0.f;
+    f16v o[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+    const u4v* Kg = static_cast<const u4v*>(a.K) + grp * a.capacity * 16;
+    const u4v* Vg = static_cast<const u4v*>(a.V) + grp * a.capacity * 16;
+    const int lrow = tid >> 4, lchunk = tid & 15;
+    u4v kr[4], vr[4];
+    auto load = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            int64_t v = (int64_t)tile * kPaKeys + 16 * i + lrow;
+            v = v < keys ? v : keys - 1;
+            const int64_t j = v < sink_end ? v : v - sink_end + lo;
+            kr[i] = Kg[j * 16 + lchunk];
+            vr[i] = Vg[j * 16 + lchunk];
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 16 * i + lrow;
+            sk[buf][r * 16 + (lchunk ^ (r & 15))] = kr[i];
+            sv[buf][r * 16 + (lchunk ^ (4 * (r & 3)))] = vr[i];
+        }
+    };
+    // Where this lane's transposing reads begin: key 4 half + (lane % 16) / 4, dims
+    // 16 (lane / 16 % 2) + 4 (lane % 4).
+    const int tkey = 4 * half + ((lane & 15) >> 2);
+    const int tchunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+
+    load(0);
+    put(0);
+    __syncthreads();
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int buf = tile & 1;
+        if (tile + 1 < tiles) load(tile + 1);
+        const int64_t v0 = (int64_t)tile * kPaKeys, vl = v0 + kPaKeys - 1;
+        const int64_t j0 = v0 - sink_end + lo;
+        // Whether some token of the wave sees a key of the tile, and whether all see all.
+        const bool in_sinks = v0 < sink_end;
+        const bool any = in_sinks || (j0 <= wave_last && (j0 < a.sink || j0 + kPaKeys - 1 > wave_first - a.window));
+        const bool all = vl < keys && (vl < sink_end || (!in_sinks && j0 + kPaKeys - 1 <= wave_first &&
+                                                          j0 > wave_last - a.window));
+        if (any) {
+            f16v s[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
+                const u4v* kp = sk[buf] + (32 * h + col) * 16;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(kp[(2 * c + half) ^ (col & 15)]), qf[c], s[h],
+                                                                  0, 0, 0);
+            }
+            if (!all) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int64_t v = v0 + 32 * h + 8 * (i / 4) + 4 * half + i % 4;
+                        const int64_t j = v < sink_end ? v : v - sink_end + lo;
+                        if (!(v < keys && j <= p && (j < a.sink || j > p - a.window))) s[h][i] = -__builtin_huge_valf();
+                    }
+            }
+            float top = -__builtin_huge_valf();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[h][i]);
+            top *= c2;
+            if (__any(top > -__builtin_huge_valf() && !(top + nm <= kPaUp + kPaSlack))) {
+                const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                const float to = kPaUp - fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+                if (to < nm) {
+                    const float c = __builtin_amdgcn_exp2f(to - nm);
+                    nm = to;
+                    sum *= c;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) o[d] *= c;
+                }
+            }
+            const float base = nm < __builtin_huge_valf() ? nm : 0.f;
+            h8v pf[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], c2, base));
+                    sum += e;
+                    pf[2 * h + i / 8][i % 8] = (_Float16)e;
+                }
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                typedef __attribute__((address_space(3))) s4v* lds_s4;
+                const u4v* vp = sv[buf] + tkey * 16 + ((4 * d + tchunk) ^ (4 * (tkey & 3)));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const char* at = reinterpret_cast<const char*>(vp + 16 * k * 16) + (lane & 1) * 8;
+                    const s4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at));
+                    const s4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + 8 * 256));
+                    const h8v vf = join_h4(a0, a1);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[k], o[d], 0, 0, 0);
+                }
+            }
+        }
+        if (tile + 1 < tiles) put(buf ^ 1);
+        __syncthreads();
+    }
+
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    const float l = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    if (i0 + 32 * wave + col < i1) {
+        h4v* out = static_cast<h4v*>(a.out) + (head * a.t + tok) * (kD / 4);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                out[8 * d + 2 * (i / 4) + half] =
+                    h4v{(_Float16)(o[d][i] * inv), (_Float16)(o[d][i + 1] * inv), (_Float16)(o[d][i + 2] * inv),
+                        (_Float16)(o[d][i + 3] * inv)};
+    }
+}
+
+}  // namespace
+
+hipError_t launch_prompt_attend(const ChunkArgs& a, hipStream_t s) {
+    const int qtiles = (a.t + kPaTokens - 1) / kPaTokens;
+    const ProfEvents pe = prof_begin("sink_window_attend");
+    hipExtLaunchKernelGGL(prompt_attend_kernel, dim3((unsigned)((int64_t)a.batch * a.hkv * a.g * qtiles)),
+                          dim3(kPaThreads), 0, s, pe.start, pe.stop, 0, a, qtiles);
+    return hipGetLastError();
+}
+
+}  // namespace pariskv

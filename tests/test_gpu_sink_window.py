@@ -1,0 +1,130 @@
+"""GPU parity of the attention of new tokens over a sliding window and the first tokens, against float64."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_07721_amd as pk
+import workloads
+from new_tokens import D, SCALE, attend64, check, draw, gpu, tolerance
+
+pytestmark = pytest.mark.gpu
+
+
+def _cfg(hkv, g):
+    return pk.Config(hkv, g, 64, workloads.rotation_signs(3))
+
+
+def _run(b, hkv, g, pos, t, sink, window, starts=None, counts=None, scale=SCALE, seed=0, slack=3):
+    """One call checked in every output; cache rows behind a sequence's last token hold NaN, and rows of out behind its
+    tokens have to stay as they were."""
+    print(f"[sink] batch {b} hkv {hkv} g {g} pos {pos} t {t} sink {sink} window {window} starts {starts} "
+          f"counts {counts}", flush=True)
+    r = np.random.default_rng(seed)
+    cap = pos + t + slack
+    K, V, q = draw(r, b, hkv, cap, D), draw(r, b, hkv, cap, D), draw(r, b, hkv * g, t, D)
+    first = [pos] * b if starts is None else [min(max(x, 0), pos) for x in starts]
+    real = [t] * b if counts is None else [min(max(x, 0), t) for x in counts]
+    for s in range(b):
+        K[s, :, first[s] + real[s]:] = V[s, :, first[s] + real[s]:] = np.nan
+        q[s, :, real[s]:] = np.nan
+    out = torch.full((b, hkv * g, t, D), 7.0, dtype=torch.float16, device="cuda")
+    st = None if starts is None else gpu(np.array(starts, np.int32))
+    ct = None if counts is None else gpu(np.array(counts, np.int32))
+    got = pk.sink_window_attend(_cfg(hkv, g), gpu(q), gpu(K), gpu(V), pos, sink, window, scale, starts=st, counts=ct,
+                                out=out).cpu().numpy()
+    for s in range(b):
+        n, m = first[s] + real[s], real[s]
+        assert (got[s, :, m:] == 7).all(), f"seq {s}: padding was written"
+        if m == 0:
+            continue
+        p, j = np.arange(first[s], n)[:, None], np.arange(n)[None]
+        visible = (j <= p) & ((j < sink) | (j > p - window))
+        for h in range(hkv * g):
+            k_, v_ = K[s, h // g, :n], V[s, h // g, :n]
+            want = attend64(q[s, h, :m], k_, v_, visible, scale)
+            check(got[s, h, :m], want, tolerance(q[s, h, :m], k_, v_, scale, half_out=True), f"seq {s} head {h}")
+
+
+@pytest.mark.parametrize("t", [1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 257, 500])
+@pytest.mark.parametrize("sink,window", [(0, 1), (4, 64), (128, 100)])
+def test_prompts(t, sink, window):
+    _run(1, 2, 2, 0, t, sink, window, seed=t)
+
+
+@pytest.mark.parametrize("pos,t", [(1, 1), (63, 1), (700, 1), (700, 16), (700, 17), (701, 128), (333, 300), (5000, 3)])
+@pytest.mark.parametrize("sink,window", [(0, 64), (4, 63), (128, 512), (1, 1), (0, 100000), (2000, 10)])
+def test_later_chunks(pos, t, sink, window):
+    _run(1, 1, 4, pos, t, sink, window, seed=pos + t)
+
+
+@pytest.mark.parametrize("g", [1, 3, 7, 16])
+@pytest.mark.parametrize("t", [1, 5, 140])
+def test_heads_per_kv_head(g, t):
+    _run(2, 3, g, 400, t, 16, 200, seed=g)
+
+
+@pytest.mark.parametrize("t", [1, 4, 300])
+def test_sequences_that_begin_at_different_positions(t):
+    _run(5, 2, 4, 900, t, 8, 128, starts=[0, 900, 450, -3, 1000], seed=t)
+
+
+@pytest.mark.parametrize("t", [2, 16, 260])
+def test_padded_prompts(t):
+    _run(5, 2, 2, 0, t, 4, 50, counts=[0, 1, t, t - 1, t + 9], seed=t)
+    _run(4, 1, 3, 600, t, 4, 50, starts=[600, 0, 30, 599], counts=[t, 0, 1, -5], seed=t)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0, -0.4])
+@pytest.mark.parametrize("t", [3, 150])
+def test_scales(scale, t):
+    _run(1, 2, 2, 100, t, 4, 64, scale=scale, seed=1)
+
+
+def test_more_than_eight_kv_heads_and_sequences():
+    _run(3, 9, 2, 50, 130, 4, 64, seed=4)
+    _run(5, 7, 1, 300, 2, 4, 64, seed=4)
+
+
+def test_both_forms_agree():
+    # 16 tokens by the few-token form, the same among 40 by the prompt form.
+    b, hkv, g, pos, t = 2, 2, 4, 1000, 40
+    r = np.random.default_rng(3)
+    K, V, q = draw(r, b, hkv, pos + t, D), draw(r, b, hkv, pos + t, D), draw(r, b, hkv * g, t, D)
+    cfg = _cfg(hkv, g)
+    whole = pk.sink_window_attend(cfg, gpu(q), gpu(K), gpu(V), pos, 8, 300, SCALE).cpu().numpy()
+    part = pk.sink_window_attend(cfg, gpu(q[:, :, :16]), gpu(K), gpu(V), pos, 8, 300, SCALE).cpu().numpy()
+    for s in range(b):
+        for h in range(hkv * g):
+            tol = tolerance(q[s, h], K[s, h // g], V[s, h // g], half_out=True)
+            check(whole[s, h, :16], part[s, h].astype(np.float64), 2 * tol, f"seq {s} head {h}")
+
+
+def test_captured_calls_replay():
+    b, hkv, g, pos = 3, 2, 4, 1500
+    r = np.random.default_rng(9)
+    cfg = _cfg(hkv, g)
+    for t in (1, 200):
+        q, K, V = (gpu(x) for x in (draw(r, b, hkv * g, t, D), draw(r, b, hkv, pos + t, D), draw(r, b, hkv, pos + t, D)))
+        starts = torch.zeros(b, dtype=torch.int32, device="cuda")
+        out = torch.zeros_like(q)
+        ws = torch.empty(pk.sink_window_workspace_size(cfg, b, pos, t, 4, 600), dtype=torch.uint8, device="cuda")
+
+        def call():
+            pk.sink_window_attend(cfg, q, K, V, pos, 4, 600, SCALE, starts=starts, out=out, workspace=ws)
+
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        for _ in range(4):
+            starts.copy_(gpu(r.integers(0, pos + 1, b).astype(np.int32)))
+            q.copy_(gpu(draw(r, b, hkv * g, t, D)))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            out.zero_()
+            call()
+            torch.cuda.synchronize()
+            assert torch.equal(got, out)
