@@ -1,8 +1,7 @@
 // Attention of a few new tokens per sequence over a long cache, on matrix instructions.
 //
 // The g heads of a KV head times the t new tokens are M = g t rows over the same keys, so a
-// key's row is read once for 16 NQ of them (NQ tiles of 16 rows a block).  Written for HBM:
-// 4 M flops a byte of a float16 cache.  Per wave and 32 keys:
+// key's row is read once for 16 NQ of them (NQ tiles of 16 rows a block).  Per wave and 32 keys:
 //   S^T = K Q^T    a lane holds 8 keys' scores of one row per tile of 16 rows,
 //   P              exp2 of the scores less the row's running maximum,
 //   O^T += V^T P^T the scores' own registers are the second operand: matrix instructions sum
@@ -32,6 +31,7 @@ constexpr int kCaWaves = kCaThreads / 64;
 constexpr int kCaKeys = 32;            // keys of a wave's step
 constexpr float kCaUp = 8.f;           // P is held scaled by 2^8 ...
 constexpr float kCaSlack = 7.f;        // ... and grows by up to 2^7 before the maximum is raised
+constexpr int64_t kCaBlocks = 1024;     // blocks that a call's keys are shared out to
 constexpr int kCaRow = kD + 4;         // floats of an output row in LDS (spreads the rows over the banks)
 
 constexpr size_t ca_lds_bytes(int nq) {
@@ -53,41 +53,43 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int d
     }
 }
 
-// Registers of 32 keys of a wave, as loaded.  K: lane l holds key l % 16 of each half; V: 8
-// loads of 4 whole rows.
-template <int BITS>
-struct KeyRegs;
-template <>
-struct KeyRegs<16> {
-    u4v k[2][4];
-};
+// Registers of 32 keys of a wave, as loaded.  K: lane l holds key l % 16 of each half, of the
+// dims that step_dim names; V: 8 loads of 4 whole rows.
 template <int BITS>
 struct KeyRegs {
-    u4v k[2][BITS / 4];  // 32 codes of a key's block l / 16
+    u4v k[2][BITS / 4];
     uint32_t scale[2];
-};
-template <int BITS>
-struct ValueRegs;
-template <>
-struct ValueRegs<16> {
-    u4v v[8];
 };
 template <int BITS>
 struct ValueRegs {
     u2v v[8];
     uint32_t scale[8];
 };
+template <>
+struct ValueRegs<16> {
+    u4v v[8];
+};
 
-// QUANT: dims of matrix step c that lane group l / 16 holds start here.  A quantised key's lane
-// group holds one whole block (one scale a lane); a float16 key's four lanes read 64 bytes in a row.
+// Dims of matrix step c that lane group l / 16 holds start here.  A quantised key's lane group
+// holds one whole block (one scale a lane); a float16 key's four lanes read 64 bytes in a row.
 template <bool QUANT>
 __device__ __forceinline__ int step_dim(int c, int grp) {
     return QUANT ? 32 * grp + 8 * c : 32 * c + 8 * grp;
 }
 
+// A step's 32 keys: rows of a float16 cache, of the drafts or of a quantised cache, of which the
+// first `valid` exist.
+struct StepRows {
+    const __half* k;
+    const __half* v;
+    const uint8_t* rec;
+    int valid;
+    int base;    // cache row of key 0
+    int drafts;  // < 0, or the number of the draft that key 0 is
+};
+
 template <int NQ, int KB, int VB, bool WINDOW>
-__global__ __launch_bounds__(kCaThreads, NQ == 4 ? 1 : 2) void chunk_attend_kernel(ChunkArgs a, int mtiles,
-                                                                                    int64_t groups) {
+__global__ __launch_bounds__(kCaThreads, 2) void chunk_attend_kernel(ChunkArgs a, int mtiles, int64_t groups) {
     constexpr bool kQuant = KB < 16;
     constexpr int kRecord = kQuant ? quant_record_bytes(KB, VB) : 0;
     constexpr int kRows = 16 * NQ;
@@ -111,16 +113,19 @@ __global__ __launch_bounds__(kCaThreads, NQ == 4 ? 1 : 2) void chunk_attend_kern
     const int64_t grp = share / a.splits;
     const int split = (int)(share % a.splits);
     const int seq = (int)(grp / a.hkv);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, lg = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, lg = lane >> 4;
     const int M = a.g * a.t, row0 = mt * kRows;
-    const KeySpan span = key_span(a, seq);
+    const KeySpan span = key_span(a, seq, 0, a.t);
 
-    // This share's steps of 32 cached keys, and the drafts behind the last share's.
-    const int64_t steps = (span.keys + kCaKeys - 1) / kCaKeys;
-    const int64_t per = (steps + a.splits - 1) / a.splits;
-    const int64_t first = split * per < steps ? split * per : steps;
-    const int64_t last = first + per < steps ? first + per : steps;
+    // Steps of 32 keys: the sinks', the cached stretch's; this share's part of them, and the
+    // drafts behind the last share's.
+    const int sink_steps = (span.sink_end + kCaKeys - 1) / kCaKeys;
+    const int steps = sink_steps + (span.hi - span.lo + kCaKeys - 1) / kCaKeys;
+    const int per = (steps + a.splits - 1) / a.splits;
+    const int first = min(split * per, steps), last = min(first + per, steps);
     const int draft_steps = (!WINDOW && split == a.splits - 1) ? (a.t + kCaKeys - 1) / kCaKeys : 0;
+    const int end = last + draft_steps;
 
     const float c2 = score_factor(a.scale);
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
@@ -152,31 +157,113 @@ __global__ __launch_bounds__(kCaThreads, NQ == 4 ? 1 : 2) void chunk_attend_kern
     // Where this lane's transposing reads begin: key 4 lg + col / 4 of a half, dims 16 d + 4 (col % 4).
     const int tkey = 4 * lg + (col >> 2);
     const unsigned char* tr = vt + tkey * 256 + ((col & 3) >> 1) * 16 + (col & 1) * 8;
+    // 16 bytes of key `key`'s V (chunk `chunk` of 16) into the wave's LDS.
+    auto put_v = [&](int key, int chunk, h8v v) {
+        *reinterpret_cast<h8v*>(vt + key * 256 + ((chunk ^ (2 * (key & 7))) << 4)) = v;
+    };
 
-    // One step: K operands kf, V in LDS; `seen(x, key)` whether row tile x sees key 0..31.
-    auto step = [&](const h8v (&kf)[2][4], bool all_seen, auto&& seen) {
-        f4v s[NQ][2];
+    auto rows_of = [&](int st) {
+        StepRows r{};
+        r.drafts = -1;
+        if (!WINDOW && st >= last) {
+            r.drafts = (st - last) * kCaKeys;
+            const int64_t at = grp * a.t + r.drafts;
+            r.k = static_cast<const __half*>(a.Kt) + at * kD;
+            r.v = static_cast<const __half*>(a.Vt) + at * kD;
+            r.valid = a.t - r.drafts;
+            return r;
+        }
+        const bool sink = WINDOW && st < sink_steps;
+        r.base = sink ? st * kCaKeys : span.lo + (st - sink_steps) * kCaKeys;
+        r.valid = (sink ? span.sink_end : span.hi) - r.base;
+        const int64_t at = grp * a.capacity + r.base;
+        if constexpr (kQuant) {
+            r.rec = a.rec + at * kRecord;
+        } else {
+            r.k = static_cast<const __half*>(a.K) + at * kD;
+            r.v = static_cast<const __half*>(a.V) + at * kD;
+        }
+        return r;
+    };
+    // Keys past the last repeat it: what lies behind is not read.
+    auto load_k = [&](const StepRows& r, KeyRegs<KB>& kr) {
 #pragma unroll
-        for (int x = 0; x < NQ; ++x)
+        for (int h = 0; h < 2; ++h) {
+            const int key = min(16 * h + col, r.valid - 1);
+            if constexpr (kQuant) {
+                const uint8_t* p = r.rec + key * kRecord;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                s[x][h] = f4v{0.f, 0.f, 0.f, 0.f};
+                for (int c = 0; c < KB / 4; ++c) kr.k[h][c] = reinterpret_cast<const u4v*>(p + lg * (4 * KB))[c];
+                kr.scale[h] = *reinterpret_cast<const uint32_t*>(p + quant_code_bytes(KB) + quant_code_bytes(VB));
+            } else {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h][c], qf[x][c], s[x][h], 0, 0, 0);
+                    kr.k[h][c] = *reinterpret_cast<const u4v*>(r.k + key * kD + step_dim<false>(c, lg));
             }
+        }
+    };
+    auto load_v = [&](const StepRows& r, ValueRegs<VB>& vr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int key = min(4 * i + lg, r.valid - 1);
+            if constexpr (kQuant) {
+                const uint8_t* p = r.rec + key * kRecord + quant_code_bytes(KB);
+                vr.v[i] = quant_load8<VB>(p + col * VB);
+                vr.scale[i] = *reinterpret_cast<const uint32_t*>(p + quant_code_bytes(VB) + 4);
+            } else {
+                vr.v[i] = reinterpret_cast<const u4v*>(r.v + key * kD)[col];
+            }
+        }
+    };
+    auto key_part = [&](const KeyRegs<KB>& kr, int h, int c) {
+        if constexpr (KB == 16) {
+            return as_h8(kr.k[h][c]);
+        } else {
+            const float sc = quant_scale_value((kr.scale[h] >> (8 * lg)) & 255u);
+            if constexpr (KB == 8)
+                return quant_decode8<8>(kr.k[h][c / 2][2 * (c % 2)], kr.k[h][c / 2][2 * (c % 2) + 1], sc);
+            else
+                return quant_decode8<4>(kr.k[h][0][c], 0u, sc);
+        }
+    };
+
+    f4v s[NQ][2];
+    auto scores = [&](auto&& kpart) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const h8v kf = kpart(h, c);
+#pragma unroll
+                for (int x = 0; x < NQ; ++x)
+                    s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                        kf, qf[x][c], c == 0 ? f4v{0.f, 0.f, 0.f, 0.f} : s[x][h], 0, 0, 0);
+            }
+    };
+    // From the step's scores s and its V in LDS; bits of w[x]: the keys that row tile x sees.
+    auto accumulate = [&](const uint32_t (&w)[NQ]) {
+        bool all_seen = true, raise = false;
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) all_seen &= w[x] == ~0u;
+        if (!__all(all_seen)) {
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                const uint32_t b = w[x] >> (4 * lg);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(b & (1u << (16 * h + i)))) s[x][h][i] = -__builtin_huge_valf();
+            }
+        }
         float top[NQ];
-        bool raise = false;
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             top[x] = -__builtin_huge_valf();
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!all_seen && !seen(x, 16 * h + 4 * lg + i)) s[x][h][i] = -__builtin_huge_valf();
-                    top[x] = fmaxf(top[x], s[x][h][i]);
-                }
+                for (int i = 0; i < 4; ++i) top[x] = fmaxf(top[x], s[x][h][i]);
             top[x] *= c2;
             // nm = inf: no key seen yet.
             raise |= top[x] > -__builtin_huge_valf() && !(top[x] + nm[x] <= kCaUp + kCaSlack);
@@ -184,8 +271,7 @@ __global__ __launch_bounds__(kCaThreads, NQ == 4 ? 1 : 2) void chunk_attend_kern
         if (__any(raise)) {
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
-                const float t = rows_max(top[x]);
-                const float to = kCaUp - t;  // inf where the row saw nothing in this step
+                const float to = kCaUp - rows_max(top[x]);  // inf where the row saw nothing in this step
                 if (to < nm[x]) {
                     const float c = __builtin_amdgcn_exp2f(to - nm[x]);  // 0 before the first key
                     nm[x] = to;
@@ -223,139 +309,83 @@ __global__ __launch_bounds__(kCaThreads, NQ == 4 ? 1 : 2) void chunk_attend_kern
             }
         }
     };
-    // 16 bytes of key `key`'s V (chunk `chunk` of 16) into the wave's LDS.
-    auto put_v = [&](int key, int chunk, h8v v) {
-        *reinterpret_cast<h8v*>(vt + key * 256 + ((chunk ^ (2 * (key & 7))) << 4)) = v;
+
+    // Drafts that some token of the sequence sees; the others may hold anything, and count as 0.
+    uint64_t used = ~0ull;
+    const int64_t* masks = !WINDOW && a.mask ? a.mask + (int64_t)seq * a.t : nullptr;
+    if (draft_steps > 0 && masks) {
+        used = lane < a.t ? (uint64_t)masks[lane] : 0ull;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1)
+            used |= (uint64_t)lane_xor((uint32_t)used, m, lane) | (uint64_t)lane_xor((uint32_t)(used >> 32), m, lane) << 32;
+    }
+    auto draft_bits = [&](int x, const StepRows& r) {
+        const uint64_t m = masks ? (uint64_t)masks[tok[x]] : ~0ull >> (63 - tok[x]);
+        return (uint32_t)(m >> r.drafts) & bits_to(r.valid - 1);
     };
 
+    // Quantised kernels take the drafts, which are float16, in a loop of their own.
+    const int main_end = kQuant ? last : end;
     KeyRegs<KB> kr;
     ValueRegs<VB> vr;
-    auto cache_row = [&](int64_t v) {
-        v = v < span.keys ? v : span.keys - 1;
-        return grp * a.capacity + (v < span.sink_end ? v : v - span.sink_end + span.lo);
-    };
-    auto load = [&](int64_t st) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t r = cache_row(st * kCaKeys + 16 * h + col);
-            if constexpr (kQuant) {
-                const uint8_t* p = a.rec + r * kRecord;
-#pragma unroll
-                for (int c = 0; c < KB / 4; ++c)
-                    kr.k[h][c] = reinterpret_cast<const u4v*>(p + lg * (4 * KB))[c];
-                kr.scale[h] = *reinterpret_cast<const uint32_t*>(p + quant_code_bytes(KB) + quant_code_bytes(VB));
-            } else {
-                const u4v* p = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.K) + r * kD) + lg;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) kr.k[h][c] = p[4 * c];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t r = cache_row(st * kCaKeys + 4 * i + lg);
-            if constexpr (kQuant) {
-                const uint8_t* p = a.rec + r * kRecord + quant_code_bytes(KB);
-                vr.v[i] = quant_load8<VB>(p + col * VB);
-                vr.scale[i] = *reinterpret_cast<const uint32_t*>(p + quant_code_bytes(VB) + 4);
-            } else {
-                vr.v[i] = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.V) + r * kD)[col];
-            }
-        }
-    };
-
-    int64_t st = first + wave;
-    if (st < last) load(st);
-    for (; st < last; st += kCaWaves) {
-        h8v kf[2][4];
+    int st = first + wave;
+    StepRows cur{};
+    if (st < main_end) {
+        cur = rows_of(st);
+        load_v(cur, vr);
+        load_k(cur, kr);
+    }
+    for (; st < main_end; st += kCaWaves) {
+        const bool more = st + kCaWaves < main_end;
+        StepRows next = cur;
+        if (more) next = rows_of(st + kCaWaves);
         wave_lds_order();  // the step before has read its V
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (kQuant)
+            if constexpr (kQuant) {
                 put_v(4 * i + lg, col,
                       quant_decode8<VB>(vr.v[i].x, vr.v[i].y,
                                         quant_scale_value((vr.scale[i] >> (8 * (col >> 2))) & 255u)));
-            else
-                put_v(4 * i + lg, col, as_h8(vr.v[i]));
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                if constexpr (kQuant) {
-                    const float sc = quant_scale_value((kr.scale[h] >> (8 * lg)) & 255u);
-                    if constexpr (KB == 8) {
-                        const u4v w = kr.k[h][c / 2];
-                        kf[h][c] = c % 2 ? quant_decode8<8>(w.z, w.w, sc) : quant_decode8<8>(w.x, w.y, sc);
-                    } else {
-                        const u4v w = kr.k[h][0];
-                        kf[h][c] = quant_decode8<4>(c == 0 ? w.x : c == 1 ? w.y : c == 2 ? w.z : w.w, 0u, sc);
-                    }
-                } else {
-                    kf[h][c] = as_h8(kr.k[h][c]);
-                }
+            } else {
+                u4v v = vr.v[i];
+                if (!WINDOW && cur.drafts >= 0 && !((used >> (cur.drafts + 4 * i + lg)) & 1)) v = u4v{0u, 0u, 0u, 0u};
+                put_v(4 * i + lg, col, as_h8(v));
             }
+        }
         wave_lds_order();
-        if (st + kCaWaves < last) load(st + kCaWaves);
-        const int64_t v0 = st * kCaKeys;
-        if constexpr (WINDOW) {
-            // Row of key 0, where the step lies in one stretch of cache rows: seen by all when
-            // every token stands at or behind its last key, and its first key is in the windows.
-            const int64_t lastv = v0 + kCaKeys - 1;
-            const bool sink = lastv < span.sink_end;
-            const int64_t j0 = v0 - span.sink_end + span.lo;
-            const bool all = lastv < span.keys &&
-                             (sink || (v0 >= span.sink_end && j0 + kCaKeys - 1 <= span.start &&
-                                       j0 > span.start + span.tokens - 1 - a.window));
-            step(kf, all, [&](int x, int key) {
-                const int64_t v = v0 + key, p = span.start + tok[x];
-                const int64_t j = v < span.sink_end ? v : v - span.sink_end + span.lo;
-                return v < span.keys && j <= p && (j < a.sink || j > p - a.window);
-            });
-        } else {
-            step(kf, v0 + kCaKeys <= span.keys, [&](int, int key) { return v0 + key < span.keys; });
+        if (more) load_v(next, vr);
+        scores([&](int h, int c) { return key_part(kr, h, c); });
+        if (more) load_k(next, kr);
+        uint32_t w[NQ];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            w[x] = bits_to(cur.valid - 1);
+            if constexpr (WINDOW) w[x] &= window_bits(span.start + tok[x], cur.base, (int)a.sink, (int)a.window);
+            else if (!kQuant && cur.drafts >= 0) w[x] = draft_bits(x, cur);
         }
+        accumulate(w);
+        cur = next;
     }
-
-    if constexpr (!WINDOW) {
-        // The drafts: float16 rows of their own, which tokens see by their masks.
-        const int64_t* masks = a.mask ? a.mask + (int64_t)seq * a.t : nullptr;
-        for (int ds = (int)((wave + kCaWaves - (last - first) % kCaWaves) % kCaWaves); ds < draft_steps;
-             ds += kCaWaves) {
-            uint64_t any = ~0ull;  // drafts that some token sees: the others may hold anything
-            if (masks) {
-                any = lane < a.t ? (uint64_t)masks[lane] : 0ull;
-#pragma unroll
-                for (int m = 1; m < 64; m <<= 1)
-                    any |= (uint64_t)lane_xor((uint32_t)any, m, lane) |
-                           (uint64_t)lane_xor((uint32_t)(any >> 32), m, lane) << 32;
-            }
-            h8v kf[2][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int64_t r = grp * a.t + min(ds * kCaKeys + 16 * h + col, a.t - 1);
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    kf[h][c] = as_h8(*reinterpret_cast<const u4v*>(static_cast<const __half*>(a.Kt) + r * kD +
-                                                                     step_dim<kQuant>(c, lg)));
-            }
+    if constexpr (kQuant) {
+        for (; st < end; st += kCaWaves) {
+            const StepRows r = rows_of(st);
             wave_lds_order();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int j = ds * kCaKeys + 4 * i + lg;
-                u4v v = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.Vt) +
-                                                         (grp * a.t + min(j, a.t - 1)) * kD)[col];
-                if (j >= a.t || !((any >> j) & 1)) v = u4v{0u, 0u, 0u, 0u};
-                put_v(4 * i + lg, col, as_h8(v));
+                const int key = 4 * i + lg;
+                u4v v = reinterpret_cast<const u4v*>(r.v + min(key, r.valid - 1) * kD)[col];
+                if (!((used >> (r.drafts + key)) & 1)) v = u4v{0u, 0u, 0u, 0u};
+                put_v(key, col, as_h8(v));
             }
             wave_lds_order();
-            uint64_t bits[NQ];
-#pragma unroll
-            for (int x = 0; x < NQ; ++x)
-                bits[x] = masks ? (uint64_t)masks[tok[x]] : ~0ull >> (63 - tok[x]);
-            step(kf, false, [&](int x, int key) {
-                const int j = ds * kCaKeys + key;
-                return j < a.t && ((bits[x] >> j) & 1);
+            scores([&](int h, int c) {
+                return as_h8(*reinterpret_cast<const u4v*>(r.k + min(16 * h + col, r.valid - 1) * kD +
+                                                           step_dim<true>(c, lg)));
             });
+            uint32_t w[NQ];
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) w[x] = draft_bits(x, r);
+            accumulate(w);
         }
     }
 
@@ -407,23 +437,48 @@ __global__ __launch_bounds__(kCaThreads, NQ == 4 ? 1 : 2) void chunk_attend_kern
     }
 }
 
-// Joins the shares' states of each row; 32 lanes a row, 8 rows a block.
+// Joins the shares' states of a row: 8 groups of 32 lanes take every eighth share, 4 dims a lane.
+constexpr int kCcGroups = 8;
 template <bool WINDOW>
-__global__ __launch_bounds__(256) void chunk_combine_kernel(ChunkArgs a, int64_t rows) {
-    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row >= rows) return;
-    const int d4 = threadIdx.x & 31;
+__global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs a, int64_t rows) {
+    __shared__ f4v so[kCcGroups][32];
+    __shared__ float snm[kCcGroups], sl[kCcGroups];
+    const int64_t row = blockIdx.x;
+    const int d4 = threadIdx.x & 31, sub = threadIdx.x >> 5;
     const int M = a.g * a.t;
     const float* ml = a.part + rows * a.splits * kD + 2 * row * a.splits;
-    float top = __builtin_huge_valf();
-    for (int s = 0; s < a.splits; ++s) top = fminf(top, ml[2 * s]);
-    float l = 0.f;
+    const f4v* part = reinterpret_cast<const f4v*>(a.part) + row * a.splits * (kD / 4) + d4;
+    float top = __builtin_huge_valf(), l = 0.f;
     f4v acc{0.f, 0.f, 0.f, 0.f};
+    for (int s = sub; s < a.splits; s += kCcGroups) {
+        const float nm = ml[2 * s], ls = ml[2 * s + 1];
+        const f4v v = part[s * (kD / 4)];
+        const float to = fminf(top, nm);
+        if (to < __builtin_huge_valf()) {
+            const float c0 = __builtin_amdgcn_exp2f(to - top), c1 = __builtin_amdgcn_exp2f(to - nm);
+            l = l * c0 + ls * c1;
+            acc = acc * c0 + v * c1;
+            top = to;
+        }
+    }
+    so[sub][d4] = acc;
+    if (d4 == 0) {
+        snm[sub] = top;
+        sl[sub] = l;
+    }
+    __syncthreads();
+    if (sub != 0) return;
+    top = __builtin_huge_valf();
+#pragma unroll
+    for (int i = 0; i < kCcGroups; ++i) top = fminf(top, snm[i]);
+    l = 0.f;
+    acc = f4v{0.f, 0.f, 0.f, 0.f};
     if (top < __builtin_huge_valf())
-        for (int s = 0; s < a.splits; ++s) {
-            const float c = __builtin_amdgcn_exp2f(top - ml[2 * s]);
-            l += c * ml[2 * s + 1];
-            acc += c * reinterpret_cast<const f4v*>(a.part)[(row * a.splits + s) * (kD / 4) + d4];
+#pragma unroll
+        for (int i = 0; i < kCcGroups; ++i) {
+            const float c = __builtin_amdgcn_exp2f(top - snm[i]);
+            l += c * sl[i];
+            acc += c * so[i][d4];
         }
     bool real = true;
     if (WINDOW && a.counts) real = (int)(row % M) % a.t < a.counts[row / M / a.hkv];
@@ -432,13 +487,14 @@ __global__ __launch_bounds__(256) void chunk_combine_kernel(ChunkArgs a, int64_t
 
 }  // namespace
 
+// 16 or 32 rows a block: 64 would need every register of a SIMD for one wave.
+static int chunk_row_tiles(int64_t rows) { return rows <= 16 ? 1 : 2; }
+
 int32_t chunk_splits(int64_t groups, int64_t rows, int64_t keys) {
-    // Rounds of the chip's 256 CUs, with one block of 64 rows a CU, 2 of 32, 4 of 16; a share is
-    // no shorter than 2 steps of every wave.
-    const int64_t per_cu = rows <= 16 ? 4 : rows <= 32 ? 2 : 1;
-    const int64_t mtiles = (rows + 63) / 64;
-    int64_t s = (256 * per_cu + groups * mtiles - 1) / (groups * mtiles);
-    const int64_t most = keys / (2 * kCaWaves * kCaKeys);
+    const int64_t nq = chunk_row_tiles(rows), mtiles = (rows + 16 * nq - 1) / (16 * nq);
+    const int64_t want = kCaBlocks;
+    int64_t s = (want + groups * mtiles - 1) / (groups * mtiles);
+    const int64_t most = keys / (2 * kCaWaves * kCaKeys);  // no shorter than 2 steps of every wave
     if (s > most) s = most;
     if (s > 256) s = 256;
     return (int32_t)(s < 1 ? 1 : s);
@@ -451,41 +507,35 @@ size_t chunk_part_bytes(int64_t groups, int64_t rows, int32_t splits) {
 hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s) {
     const int64_t groups = (int64_t)a.batch * a.hkv;
     const int M = a.g * a.t;
-    const int nq = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+    const int nq = chunk_row_tiles(M);
     const int mtiles = (M + 16 * nq - 1) / (16 * nq);
     const dim3 grid((unsigned)(groups * a.splits * mtiles));
     ProfEvents pe = prof_begin(a.window > 0 ? "sink_window_attend" : a.rec ? "quant_tree_attend" : "tree_attend");
     auto go = [&](auto kernel) {
         hipExtLaunchKernelGGL(kernel, grid, dim3(kCaThreads), 0, s, pe.start, pe.stop, 0, a, mtiles, groups);
     };
-    auto rows = [&](auto k1, auto k2, auto k4) { nq == 1 ? go(k1) : nq == 2 ? go(k2) : go(k4); };
+    auto rows = [&](auto k1, auto k2) { nq == 1 ? go(k1) : go(k2); };
     if (a.window > 0)
-        rows(chunk_attend_kernel<1, 16, 16, true>, chunk_attend_kernel<2, 16, 16, true>,
-             chunk_attend_kernel<4, 16, 16, true>);
+        rows(chunk_attend_kernel<1, 16, 16, true>, chunk_attend_kernel<2, 16, 16, true>);
     else if (!a.rec)
-        rows(chunk_attend_kernel<1, 16, 16, false>, chunk_attend_kernel<2, 16, 16, false>,
-             chunk_attend_kernel<4, 16, 16, false>);
+        rows(chunk_attend_kernel<1, 16, 16, false>, chunk_attend_kernel<2, 16, 16, false>);
     else if (a.k_bits == 8 && a.v_bits == 8)
-        rows(chunk_attend_kernel<1, 8, 8, false>, chunk_attend_kernel<2, 8, 8, false>,
-             chunk_attend_kernel<4, 8, 8, false>);
+        rows(chunk_attend_kernel<1, 8, 8, false>, chunk_attend_kernel<2, 8, 8, false>);
     else if (a.k_bits == 8)
-        rows(chunk_attend_kernel<1, 8, 4, false>, chunk_attend_kernel<2, 8, 4, false>,
-             chunk_attend_kernel<4, 8, 4, false>);
+        rows(chunk_attend_kernel<1, 8, 4, false>, chunk_attend_kernel<2, 8, 4, false>);
     else if (a.v_bits == 8)
-        rows(chunk_attend_kernel<1, 4, 8, false>, chunk_attend_kernel<2, 4, 8, false>,
-             chunk_attend_kernel<4, 4, 8, false>);
+        rows(chunk_attend_kernel<1, 4, 8, false>, chunk_attend_kernel<2, 4, 8, false>);
     else
-        rows(chunk_attend_kernel<1, 4, 4, false>, chunk_attend_kernel<2, 4, 4, false>,
-             chunk_attend_kernel<4, 4, 4, false>);
+        rows(chunk_attend_kernel<1, 4, 4, false>, chunk_attend_kernel<2, 4, 4, false>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t all = groups * M;
-    const dim3 cgrid((unsigned)((all + 7) / 8));
+    const dim3 cgrid((unsigned)all);
     pe = prof_begin("chunk_combine");
     if (a.window > 0)
-        hipExtLaunchKernelGGL(chunk_combine_kernel<true>, cgrid, dim3(256), 0, s, pe.start, pe.stop, 0, a, all);
+        hipExtLaunchKernelGGL(chunk_combine_kernel<true>, cgrid, dim3(32 * kCcGroups), 0, s, pe.start, pe.stop, 0, a, all);
     else
-        hipExtLaunchKernelGGL(chunk_combine_kernel<false>, cgrid, dim3(256), 0, s, pe.start, pe.stop, 0, a, all);
+        hipExtLaunchKernelGGL(chunk_combine_kernel<false>, cgrid, dim3(32 * kCcGroups), 0, s, pe.start, pe.stop, 0, a, all);
     return hipGetLastError();
 }
 

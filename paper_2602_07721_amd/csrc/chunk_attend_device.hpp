@@ -45,34 +45,40 @@ __device__ __forceinline__ float score_factor(float scale) {
     return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f);
 }
 
-// Keys of one (sequence, KV head), as the kernel walks them.
+// Bits 0..x of a word (none for x < 0).
+__device__ __forceinline__ uint32_t bits_to(int x) { return x < 0 ? 0u : x >= 31 ? ~0u : (2u << x) - 1u; }
+
+// Which of 32 keys at cache rows base, base + 1, ... the token at position p sees.
+__device__ __forceinline__ uint32_t window_bits(int p, int base, int sink, int window) {
+    return bits_to(p - base) & (bits_to(sink - 1 - base) | ~bits_to(p - window - base));
+}
+
+// The cache rows that some tokens of a sequence see: [0, sink_end) and [lo, hi), with the first
+// token's position (sliding window; sink_end = lo = 0 in a tree).
 struct KeySpan {
-    int64_t sink_end, lo, keys;  // cached key v: row v below sink_end, else v - sink_end + lo
-    int64_t start;               // position of new token 0 (sliding window)
-    int32_t tokens;              // new tokens
+    int sink_end, lo, hi;
+    int start;
+    int tokens;  // new tokens
 };
 
-__device__ __forceinline__ KeySpan key_span(const ChunkArgs& a, int seq) {
+// Of tokens [i0, i1) of sequence seq, at most the tokens there are.
+__device__ __forceinline__ KeySpan key_span(const ChunkArgs& a, int seq, int i0, int i1) {
     KeySpan s;
-    int64_t len = a.n;
-    if (a.lens) {
-        const int64_t v = a.lens[seq];
-        len = v < 0 ? 0 : v < a.n ? v : a.n;
-    }
-    s.tokens = a.t;
-    if (a.counts) {
-        const int32_t v = a.counts[seq];
-        s.tokens = v < 0 ? 0 : v < a.t ? v : a.t;
-    }
+    const int n = (int)a.n;
+    const int len = a.lens ? min(max(a.lens[seq], 0), n) : n;
+    s.tokens = a.counts ? min(max(a.counts[seq], 0), a.t) : a.t;
     s.start = len;
     s.sink_end = s.lo = 0;
-    s.keys = len;
+    s.hi = len;
     if (a.window > 0) {
-        const int64_t hi = s.tokens > 0 ? len + s.tokens : 0;
-        s.lo = len - a.window + 1 > 0 ? len - a.window + 1 : 0;
-        if (s.lo > hi) s.lo = hi;
-        s.sink_end = a.sink < s.lo ? a.sink : s.lo;
-        s.keys = s.sink_end + hi - s.lo;
+        i1 = min(i1, s.tokens);
+        if (i0 >= i1) {
+            s.hi = 0;
+        } else {
+            s.hi = len + i1;
+            s.lo = max(0, len + i0 - (int)a.window + 1);
+            s.sink_end = min((int)a.sink, s.lo);
+        }
     }
     return s;
 }

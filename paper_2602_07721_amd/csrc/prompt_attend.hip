@@ -49,23 +49,22 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     }
     const int qt = qtiles - 1 - (int)(in / a.g);
     const int seq = (int)(grp / a.hkv);
-    const KeySpan whole = key_span(a, seq);
     const int i0 = qt * kPaTokens;
-    if (i0 >= whole.tokens) return;  // before any barrier, the whole block
-    const int i1 = min(i0 + kPaTokens, whole.tokens);
-    const int64_t p0 = whole.start + i0, hi = whole.start + i1;
-    const int64_t lo = p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
-    const int64_t sink_end = a.sink < lo ? a.sink : lo;
-    const int64_t keys = sink_end + hi - lo;
-    const int tiles = (int)((keys + kPaKeys - 1) / kPaKeys);
+    const KeySpan span = key_span(a, seq, i0, i0 + kPaTokens);
+    if (i0 >= span.tokens) return;  // before any barrier, the whole block
+    const int i1 = min(i0 + kPaTokens, span.tokens);
+    const int sink = (int)a.sink, window = (int)a.window;
+    // Tiles of 64 keys: the sinks', then the stretch's.
+    const int sink_tiles = (span.sink_end + kPaKeys - 1) / kPaKeys;
+    const int tiles = sink_tiles + (span.hi - span.lo + kPaKeys - 1) / kPaKeys;
 
     const int64_t head = grp * a.g + in % a.g;  // (seq, query head)
     const float c2 = score_factor(a.scale);
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
     const int tok = min(i0 + 32 * wave + col, i1 - 1);
-    const int64_t p = whole.start + tok;
-    const int64_t wave_first = whole.start + min(i0 + 32 * wave, i1 - 1);
-    const int64_t wave_last = whole.start + min(i0 + 32 * wave + 31, i1 - 1);
+    const int p = span.start + tok;
+    const int wave_first = span.start + min(i0 + 32 * wave, i1 - 1);
+    const int wave_last = span.start + min(i0 + 32 * wave + 31, i1 - 1);
     const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) + (head * a.t + tok) * kD);
     h8v qf[8];
 #pragma unroll
@@ -82,14 +81,20 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     const u4v* Vg = static_cast<const u4v*>(a.V) + grp * a.capacity * 16;
     const int lrow = tid >> 4, lchunk = tid & 15;
     u4v kr[4], vr[4];
+    // First row of a tile, and how many of its keys there are.
+    auto tile_base = [&](int tile) {
+        return tile < sink_tiles ? tile * kPaKeys : span.lo + (tile - sink_tiles) * kPaKeys;
+    };
+    auto tile_keys = [&](int tile) { return (tile < sink_tiles ? span.sink_end : span.hi) - tile_base(tile); };
+    // Keys past the last repeat it: what lies behind is not read.
     auto load = [&](int tile) {
+        const int64_t base = (int64_t)tile_base(tile) * 16;
+        const int most = tile_keys(tile) - 1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            int64_t v = (int64_t)tile * kPaKeys + 16 * i + lrow;
-            v = v < keys ? v : keys - 1;
-            const int64_t j = v < sink_end ? v : v - sink_end + lo;
-            kr[i] = Kg[j * 16 + lchunk];
-            vr[i] = Vg[j * 16 + lchunk];
+            const int at = min(16 * i + lrow, most) * 16 + lchunk;
+            kr[i] = (Kg + base)[at];
+            vr[i] = (Vg + base)[at];
         }
     };
     auto put = [&](int buf) {
@@ -111,13 +116,11 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     for (int tile = 0; tile < tiles; ++tile) {
         const int buf = tile & 1;
         if (tile + 1 < tiles) load(tile + 1);
-        const int64_t v0 = (int64_t)tile * kPaKeys, vl = v0 + kPaKeys - 1;
-        const int64_t j0 = v0 - sink_end + lo;
-        // Whether some token of the wave sees a key of the tile, and whether all see all.
-        const bool in_sinks = v0 < sink_end;
-        const bool any = in_sinks || (j0 <= wave_last && (j0 < a.sink || j0 + kPaKeys - 1 > wave_first - a.window));
-        const bool all = vl < keys && (vl < sink_end || (!in_sinks && j0 + kPaKeys - 1 <= wave_first &&
-                                                          j0 > wave_last - a.window));
+        const int base_row = tile_base(tile), valid = tile_keys(tile);
+        // Whether some token of the wave sees a key of the tile (its first key is at or before the
+        // last token, and its first token's window or the sinks reach into it).
+        const bool any = base_row <= wave_last &&
+                         (base_row < sink || base_row + kPaKeys - 1 > wave_first - window);
         if (any) {
             f16v s[2];
 #pragma unroll
@@ -130,15 +133,18 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
                     s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(kp[(2 * c + half) ^ (col & 15)]), qf[c], s[h],
                                                                   0, 0, 0);
             }
-            if (!all) {
+            uint32_t w[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
+                w[h] = bits_to(valid - 1 - 32 * h) & window_bits(p, base_row + 32 * h, sink, window);
+            if (!__all((w[0] & w[1]) == ~0u)) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int64_t v = v0 + 32 * h + 8 * (i / 4) + 4 * half + i % 4;
-                        const int64_t j = v < sink_end ? v : v - sink_end + lo;
-                        if (!(v < keys && j <= p && (j < a.sink || j > p - a.window))) s[h][i] = -__builtin_huge_valf();
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t b = w[h] >> (4 * half);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(b & (1u << (8 * (i / 4) + i % 4)))) s[h][i] = -__builtin_huge_valf();
+                }
             }
             float top = -__builtin_huge_valf();
 #pragma unroll
