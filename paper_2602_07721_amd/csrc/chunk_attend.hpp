@@ -48,6 +48,9 @@ inline int64_t chunk_keys(int64_t n, int64_t t, int64_t sink, int64_t window) {
 int32_t chunk_splits(int64_t groups, int64_t rows, int64_t keys);
 size_t chunk_part_bytes(int64_t groups, int64_t rows, int32_t splits);
 hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s);
+// Its first kernel for blocks of 64 or 128 rows (tile_attend.hip).
+hipError_t launch_tile_attend(const ChunkArgs& a, int block, int row_tiles, int64_t groups, const char* name,
+                              hipStream_t s);
 
 // Whether the sliding window takes the few-token form: blocks of it share a sequence's keys,
 // blocks of the prompt form hold 128 tokens of a head.

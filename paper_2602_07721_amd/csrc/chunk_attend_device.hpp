@@ -83,4 +83,243 @@ __device__ __forceinline__ KeySpan key_span(const ChunkArgs& a, int seq, int i0,
     return s;
 }
 
+// ---- few new tokens: a wave's 16 NQ rows over steps of 32 keys
+
+constexpr int kCaKeys = 32;      // keys of a step
+constexpr float kCaUp = 8.f;     // P is held scaled by 2^8 ...
+constexpr float kCaSlack = 7.f;  // ... and grows by up to 2^7 before the maximum is raised
+constexpr int kCaRow = kD + 4;   // floats of an output row in LDS (spreads the rows over the banks)
+// LDS of a wave's outputs [row][kCaRow], maxima and sums.
+constexpr int ca_state_bytes(int nq) { return 16 * nq * (kCaRow + 2) * 4; }
+
+// What a block works on: rows [row0, ...) of a (sequence, KV head)'s g t, share `split` of the keys.
+struct ChunkPlace {
+    int64_t grp;
+    int split, seq, tile;
+};
+// Consecutive blocks go to the 8 XCDs in turn: the row tiles of one share of the keys are 8
+// apart, so that one XCD's L2 serves them all.
+__device__ __forceinline__ ChunkPlace chunk_place(const ChunkArgs& a, int row_tiles, int64_t groups) {
+    ChunkPlace p;
+    int64_t id = blockIdx.x, share;
+    const int64_t shares = groups * a.splits;
+    const int64_t full = shares / 8 * 8 * row_tiles;
+    if (id < full) {
+        share = id / (8 * row_tiles) * 8 + id % 8;
+        p.tile = (int)(id / 8 % row_tiles);
+    } else {
+        id -= full;
+        share = full / row_tiles + id / row_tiles;
+        p.tile = (int)(id % row_tiles);
+    }
+    p.grp = share / a.splits;
+    p.split = (int)(share % a.splits);
+    p.seq = (int)(p.grp / a.hkv);
+    return p;
+}
+
+// Drafts that some token of the sequence sees, bit by bit; the others may hold anything.  Every
+// lane of the wave calls it.
+__device__ __forceinline__ uint64_t used_drafts(const ChunkArgs& a, int seq, int lane) {
+    if (!a.mask) return ~0ull;
+    uint64_t used = lane < a.t ? (uint64_t)a.mask[(int64_t)seq * a.t + lane] : 0ull;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1)
+        used |= (uint64_t)lane_xor((uint32_t)used, m, lane) | (uint64_t)lane_xor((uint32_t)(used >> 32), m, lane) << 32;
+    return used;
+}
+// Which of the drafts first, first + 1, ... (valid of them) token tok sees.
+__device__ __forceinline__ uint32_t draft_bits(const ChunkArgs& a, int seq, int tok, int first, int valid) {
+    const uint64_t m = a.mask ? (uint64_t)a.mask[(int64_t)seq * a.t + tok] : ~0ull >> (63 - tok);
+    return first > 63 ? 0u : (uint32_t)(m >> first) & bits_to(valid - 1);
+}
+
+// 16 bytes of key `key`'s V (chunk `chunk` of 16) in a tile of V in LDS.  The XOR spreads the 16
+// rows of a transposing read over all banks.
+__device__ __forceinline__ void put_v(unsigned char* vt, int key, int chunk, h8v v) {
+    *reinterpret_cast<h8v*>(vt + key * 256 + ((chunk ^ (2 * (key & 7))) << 4)) = v;
+}
+
+// The softmax of NQ tiles of 16 rows.  Lane l = col + 16 lg: row col of each tile.
+template <int NQ>
+struct ChunkRows {
+    // A row's running maximum m as nm = 8 - m (P = 2^(c2 s + nm); infinite before the first key),
+    // its sum over this lane's keys, its outputs: dims 16 d + 4 lg + i.
+    float nm[NQ], sum[NQ], c2;
+    f4v o[NQ][8];
+    // A step's scores: keys 16 h + 4 lg + i.
+    f4v s[NQ][2];
+
+    __device__ __forceinline__ void init(float factor) {
+        c2 = factor;
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            nm[x] = __builtin_huge_valf();
+            sum[x] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) o[x][d] = f4v{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // S^T = K Q^T of 32 keys: kpart(h, c) gives the operand of half h, matrix step c.
+    template <class F>
+    __device__ __forceinline__ void scores(const h8v (&qf)[NQ][4], F&& kpart) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const h8v kf = kpart(h, c);
+#pragma unroll
+                for (int x = 0; x < NQ; ++x)
+                    s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                        kf, qf[x][c], c == 0 ? f4v{0.f, 0.f, 0.f, 0.f} : s[x][h], 0, 0, 0);
+            }
+    }
+
+    // O^T += V^T P^T from the scores and the step's V in LDS; bits of w[x]: the keys row tile x
+    // sees.  tkey = 4 lg + col / 4 and tr = where this lane's transposing reads of V begin.
+    __device__ __forceinline__ void accumulate(const uint32_t (&w)[NQ], const unsigned char* tr, int tkey, int lg) {
+        bool all_seen = true, raise = false;
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) all_seen &= w[x] == ~0u;
+        if (!__all(all_seen)) {
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                const uint32_t b = w[x] >> (4 * lg);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(b & (1u << (16 * h + i)))) s[x][h][i] = -__builtin_huge_valf();
+            }
+        }
+        float top[NQ];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            top[x] = -__builtin_huge_valf();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top[x] = fmaxf(top[x], s[x][h][i]);
+            top[x] *= c2;
+            raise |= top[x] > -__builtin_huge_valf() && !(top[x] + nm[x] <= kCaUp + kCaSlack);
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                const float to = kCaUp - rows_max(top[x]);  // inf where the row saw nothing in this step
+                if (to < nm[x]) {
+                    const float c = __builtin_amdgcn_exp2f(to - nm[x]);  // 0 before the first key
+                    nm[x] = to;
+                    sum[x] *= c;
+#pragma unroll
+                    for (int d = 0; d < 8; ++d) o[x][d] *= c;
+                }
+            }
+        }
+        h8v hi[NQ], lo[NQ];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            const float base = nm[x] < __builtin_huge_valf() ? nm[x] : 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][h][i], c2, base));
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][h][i + 1], c2, base));
+                    sum[x] += p0 + p1;
+                    // Two values an instruction; p - hi is exact.
+                    const h2v ph = __builtin_convertvector((f2v{p0, p1}), h2v);
+                    const h2v pl = __builtin_convertvector((f2v{__builtin_fmaf((float)ph[0], -1.f, p0),
+                                                                __builtin_fmaf((float)ph[1], -1.f, p1)}), h2v);
+                    hi[x][4 * h + i] = ph[0];
+                    hi[x][4 * h + i + 1] = ph[1];
+                    lo[x][4 * h + i] = pl[0];
+                    lo[x][4 * h + i + 1] = pl[1];
+                }
+        }
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+            typedef __attribute__((address_space(3))) s4v* lds_s4;
+            const unsigned char* at = tr + ((d ^ (tkey & 7)) << 5);
+            const s4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at));
+            const s4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + 16 * 256));
+            const h8v vf = join_h4(v0, v1);
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, hi[x], o[x][d], 0, 0, 0);
+                o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, lo[x], o[x][d], 0, 0, 0);
+            }
+        }
+    }
+
+    // Leaves the state in ca_state_bytes(NQ) of LDS.
+    __device__ __forceinline__ void leave(unsigned char* to, int col, int lg) const {
+        float* so = reinterpret_cast<float*>(to);
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            const float l = rows_sum(sum[x]);
+            const int r = 16 * x + col;
+            if (lg == 0) {
+                so[16 * NQ * kCaRow + r] = nm[x];
+                so[16 * NQ * (kCaRow + 1) + r] = l;
+            }
+#pragma unroll
+            for (int d = 0; d < 8; ++d) *reinterpret_cast<f4v*>(so + r * kCaRow + 16 * d + 4 * lg) = o[x][d];
+        }
+    }
+};
+
+// 4 dims of an output row: float32, or float16 where the prompt's next product reads it.  Rows
+// of tokens that are not there are left as they were.
+template <bool WINDOW>
+__device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int d4, float inv, f4v acc, bool real) {
+    acc *= inv;
+    if constexpr (WINDOW) {
+        const h4v h{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
+        if (real) static_cast<h4v*>(a.out)[row * (kD / 4) + d4] = h;
+    } else {
+        static_cast<f4v*>(a.out)[row * (kD / 4) + d4] = acc;
+    }
+}
+
+// Joins the states that WAVES waves left `stride` bytes apart for rows [row0, row0 + 16 NQ) of
+// group grp, and writes the rows, or the share's part of them.  32 lanes a row, 4 dims a lane;
+// `sub` of `subs` such sets of lanes.
+template <int NQ, int WAVES, bool WINDOW>
+__device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace& pl, int64_t groups, int row0, int tokens,
+                                           const unsigned char* states, int stride, int sub, int subs) {
+    constexpr int kRows = 16 * NQ;
+    const int M = a.g * a.t, d4 = threadIdx.x & 31;
+    const float* of = reinterpret_cast<const float*>(states);
+    for (int r = sub; r < kRows; r += subs) {
+        if (row0 + r >= M) break;
+        float top = __builtin_huge_valf();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fminf(top, of[w * (stride / 4) + kRows * kCaRow + r]);
+        float l = 0.f;
+        f4v acc{0.f, 0.f, 0.f, 0.f};
+        if (top < __builtin_huge_valf())
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float* ow = of + w * (stride / 4);
+                const float c = __builtin_amdgcn_exp2f(top - ow[kRows * kCaRow + r]);
+                l += c * ow[kRows * (kCaRow + 1) + r];
+                acc += c * *reinterpret_cast<const f4v*>(ow + r * kCaRow + 4 * d4);
+            }
+        const int64_t row = pl.grp * M + row0 + r;
+        if (a.splits > 1) {
+            const int64_t at = row * a.splits + pl.split;
+            reinterpret_cast<f4v*>(a.part)[at * (kD / 4) + d4] = acc;
+            if (d4 == 0) {
+                float* ml = a.part + groups * M * a.splits * kD + 2 * at;
+                ml[0] = top;
+                ml[1] = l;
+            }
+        } else {
+            store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, (row0 + r) % a.t < tokens);
+        }
+    }
+}
+
 }  // namespace pariskv

@@ -29,6 +29,7 @@ namespace pariskv {
 typedef _Float16 h2v __attribute__((ext_vector_type(2)));
 typedef _Float16 h4v __attribute__((ext_vector_type(4)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef float f2v __attribute__((ext_vector_type(2)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 // Loaded words, as a vector type that arrays of stay in registers (HIP's uint4 is a class).
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));

@@ -1,0 +1,255 @@
+// Attention of a few new tokens per sequence where they make more than 32 rows over the same
+// keys (chunk_attend.hip has the method and the kernel for fewer).
+//
+// 8 waves: SETS sets of 32 rows, and 8 / SETS waves a set that take 32 keys each of a tile of
+// keys.  The tile is read from HBM once and lies in LDS as float16 for all sets: waves that
+// fetched the same rows at the same time for themselves had them fetched from HBM twice, for
+// misses on one cache line are not joined while it is on its way (16 drafts x 4 heads, 8 x 8 x
+// 128K float16 rows: 1317 us so, 920 with the sets in blocks of their own, MEASURED us here).  The
+// next tiles are in flight in registers meanwhile.  Records are taken apart once for all rows.
+
+#include <hip/hip_fp16.h>
+
+#include "chunk_attend_device.hpp"
+
+namespace pariskv {
+
+namespace {
+
+constexpr int kTaWaves = 8;
+constexpr int kTaThreads = 64 * kTaWaves;
+
+template <int SETS, int KB, int VB, bool WINDOW>
+__global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a, int row_tiles, int64_t groups) {
+    constexpr int NQ = 2;
+    constexpr bool kQuant = KB < 16;
+    constexpr int kRecord = kQuant ? quant_record_bytes(KB, VB) : 0;
+    constexpr int kParts = kTaWaves / SETS;      // waves that share a set's keys
+    constexpr int kTile = kCaKeys * kParts;      // keys of a tile
+    constexpr int kRowLoads = kTile * 16 / kTaThreads;  // 16-byte pieces of K (of V) a thread holds
+    constexpr int kChunks = kTile * kRecord / 16;
+    constexpr int kLoads = kQuant ? (kChunks + kTaThreads - 1) / kTaThreads : 2 * kRowLoads;
+    constexpr int kTileBytes = kTile * kD * 2;
+    // Float16: two buffers of K and V.  Records: one of K and V, one of the records.
+    constexpr int kBuffers = kQuant ? 1 : 2;
+    constexpr int kUse = 2 * kBuffers * kTileBytes + kTile * kRecord, kState = ca_state_bytes(NQ);
+    constexpr int kLds = kUse > kTaWaves * kState ? kUse : kTaWaves * kState;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[kLds];
+
+    const ChunkPlace pl = chunk_place(a, row_tiles, groups);
+    const int64_t grp = pl.grp;
+    const int seq = pl.seq;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part = wave % kParts, set = wave / kParts;
+    const int col = lane & 15, lg = lane >> 4;
+    const int M = a.g * a.t, row0 = (pl.tile * SETS + set) * 16 * NQ;
+    const KeySpan span = key_span(a, seq, 0, a.t);
+
+    // Tiles: the sinks', the cached stretch's; this share's part of them, and the drafts behind
+    // the last share's.
+    const int sink_tiles = (span.sink_end + kTile - 1) / kTile;
+    const int tiles = sink_tiles + (span.hi - span.lo + kTile - 1) / kTile;
+    const int per = (tiles + a.splits - 1) / a.splits;
+    const int first = min(pl.split * per, tiles), last = min(first + per, tiles);
+    const int end = last + ((!WINDOW && pl.split == a.splits - 1) ? (a.t + kTile - 1) / kTile : 0);
+
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    h8v qf[NQ][4];
+    int tok[NQ];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        const int r = min(row0 + 16 * x + col, M - 1);
+        tok[x] = r % a.t;
+        const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) + (grp * M + r) * kD);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) qf[x][c] = query_part(qr[4 * c + lg], flip);
+    }
+    ChunkRows<NQ> rows;
+    rows.init(score_factor(a.scale));
+
+    // Of a tile: cache row (or draft) of its first key, and how many of its keys there are.
+    auto tile_base = [&](int t) {
+        if (!WINDOW && t >= last) return (t - last) * kTile;
+        return WINDOW && t < sink_tiles ? t * kTile : span.lo + (t - sink_tiles) * kTile;
+    };
+    auto tile_keys = [&](int t) {
+        const int stop = !WINDOW && t >= last ? a.t : WINDOW && t < sink_tiles ? span.sink_end : span.hi;
+        return stop - tile_base(t);
+    };
+    unsigned char* kt = lds;
+    unsigned char* vt = lds + kBuffers * kTileBytes;
+    unsigned char* rt = lds + 2 * kBuffers * kTileBytes;
+    const int lrow = tid >> 4, lchunk = tid & 15;
+    constexpr int kStepRows = kTaThreads / 16;  // rows that the block's 16-byte pieces cover at once
+    auto put = [&](int buf, int key, h8v k, h8v v) {
+        *reinterpret_cast<h8v*>(kt + buf * kTileBytes + key * 256 + ((lchunk ^ (key & 15)) << 4)) = k;
+        put_v(vt + buf * kTileBytes, key, lchunk, v);
+    };
+
+    // What lies behind the last key is not read: rows repeat it, records are cleared in place().
+    auto load = [&](int t, u4v (&regs)[kLoads]) {
+        const int most = tile_keys(t) - 1;
+        const bool drafts = !WINDOW && t >= last;
+        if constexpr (kQuant) {
+            if (drafts) return;
+            const u4v* p = reinterpret_cast<const u4v*>(a.rec + (grp * a.capacity + tile_base(t)) * kRecord);
+            const int top = (most + 1) * (kRecord / 16) - 1;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) regs[i] = p[min(kTaThreads * i + tid, top)];
+        } else {
+            const int64_t at = (drafts ? grp * a.t : grp * a.capacity) + tile_base(t);
+            const u4v* K = static_cast<const u4v*>(drafts ? a.Kt : a.K) + at * 16;
+            const u4v* V = static_cast<const u4v*>(drafts ? a.Vt : a.V) + at * 16;
+#pragma unroll
+            for (int i = 0; i < kRowLoads; ++i) {
+                const int from = min(kStepRows * i + lrow, most) * 16 + lchunk;
+                regs[i] = K[from];
+                regs[kRowLoads + i] = V[from];
+            }
+        }
+    };
+    const uint64_t used = end > last ? used_drafts(a, seq, lane) : ~0ull;
+    // Puts a float16 tile into buffer buf; drafts that nobody sees count as 0.
+    auto put_rows = [&](int t, int buf, const u4v* k, const u4v* v) {
+        const int first_draft = !WINDOW && t >= last ? tile_base(t) : -1;
+#pragma unroll
+        for (int i = 0; i < kRowLoads; ++i) {
+            const int key = kStepRows * i + lrow;
+            u4v x = v[i];
+            if (!WINDOW && first_draft >= 0 && (first_draft + key > 63 || !((used >> (first_draft + key)) & 1)))
+                x = u4v{0u, 0u, 0u, 0u};
+            put(buf, key, as_h8(k[i]), as_h8(x));
+        }
+    };
+    // Puts tile t, loaded into regs, into LDS as float16.  Every wave of the block calls it, and
+    // for records it holds a barrier.
+    auto place = [&](int t, int buf, u4v (&regs)[kLoads]) {
+        if constexpr (kQuant) {
+            if (t >= last) {  // drafts: straight from memory, once a call
+                const int most = tile_keys(t) - 1;
+                u4v k[kRowLoads], v[kRowLoads];
+#pragma unroll
+                for (int i = 0; i < kRowLoads; ++i) {
+                    const int64_t from = (grp * a.t + tile_base(t) + min(kStepRows * i + lrow, most)) * 16 + lchunk;
+                    k[i] = static_cast<const u4v*>(a.Kt)[from];
+                    v[i] = static_cast<const u4v*>(a.Vt)[from];
+                }
+                put_rows(t, buf, k, v);
+                return;
+            }
+            // Records that are not there: codes of 0, not what the bytes of another part would mean.
+            const int have = tile_keys(t) * (kRecord / 16);
+            if (have < kChunks)
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+                    if (kTaThreads * i + tid >= have) regs[i] = u4v{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                if (kTaThreads * (i + 1) <= kChunks || kTaThreads * i + tid < kChunks)
+                    reinterpret_cast<u4v*>(rt)[kTaThreads * i + tid] = regs[i];
+            __syncthreads();
+            u2v kc[kRowLoads], vc[kRowLoads];
+            uint32_t ks[kRowLoads], vs[kRowLoads];
+#pragma unroll
+            for (int i = 0; i < kRowLoads; ++i) {
+                const unsigned char* p = rt + (kStepRows * i + lrow) * kRecord;
+                kc[i] = quant_load8<KB>(p + lchunk * KB);
+                vc[i] = quant_load8<VB>(p + quant_code_bytes(KB) + lchunk * VB);
+                ks[i] = p[quant_code_bytes(KB) + quant_code_bytes(VB) + (lchunk >> 2)];
+                vs[i] = p[quant_code_bytes(KB) + quant_code_bytes(VB) + 4 + (lchunk >> 2)];
+            }
+#pragma unroll
+            for (int i = 0; i < kRowLoads; ++i)
+                put(buf, kStepRows * i + lrow, quant_decode8<KB>(kc[i][0], kc[i][1], quant_scale_value(ks[i])),
+                    quant_decode8<VB>(vc[i][0], vc[i][1], quant_scale_value(vs[i])));
+        } else {
+            put_rows(t, buf, regs, regs + kRowLoads);
+        }
+    };
+
+    // Where this lane's reads of a tile begin: its K operands and its transposing reads of V.
+    const int tkey = 4 * lg + (col >> 2);
+    const unsigned char* kr = kt + (part * kCaKeys + col) * 256;
+    const unsigned char* tr = vt + (part * kCaKeys + tkey) * 256 + ((col & 3) >> 1) * 16 + (col & 1) * 8;
+    auto compute = [&](int t, int buf) {
+        const int base = tile_base(t) + part * kCaKeys, valid = tile_keys(t) - part * kCaKeys;
+        if (valid <= 0 || row0 >= M) return;
+        rows.scores(qf, [&](int h, int c) {
+            return *reinterpret_cast<const h8v*>(kr + buf * kTileBytes + 16 * h * 256 + (((4 * c + lg) ^ col) << 4));
+        });
+        uint32_t w[NQ];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            w[x] = bits_to(valid - 1);
+            if constexpr (WINDOW) w[x] &= window_bits(span.start + tok[x], base, (int)a.sink, (int)a.window);
+            else if (t >= last) w[x] = draft_bits(a, seq, tok[x], base, valid);
+        }
+        rows.accumulate(w, tr + buf * kTileBytes, tkey, lg);
+    };
+
+    u4v regs[2][kLoads];
+    if (first < end) load(first, regs[0]);
+    if (first + 1 < end) load(first + 1, regs[1]);
+    if constexpr (kQuant) {
+        // place() waits for every wave to be done with the tile before: at its own barrier, or,
+        // for drafts, at this one.
+        auto turn = [&](int t, u4v (&r)[kLoads]) {
+            if (t >= last) __syncthreads();
+            place(t, 0, r);
+            if (t + 2 < end) load(t + 2, r);
+            __syncthreads();
+            compute(t, 0);
+        };
+        for (int t = first; t < end; t += 2) {
+            turn(t, regs[0]);
+            if (t + 1 < end) turn(t + 1, regs[1]);
+        }
+    } else {
+        if (first < end) place(first, 0, regs[0]);
+        if (first + 2 < end) load(first + 2, regs[0]);
+        // Tile t lies in buffer b; r holds tile t + 1 and takes tile t + 3.
+        auto turn = [&](int t, int b, u4v (&r)[kLoads]) {
+            __syncthreads();
+            compute(t, b);
+            if (t + 1 < end) place(t + 1, b ^ 1, r);
+            if (t + 3 < end) load(t + 3, r);
+        };
+        for (int t = first; t < end; t += 2) {
+            turn(t, 0, regs[1]);
+            if (t + 1 < end) turn(t + 1, 1, regs[0]);
+        }
+    }
+
+    __syncthreads();
+    rows.leave(lds + wave * kState, col, lg);
+    __syncthreads();
+    join_waves<NQ, kParts, WINDOW>(a, pl, groups, row0, span.tokens, lds + set * kParts * kState, kState,
+                                   (tid >> 5) % (2 * kParts), 2 * kParts);
+}
+
+}  // namespace
+
+hipError_t launch_tile_attend(const ChunkArgs& a, int block, int row_tiles, int64_t groups, const char* name,
+                              hipStream_t s) {
+    const ProfEvents pe = prof_begin(name);
+    auto go = [&](auto kernel) {
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)(groups * a.splits * row_tiles)), dim3(kTaThreads), 0, s, pe.start,
+                              pe.stop, 0, a, row_tiles, groups);
+    };
+    auto rows = [&](auto k64, auto k128) { block == 64 ? go(k64) : go(k128); };
+    if (a.window > 0)
+        rows(tile_attend_kernel<2, 16, 16, true>, tile_attend_kernel<4, 16, 16, true>);
+    else if (!a.rec)
+        rows(tile_attend_kernel<2, 16, 16, false>, tile_attend_kernel<4, 16, 16, false>);
+    else if (a.k_bits == 8 && a.v_bits == 8)
+        rows(tile_attend_kernel<2, 8, 8, false>, tile_attend_kernel<4, 8, 8, false>);
+    else if (a.k_bits == 8)
+        rows(tile_attend_kernel<2, 8, 4, false>, tile_attend_kernel<4, 8, 4, false>);
+    else if (a.v_bits == 8)
+        rows(tile_attend_kernel<2, 4, 8, false>, tile_attend_kernel<4, 4, 8, false>);
+    else
+        rows(tile_attend_kernel<2, 4, 4, false>, tile_attend_kernel<4, 4, 4, false>);
+    return hipGetLastError();
+}
+
+}  // namespace pariskv
