@@ -973,11 +973,10 @@ static int check_tree_sizes(const pariskv_config* cfg, int32_t batch, int64_t n,
     return PARISKV_OK;
 }
 
-// Bytes of a few-token call's workspace and its number of shares.
-static size_t chunk_workspace(const ChunkArgs& a, int32_t* splits) {
-    const int64_t groups = (int64_t)a.batch * a.hkv, rows = (int64_t)a.g * a.t;
-    *splits = chunk_splits(groups, rows, chunk_keys(a.n, a.t, a.sink, a.window));
-    const size_t bytes = chunk_part_bytes(groups, rows, *splits);
+// Plans a few-token call; bytes of its workspace.
+static size_t chunk_workspace(ChunkArgs& a) {
+    chunk_plan(a);
+    const size_t bytes = chunk_part_bytes(a);
     return bytes < 256 ? 256 : (bytes + 255) / 256 * 256;
 }
 
@@ -997,7 +996,7 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
     a.g = cfg->q_per_kv;
     a.t = t;
     a.n = n;
-    return chunk_workspace(a, &a.splits);
+    return chunk_workspace(a);
 }
 
 static int tree_impl(const pariskv_config* cfg, const void* q, const void* K, const void* V,
@@ -1049,7 +1048,7 @@ static int tree_impl(const pariskv_config* cfg, const void* q, const void* K, co
     a.t = t;
     a.scale = scale;
     a.out = out;
-    const size_t need = chunk_workspace(a, &a.splits);
+    const size_t need = chunk_workspace(a);
     if ((rc = check_workspace(workspace, ws_bytes, need)) != PARISKV_OK) return rc;
     a.part = static_cast<float*>(workspace);
     const hipError_t e = launch_chunk_attend(a, static_cast<hipStream_t>(stream));
@@ -1105,7 +1104,7 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
     if (check_sink_window_sizes(cfg, batch, pos, t, sink, window) != PARISKV_OK) return 0;
     ChunkArgs a{};
     sink_window_shape(cfg, batch, pos, t, sink, window, &a);
-    return t > 0 && few_tokens(a) ? chunk_workspace(a, &a.splits) : 256;
+    return t > 0 && few_tokens(a) ? chunk_workspace(a) : 256;
 }
 
 int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const void* K, const void* V,
@@ -1137,7 +1136,7 @@ int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const v
     a.scale = scale;
     a.out = out;
     const bool few = few_tokens(a);
-    const size_t need = few ? chunk_workspace(a, &a.splits) : 256;
+    const size_t need = few ? chunk_workspace(a) : 256;
     if ((rc = check_workspace(workspace, ws_bytes, need)) != PARISKV_OK) return rc;
     a.part = static_cast<float*>(workspace);
     const hipError_t e = few ? launch_chunk_attend(a, static_cast<hipStream_t>(stream))

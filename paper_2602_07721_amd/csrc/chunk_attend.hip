@@ -93,10 +93,11 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
     // drafts behind the last share's.
     const int sink_steps = (span.sink_end + kCaKeys - 1) / kCaKeys;
     const int steps = sink_steps + (span.hi - span.lo + kCaKeys - 1) / kCaKeys;
-    const int per = (steps + a.splits - 1) / a.splits;
-    const int first = min(pl.split * per, steps), last = min(first + per, steps);
-    const int draft_steps = (!WINDOW && pl.split == a.splits - 1) ? (a.t + kCaKeys - 1) / kCaKeys : 0;
+    const bool closing = pl.split == a.splits - 1;  // takes what is left, and the drafts
+    const int first = min(pl.split * a.per, steps), last = closing ? steps : min(first + a.per, steps);
+    const int draft_steps = (!WINDOW && closing) ? (a.t + kCaKeys - 1) / kCaKeys : 0;
     const int end = last + draft_steps;
+    if (first >= end && a.splits > 1) return leave_idle(a, pl, groups, row0, 16 * NQ);
 
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
     h8v qf[NQ][4];
@@ -277,26 +278,24 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
 // Joins the shares' states of a row: 8 groups of 32 lanes take every eighth share, 4 dims a lane.
 constexpr int kCcGroups = 8;
 template <bool WINDOW>
-__global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs a, int64_t rows) {
+__global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs a, int64_t groups) {
     __shared__ f4v so[kCcGroups][32];
     __shared__ float snm[kCcGroups], sl[kCcGroups];
-    const int64_t row = blockIdx.x;
+    const uint32_t row = blockIdx.x;
     const int d4 = threadIdx.x & 31, sub = threadIdx.x >> 5;
-    const int M = a.g * a.t;
-    const float* ml = a.part + rows * a.splits * kD + 2 * row * a.splits;
-    const f4v* part = reinterpret_cast<const f4v*>(a.part) + row * a.splits * (kD / 4) + d4;
+    const float2* state = part_state(a, groups, row);
+    const f4v* part = reinterpret_cast<const f4v*>(a.part) + (int64_t)row * a.splits * (kD / 4) + d4;
     float top = __builtin_huge_valf(), l = 0.f;
     f4v acc{0.f, 0.f, 0.f, 0.f};
     for (int s = sub; s < a.splits; s += kCcGroups) {
-        const float nm = ml[2 * s], ls = ml[2 * s + 1];
+        const float2 st = state[s];
         const f4v v = part[s * (kD / 4)];
-        const float to = fminf(top, nm);
-        if (to < __builtin_huge_valf()) {
-            const float c0 = __builtin_amdgcn_exp2f(to - top), c1 = __builtin_amdgcn_exp2f(to - nm);
-            l = l * c0 + ls * c1;
-            acc = acc * c0 + v * c1;
-            top = to;
-        }
+        if (st.x == __builtin_huge_valf()) continue;  // saw no key; its outputs may not have been written
+        const float to = fminf(top, st.x);
+        const float c0 = __builtin_amdgcn_exp2f(to - top), c1 = __builtin_amdgcn_exp2f(to - st.x);
+        l = l * c0 + st.y * c1;
+        acc = acc * c0 + v * c1;
+        top = to;
     }
     so[sub][d4] = acc;
     if (d4 == 0) {
@@ -318,7 +317,10 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
             acc += c * so[i][d4];
         }
     bool real = true;
-    if (WINDOW && a.counts) real = (int)(row % M) % a.t < a.counts[row / M / a.hkv];
+    if (WINDOW && a.counts) {
+        const uint32_t M = (uint32_t)(a.g * a.t);
+        real = (int)(row % M % (uint32_t)a.t) < a.counts[row / M / (uint32_t)a.hkv];
+    }
     store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, real);
 }
 
@@ -328,20 +330,29 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
 // register of a SIMD), more by tile_attend.hip, whose waves share the keys' tiles.
 static int chunk_block_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
-int32_t chunk_splits(int64_t groups, int64_t rows, int64_t keys) {
+void chunk_plan(ChunkArgs& a) {
+    const int64_t groups = (int64_t)a.batch * a.hkv, rows = (int64_t)a.g * a.t;
     const int64_t block = chunk_block_rows(rows), blocks = groups * ((rows + block - 1) / block);
-    // About two rounds of the blocks that the chip holds (2 a CU, one of the larger ones), so that
-    // sequences of different lengths even out; no share shorter than 2 steps of every wave.
-    const int64_t want = block <= 32 ? 1024 : 512;
-    int64_t s = (want + blocks - 1) / blocks;
-    const int64_t most = keys / (2 * kCaWaves * kCaKeys);
-    if (s > most) s = most;
-    if (s > 256) s = 256;
-    return (int32_t)(s < 1 ? 1 : s);
+    int64_t steps = (a.n + kCaKeys - 1) / kCaKeys;
+    if (a.window > 0) {
+        const int64_t near = a.window + a.t - 1, all = a.n + a.t, sinks = a.sink < a.n ? a.sink : a.n;
+        steps = (sinks + kCaKeys - 1) / kCaKeys + ((near < all ? near : all) + kCaKeys - 1) / kCaKeys;
+    }
+    // About two rounds of the blocks that the chip holds at a time (2 a CU); a share is a multiple
+    // of 4 steps, one for every wave.
+    const int64_t want = 1024;
+    int64_t splits = (want + blocks - 1) / blocks;
+    if (splits > 256) splits = 256;
+    int64_t per = (steps + splits - 1) / splits;
+    per = (per + kCaWaves - 1) / kCaWaves * kCaWaves;
+    if (per < kCaWaves) per = kCaWaves;
+    splits = (steps + per - 1) / per;
+    a.per = (int32_t)per;
+    a.splits = (int32_t)(splits < 1 ? 1 : splits);
 }
 
-size_t chunk_part_bytes(int64_t groups, int64_t rows, int32_t splits) {
-    return splits > 1 ? (size_t)(groups * rows) * (size_t)splits * (kD + 2) * 4 : 0;
+size_t chunk_part_bytes(const ChunkArgs& a) {
+    return a.splits > 1 ? (size_t)a.batch * a.hkv * a.g * a.t * (size_t)a.splits * (kD + 2) * 4 : 0;
 }
 
 hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s) {
@@ -378,7 +389,7 @@ hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s) {
     const ProfEvents pe = prof_begin("chunk_combine");
     const int64_t all = groups * M;
     auto combine = [&](auto kernel) {
-        hipExtLaunchKernelGGL(kernel, dim3((unsigned)all), dim3(32 * kCcGroups), 0, s, pe.start, pe.stop, 0, a, all);
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)all), dim3(32 * kCcGroups), 0, s, pe.start, pe.stop, 0, a, groups);
     };
     a.window > 0 ? combine(chunk_combine_kernel<true>) : combine(chunk_combine_kernel<false>);
     return hipGetLastError();

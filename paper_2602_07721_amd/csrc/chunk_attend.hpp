@@ -34,19 +34,13 @@ struct ChunkArgs {
     float scale;
     void* out;            // [batch][hkv g][t][D], float32 (tree) or float16 (sliding window)
     float* part;          // chunk_part_bytes
-    int32_t splits;
+    int32_t splits;       // blocks that share a (sequence, KV head)'s keys, each `per` steps of 32
+    int32_t per;          // of them; sequences with fewer keys leave the last ones idle
 };
 
-// Most keys a sequence of the call can have (its size, before any device-side length).
-inline int64_t chunk_keys(int64_t n, int64_t t, int64_t sink, int64_t window) {
-    if (window == 0) return n;
-    const int64_t all = n + t;  // and no more than the sinks and t windows that overlap
-    const int64_t near = window >= all ? all : window + t - 1;
-    return near >= all || sink >= all - near ? all : near + sink;
-}
-// Blocks that share the keys of one (sequence, KV head).
-int32_t chunk_splits(int64_t groups, int64_t rows, int64_t keys);
-size_t chunk_part_bytes(int64_t groups, int64_t rows, int32_t splits);
+// Sets splits and per from the call's sizes alone (not from lens and counts).
+void chunk_plan(ChunkArgs& a);
+size_t chunk_part_bytes(const ChunkArgs& a);
 hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s);
 // Its first kernel for blocks of 64 or 128 rows (tile_attend.hip).
 hipError_t launch_tile_attend(const ChunkArgs& a, int block, int row_tiles, int64_t groups, const char* name,

@@ -92,30 +92,44 @@ constexpr int kCaRow = kD + 4;   // floats of an output row in LDS (spreads the 
 // LDS of a wave's outputs [row][kCaRow], maxima and sums.
 constexpr int ca_state_bytes(int nq) { return 16 * nq * (kCaRow + 2) * 4; }
 
-// What a block works on: rows [row0, ...) of a (sequence, KV head)'s g t, share `split` of the keys.
+// What a block works on: tile `tile` of the rows of (sequence, KV head) grp, share `split` of its keys.
 struct ChunkPlace {
     int64_t grp;
     int split, seq, tile;
 };
 // Consecutive blocks go to the 8 XCDs in turn: the row tiles of one share of the keys are 8
-// apart, so that one XCD's L2 serves them all.
-__device__ __forceinline__ ChunkPlace chunk_place(const ChunkArgs& a, int row_tiles, int64_t groups) {
+// apart, so that one XCD's L2 serves them all.  (The host keeps the number of blocks below 2^31.)
+__device__ __forceinline__ ChunkPlace chunk_place(const ChunkArgs& a, uint32_t row_tiles, uint32_t groups) {
     ChunkPlace p;
-    int64_t id = blockIdx.x, share;
-    const int64_t shares = groups * a.splits;
-    const int64_t full = shares / 8 * 8 * row_tiles;
-    if (id < full) {
-        share = id / (8 * row_tiles) * 8 + id % 8;
-        p.tile = (int)(id / 8 % row_tiles);
-    } else {
-        id -= full;
-        share = full / row_tiles + id / row_tiles;
-        p.tile = (int)(id % row_tiles);
+    uint32_t id = blockIdx.x, share = id;
+    p.tile = 0;
+    if (row_tiles > 1) {
+        const uint32_t full = groups * (uint32_t)a.splits / 8 * 8 * row_tiles;
+        if (id < full) {
+            share = id / (8 * row_tiles) * 8 + id % 8;
+            p.tile = (int)(id / 8 % row_tiles);
+        } else {
+            id -= full;
+            share = full / row_tiles + id / row_tiles;
+            p.tile = (int)(id % row_tiles);
+        }
     }
-    p.grp = share / a.splits;
-    p.split = (int)(share % a.splits);
-    p.seq = (int)(p.grp / a.hkv);
+    const uint32_t grp = share / (uint32_t)a.splits;
+    p.grp = grp;
+    p.split = (int)(share % (uint32_t)a.splits);
+    p.seq = (int)(grp / (uint32_t)a.hkv);
     return p;
+}
+
+// The maximum and sum of a row's part in the workspace (behind all rows' outputs).
+__device__ __forceinline__ float2* part_state(const ChunkArgs& a, int64_t groups, int64_t row) {
+    return reinterpret_cast<float2*>(a.part + groups * a.g * a.t * a.splits * kD) + row * a.splits;
+}
+// A share without keys: its rows' states say so (their outputs are not read).
+__device__ __forceinline__ void leave_idle(const ChunkArgs& a, const ChunkPlace& pl, int64_t groups, int row0, int rows) {
+    const int M = a.g * a.t;
+    for (int r = row0 + (int)threadIdx.x; r < min(row0 + rows, M); r += (int)blockDim.x)
+        part_state(a, groups, pl.grp * M + r)[pl.split] = float2{__builtin_huge_valf(), 0.f};
 }
 
 // Drafts that some token of the sequence sees, bit by bit; the others may hold anything.  Every
@@ -311,11 +325,7 @@ __device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace&
         if (a.splits > 1) {
             const int64_t at = row * a.splits + pl.split;
             reinterpret_cast<f4v*>(a.part)[at * (kD / 4) + d4] = acc;
-            if (d4 == 0) {
-                float* ml = a.part + groups * M * a.splits * kD + 2 * at;
-                ml[0] = top;
-                ml[1] = l;
-            }
+            if (d4 == 0) part_state(a, groups, row)[pl.split] = float2{top, l};
         } else {
             store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, (row0 + r) % a.t < tokens);
         }

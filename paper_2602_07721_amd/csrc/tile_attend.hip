@@ -1,8 +1,8 @@
 // Attention of a few new tokens per sequence where they make more than 32 rows over the same
 // keys (chunk_attend.hip has the method and the kernel for fewer).
 //
-// 8 waves: SETS sets of 32 rows, and 8 / SETS waves a set that take 32 keys each of a tile of
-// keys.  The tile is read from HBM once and lies in LDS as float16 for all sets: waves that
+// 4 waves: SETS sets of 32 rows, and 4 / SETS waves a set that take 32 keys each of a tile of
+// keys.  Two such blocks share a CU: one computes while the other waits at its barrier.  The tile is read from HBM once and lies in LDS as float16 for all sets: waves that
 // fetched the same rows at the same time for themselves had them fetched from HBM twice, for
 // misses on one cache line are not joined while it is on its way (16 drafts x 4 heads, 8 x 8 x
 // 128K float16 rows: 1317 us so, 920 with the sets in blocks of their own, MEASURED us here).  The
@@ -16,7 +16,7 @@ namespace pariskv {
 
 namespace {
 
-constexpr int kTaWaves = 8;
+constexpr int kTaWaves = 4;
 constexpr int kTaThreads = 64 * kTaWaves;
 
 template <int SETS, int KB, int VB, bool WINDOW>
@@ -49,9 +49,11 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
     // the last share's.
     const int sink_tiles = (span.sink_end + kTile - 1) / kTile;
     const int tiles = sink_tiles + (span.hi - span.lo + kTile - 1) / kTile;
-    const int per = (tiles + a.splits - 1) / a.splits;
-    const int first = min(pl.split * per, tiles), last = min(first + per, tiles);
-    const int end = last + ((!WINDOW && pl.split == a.splits - 1) ? (a.t + kTile - 1) / kTile : 0);
+    const int per = a.per * kCaKeys / kTile;
+    const bool closing = pl.split == a.splits - 1;  // takes what is left, and the drafts
+    const int first = min(pl.split * per, tiles), last = closing ? tiles : min(first + per, tiles);
+    const int end = last + ((!WINDOW && closing) ? (a.t + kTile - 1) / kTile : 0);
+    if (first >= end && a.splits > 1) return leave_idle(a, pl, groups, pl.tile * SETS * 16 * NQ, SETS * 16 * NQ);
 
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
     h8v qf[NQ][4];
