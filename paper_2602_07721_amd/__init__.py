@@ -627,15 +627,11 @@ def offload_rows(K_src, V_src, src_row, K_dst, V_dst, dst_row, t, stream=None):
 
 def _require_here(stream, *tensors):
     """The library launches on the current device: every GPU tensor and the stream must be there."""
-    torch = _torch()
-    here = None
+    here = _torch().cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda:
-            if here is None:
-                here = torch.cuda.current_device()
-            if t.device.index != here:
-                raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
-    if stream is not None and here is not None and stream.device.index != here:
+        if t is not None and t.get_device() != here and t.is_cuda:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+    if stream is not None and stream.device.index != here:
         raise ValueError(f"stream on {stream.device}, but the current device is cuda:{here}")
 
 
@@ -653,7 +649,9 @@ class QuantCache:
     on the GPU, or in pinned host memory with host_mapped."""
 
     def __init__(self, rec, k_bits=8, v_bits=8, host_mapped=False):
-        self.rec, self.k_bits, self.v_bits, self.host_mapped = rec, int(k_bits), int(v_bits), bool(host_mapped)
+        self.rec, self.host_mapped = rec, bool(host_mapped)
+        self.k_bits, self.v_bits = int(k_bits), int(v_bits)
+        self._bytes = self.record_bytes(k_bits, v_bits)
 
     @staticmethod
     def record_bytes(k_bits, v_bits):
@@ -675,13 +673,12 @@ class QuantCache:
         return int(self.rec.shape[2])
 
     def c(self, cfg, batch, dev):
-        torch = _torch()
-        bytes_ = self.record_bytes(self.k_bits, self.v_bits)
-        ptr = _arg(self.rec, "cache.rec", torch.uint8, (batch, cfg.n_kv_heads, _rows(self.rec), bytes_),
-                   None if self.host_mapped else dev)
-        if self.host_mapped and (self.rec.is_cuda or not self.rec.is_pinned()):
+        rec, host = self.rec, self.host_mapped
+        ptr = _arg(rec, "cache.rec", _torch().uint8, (batch, cfg.n_kv_heads, _rows(rec), self._bytes),
+                   None if host else dev)
+        if host and (rec.is_cuda or not rec.is_pinned()):
             raise ValueError("cache.rec must be pinned host memory when host_mapped")
-        self._c = _QuantCache(ptr, self.capacity, self.k_bits, self.v_bits, int(self.host_mapped))
+        self._c = _QuantCache(ptr, rec.shape[2], self.k_bits, self.v_bits, host)
         return ctypes.byref(self._c)
 
 

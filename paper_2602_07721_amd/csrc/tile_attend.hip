@@ -25,7 +25,8 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
     constexpr bool kQuant = KB < 16;
     constexpr int kRecord = kQuant ? quant_record_bytes(KB, VB) : 0;
     constexpr int kParts = kTaWaves / SETS;      // waves that share a set's keys
-    constexpr int kTile = kCaKeys * kParts;      // keys of a tile
+    constexpr int kSub = SETS == 4 ? 2 : 1;      // 32-key steps of a wave in a tile
+    constexpr int kTile = kCaKeys * kParts * kSub;  // keys of a tile
     constexpr int kRowLoads = kTile * 16 / kTaThreads;  // 16-byte pieces of K (of V) a thread holds
     constexpr int kChunks = kTile * kRecord / 16;
     constexpr int kLoads = kQuant ? (kChunks + kTaThreads - 1) / kTaThreads : 2 * kRowLoads;
@@ -171,22 +172,28 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
 
     // Where this lane's reads of a tile begin: its K operands and its transposing reads of V.
     const int tkey = 4 * lg + (col >> 2);
-    const unsigned char* kr = kt + (part * kCaKeys + col) * 256;
-    const unsigned char* tr = vt + (part * kCaKeys + tkey) * 256 + ((col & 3) >> 1) * 16 + (col & 1) * 8;
+    const unsigned char* kr = kt + (part * kSub * kCaKeys + col) * 256;
+    const unsigned char* tr = vt + (part * kSub * kCaKeys + tkey) * 256 + ((col & 3) >> 1) * 16 + (col & 1) * 8;
     auto compute = [&](int t, int buf) {
-        const int base = tile_base(t) + part * kCaKeys, valid = tile_keys(t) - part * kCaKeys;
-        if (valid <= 0 || row0 >= M) return;
-        rows.scores(qf, [&](int h, int c) {
-            return *reinterpret_cast<const h8v*>(kr + buf * kTileBytes + 16 * h * 256 + (((4 * c + lg) ^ col) << 4));
-        });
-        uint32_t w[NQ];
+        if (row0 >= M) return;
+#pragma unroll 1
+        for (int sub = 0; sub < kSub; ++sub) {
+            const int at = (part * kSub + sub) * kCaKeys;
+            const int base = tile_base(t) + at, valid = tile_keys(t) - at;
+            if (valid <= 0) return;
+            const unsigned char* ks = kr + buf * kTileBytes + sub * kCaKeys * 256;
+            rows.scores(qf, [&](int h, int c) {
+                return *reinterpret_cast<const h8v*>(ks + 16 * h * 256 + (((4 * c + lg) ^ col) << 4));
+            });
+            uint32_t w[NQ];
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            w[x] = bits_to(valid - 1);
-            if constexpr (WINDOW) w[x] &= window_bits(span.start + tok[x], base, (int)a.sink, (int)a.window);
-            else if (t >= last) w[x] = draft_bits(a, seq, tok[x], base, valid);
+            for (int x = 0; x < NQ; ++x) {
+                w[x] = bits_to(valid - 1);
+                if constexpr (WINDOW) w[x] &= window_bits(span.start + tok[x], base, (int)a.sink, (int)a.window);
+                else if (t >= last) w[x] = draft_bits(a, seq, tok[x], base, valid);
+            }
+            rows.accumulate(w, tr + buf * kTileBytes + sub * kCaKeys * 256, tkey, lg);
         }
-        rows.accumulate(w, tr + buf * kTileBytes, tkey, lg);
     };
 
     u4v regs[2][kLoads];
