@@ -340,7 +340,7 @@ void chunk_plan(ChunkArgs& a) {
     }
     // About two rounds of the blocks that the chip holds at a time (2 a CU); a share is a multiple
     // of 4 steps, one for every wave.
-    const int64_t want = 1024;
+    const int64_t want = block <= 32 ? 1024 : 512;
     int64_t splits = (want + blocks - 1) / blocks;
     if (splits > 256) splits = 256;
     int64_t per = (steps + splits - 1) / splits;

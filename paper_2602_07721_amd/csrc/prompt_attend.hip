@@ -19,6 +19,12 @@ namespace pariskv {
 
 namespace {
 
+// 16 bytes of global memory a lane straight into LDS, at lds + 16 x lane.
+__device__ __forceinline__ void to_lds(const u4v* from, u4v* lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
+                                     (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);
+}
+
 typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int kPaThreads = 256;
@@ -30,15 +36,14 @@ constexpr float kPaSlack = 7.f; // running maximum is raised: below 2^16, and sm
 __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs a, int qtiles) {
     __shared__ u4v sk[2][kPaKeys * 16];
     __shared__ u4v sv[2][kPaKeys * 16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
 
     // The tiles with the most keys first (the last tokens of a prompt see the most), and the
     // heads of one KV head on one XCD, whose L2 then holds their keys.
-    const int64_t groups = (int64_t)a.batch * a.hkv;
-    int64_t id = blockIdx.x;
-    const int64_t per = (int64_t)qtiles * a.g;  // blocks of one (sequence, KV head)
-    int64_t grp, in;
-    const int64_t full = groups / 8 * 8 * per;
+    const uint32_t groups = (uint32_t)(a.batch * a.hkv), per = (uint32_t)(qtiles * a.g);
+    uint32_t id = blockIdx.x, grp, in;
+    const uint32_t full = groups / 8 * 8 * per;
     if (id < full) {
         grp = id / (8 * per) * 8 + id % 8;
         in = id / 8 % per;
@@ -47,8 +52,8 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
         grp = full / per + id / per;
         in = id % per;
     }
-    const int qt = qtiles - 1 - (int)(in / a.g);
-    const int seq = (int)(grp / a.hkv);
+    const int qt = qtiles - 1 - (int)(in / (uint32_t)a.g);
+    const int seq = (int)(grp / (uint32_t)a.hkv);
     const int i0 = qt * kPaTokens;
     const KeySpan span = key_span(a, seq, i0, i0 + kPaTokens);
     if (i0 >= span.tokens) return;  // before any barrier, the whole block
@@ -58,7 +63,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     const int sink_tiles = (span.sink_end + kPaKeys - 1) / kPaKeys;
     const int tiles = sink_tiles + (span.hi - span.lo + kPaKeys - 1) / kPaKeys;
 
-    const int64_t head = grp * a.g + in % a.g;  // (seq, query head)
+    const int64_t head = (int64_t)grp * a.g + in % (uint32_t)a.g;  // (seq, query head)
     const float c2 = score_factor(a.scale);
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
     const int tok = min(i0 + 32 * wave + col, i1 - 1);
@@ -77,32 +82,25 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-    const u4v* Kg = static_cast<const u4v*>(a.K) + grp * a.capacity * 16;
-    const u4v* Vg = static_cast<const u4v*>(a.V) + grp * a.capacity * 16;
-    const int lrow = tid >> 4, lchunk = tid & 15;
-    u4v kr[4], vr[4];
+    const u4v* Kg = static_cast<const u4v*>(a.K) + (int64_t)grp * a.capacity * 16;
+    const u4v* Vg = static_cast<const u4v*>(a.V) + (int64_t)grp * a.capacity * 16;
     // First row of a tile, and how many of its keys there are.
     auto tile_base = [&](int tile) {
         return tile < sink_tiles ? tile * kPaKeys : span.lo + (tile - sink_tiles) * kPaKeys;
     };
     auto tile_keys = [&](int tile) { return (tile < sink_tiles ? span.sink_end : span.hi) - tile_base(tile); };
-    // Keys past the last repeat it: what lies behind is not read.
-    auto load = [&](int tile) {
+    // This wave's quarter of a tile straight into LDS, 4 rows an instruction, lane i's 16 bytes
+    // behind lane i - 1's: the swizzle is in what a lane reads.  Keys past the last repeat it:
+    // what lies behind is not read.
+    auto load = [&](int tile, int buf) {
         const int64_t base = (int64_t)tile_base(tile) * 16;
         const int most = tile_keys(tile) - 1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int at = min(16 * i + lrow, most) * 16 + lchunk;
-            kr[i] = (Kg + base)[at];
-            vr[i] = (Vg + base)[at];
-        }
-    };
-    auto put = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 16 * i + lrow;
-            sk[buf][r * 16 + (lchunk ^ (r & 15))] = kr[i];
-            sv[buf][r * 16 + (lchunk ^ (4 * (r & 3)))] = vr[i];
+            const int first = 16 * i + 4 * wave, r = first + (lane >> 4), c = lane & 15;
+            const int row = min(r, most) * 16;
+            to_lds(Kg + base + (row + (c ^ (r & 15))), &sk[buf][first * 16]);
+            to_lds(Vg + base + (row + (c ^ (4 * (r & 3)))), &sv[buf][first * 16]);
         }
     };
     // Where this lane's transposing reads begin: key 4 half + (lane % 16) / 4, dims
@@ -110,12 +108,11 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     const int tkey = 4 * half + ((lane & 15) >> 2);
     const int tchunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 
-    load(0);
-    put(0);
+    load(0, 0);
     __syncthreads();
     for (int tile = 0; tile < tiles; ++tile) {
         const int buf = tile & 1;
-        if (tile + 1 < tiles) load(tile + 1);
+        if (tile + 1 < tiles) load(tile + 1, buf ^ 1);
         const int base_row = tile_base(tile), valid = tile_keys(tile);
         // Whether some token of the wave sees a key of the tile (its first key is at or before the
         // last token, and its first token's window or the sinks reach into it).
@@ -124,20 +121,20 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
         if (any) {
             f16v s[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
-                const u4v* kp = sk[buf] + (32 * h + col) * 16;
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(kp[(2 * c + half) ^ (col & 15)]), qf[c], s[h],
-                                                                  0, 0, 0);
-            }
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                        as_h8(sk[buf][(32 * h + col) * 16 + ((2 * c + half) ^ (col & 15))]), qf[c], s[h], 0, 0, 0);
             uint32_t w[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 w[h] = bits_to(valid - 1 - 32 * h) & window_bits(p, base_row + 32 * h, sink, window);
-            if (!__all((w[0] & w[1]) == ~0u)) {
+            if (__builtin_expect(!__all((w[0] & w[1]) == ~0u), 0)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t b = w[h] >> (4 * half);
@@ -152,9 +149,9 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[h][i]);
             top *= c2;
-            if (__any(top > -__builtin_huge_valf() && !(top + nm <= kPaUp + kPaSlack))) {
-                const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                const float to = kPaUp - fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+            if (__builtin_expect(__any(top > -__builtin_huge_valf() && !(top + nm <= kPaUp + kPaSlack)), 0)) {
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                const float to = kPaUp - fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
                 if (to < nm) {
                     const float c = __builtin_amdgcn_exp2f(to - nm);
                     nm = to;
@@ -164,35 +161,34 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
                 }
             }
             const float base = nm < __builtin_huge_valf() ? nm : 0.f;
-            h8v pf[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+                h8v pf[2];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], c2, base));
                     sum += e;
-                    pf[2 * h + i / 8][i % 8] = (_Float16)e;
+                    pf[i / 8][i % 8] = (_Float16)e;
                 }
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                typedef __attribute__((address_space(3))) s4v* lds_s4;
-                const u4v* vp = sv[buf] + tkey * 16 + ((4 * d + tchunk) ^ (4 * (tkey & 3)));
+                for (int k = 0; k < 2; ++k) {
+                    typedef __attribute__((address_space(3))) s4v* lds_s4;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const char* at = reinterpret_cast<const char*>(vp + 16 * k * 16) + (lane & 1) * 8;
-                    const s4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at));
-                    const s4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + 8 * 256));
-                    const h8v vf = join_h4(a0, a1);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[k], o[d], 0, 0, 0);
+                    for (int d = 0; d < 4; ++d) {
+                        const u4v* vp = sv[buf] + tkey * 16 + ((4 * d + tchunk) ^ (4 * (tkey & 3)));
+                        const char* at = reinterpret_cast<const char*>(vp + 16 * (2 * h + k) * 16) + (lane & 1) * 8;
+                        const s4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at));
+                        const s4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + 8 * 256));
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(join_h4(a0, a1), pf[k], o[d], 0, 0, 0);
+                    }
                 }
             }
         }
-        if (tile + 1 < tiles) put(buf ^ 1);
-        __syncthreads();
+        __syncthreads();  // and the next tile is there
     }
 
-    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
-    const float l = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    const float l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
     const float inv = l > 0.f ? 1.f / l : 0.f;
     if (i0 + 32 * wave + col < i1) {
         h4v* out = static_cast<h4v*>(a.out) + (head * a.t + tok) * (kD / 4);

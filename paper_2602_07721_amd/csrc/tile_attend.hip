@@ -19,6 +19,17 @@ namespace {
 constexpr int kTaWaves = 4;
 constexpr int kTaThreads = 64 * kTaWaves;
 
+// What a thread holds of a tile on its way: 8 dims of K and of V of N keys.
+template <int N, int KB, int VB>
+struct TileRegs {
+    u2v k[N], v[N];
+    uint32_t ks[N], vs[N];
+};
+template <int N>
+struct TileRegs<N, 16, 16> {
+    u4v k[N], v[N];
+};
+
 template <int SETS, int KB, int VB, bool WINDOW>
 __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a, int row_tiles, int64_t groups) {
     constexpr int NQ = 2;
@@ -28,12 +39,8 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
     constexpr int kSub = SETS == 4 ? 2 : 1;      // 32-key steps of a wave in a tile
     constexpr int kTile = kCaKeys * kParts * kSub;  // keys of a tile
     constexpr int kRowLoads = kTile * 16 / kTaThreads;  // 16-byte pieces of K (of V) a thread holds
-    constexpr int kChunks = kTile * kRecord / 16;
-    constexpr int kLoads = kQuant ? (kChunks + kTaThreads - 1) / kTaThreads : 2 * kRowLoads;
     constexpr int kTileBytes = kTile * kD * 2;
-    // Float16: two buffers of K and V.  Records: one of K and V, one of the records.
-    constexpr int kBuffers = kQuant ? 1 : 2;
-    constexpr int kUse = 2 * kBuffers * kTileBytes + kTile * kRecord, kState = ca_state_bytes(NQ);
+    constexpr int kUse = 4 * kTileBytes, kState = ca_state_bytes(NQ);  // two buffers of K and V
     constexpr int kLds = kUse > kTaWaves * kState ? kUse : kTaWaves * kState;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kLds];
 
@@ -80,8 +87,7 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
         return stop - tile_base(t);
     };
     unsigned char* kt = lds;
-    unsigned char* vt = lds + kBuffers * kTileBytes;
-    unsigned char* rt = lds + 2 * kBuffers * kTileBytes;
+    unsigned char* vt = lds + 2 * kTileBytes;
     const int lrow = tid >> 4, lchunk = tid & 15;
     constexpr int kStepRows = kTaThreads / 16;  // rows that the block's 16-byte pieces cover at once
     auto put = [&](int buf, int key, h8v k, h8v v) {
@@ -89,16 +95,21 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
         put_v(vt + buf * kTileBytes, key, lchunk, v);
     };
 
-    // What lies behind the last key is not read: rows repeat it, records are cleared in place().
-    auto load = [&](int t, u4v (&regs)[kLoads]) {
+    // What lies behind the last key is not read: it is repeated.
+    auto load = [&](int t, TileRegs<kRowLoads, KB, VB>& regs) {
         const int most = tile_keys(t) - 1;
         const bool drafts = !WINDOW && t >= last;
         if constexpr (kQuant) {
             if (drafts) return;
-            const u4v* p = reinterpret_cast<const u4v*>(a.rec + (grp * a.capacity + tile_base(t)) * kRecord);
-            const int top = (most + 1) * (kRecord / 16) - 1;
+            const uint8_t* p = a.rec + (grp * a.capacity + tile_base(t)) * kRecord;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) regs[i] = p[min(kTaThreads * i + tid, top)];
+            for (int i = 0; i < kRowLoads; ++i) {
+                const int at = min(kStepRows * i + lrow, most) * kRecord;
+                regs.k[i] = quant_load8<KB>(p + (at + lchunk * KB));
+                regs.v[i] = quant_load8<VB>(p + (at + quant_code_bytes(KB) + lchunk * VB));
+                regs.ks[i] = p[at + quant_code_bytes(KB) + quant_code_bytes(VB) + (lchunk >> 2)];
+                regs.vs[i] = p[at + quant_code_bytes(KB) + quant_code_bytes(VB) + 4 + (lchunk >> 2)];
+            }
         } else {
             const int64_t at = (drafts ? grp * a.t : grp * a.capacity) + tile_base(t);
             const u4v* K = static_cast<const u4v*>(drafts ? a.Kt : a.K) + at * 16;
@@ -106,67 +117,38 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
 #pragma unroll
             for (int i = 0; i < kRowLoads; ++i) {
                 const int from = min(kStepRows * i + lrow, most) * 16 + lchunk;
-                regs[i] = K[from];
-                regs[kRowLoads + i] = V[from];
+                regs.k[i] = K[from];
+                regs.v[i] = V[from];
             }
         }
     };
     const uint64_t used = end > last ? used_drafts(a, seq, lane) : ~0ull;
-    // Puts a float16 tile into buffer buf; drafts that nobody sees count as 0.
-    auto put_rows = [&](int t, int buf, const u4v* k, const u4v* v) {
-        const int first_draft = !WINDOW && t >= last ? tile_base(t) : -1;
+    // Puts tile t, loaded into regs, into buffer buf as float16; drafts that nobody sees count as 0.
+    auto place = [&](int t, int buf, const TileRegs<kRowLoads, KB, VB>& regs) {
+        const bool drafts = !WINDOW && t >= last;
+        if (kQuant && !drafts) {
+            if constexpr (kQuant)
+#pragma unroll
+                for (int i = 0; i < kRowLoads; ++i)
+                    put(buf, kStepRows * i + lrow, quant_decode8<KB>(regs.k[i][0], regs.k[i][1], quant_scale_value(regs.ks[i])),
+                        quant_decode8<VB>(regs.v[i][0], regs.v[i][1], quant_scale_value(regs.vs[i])));
+            return;
+        }
+        const int first_draft = tile_base(t), most = tile_keys(t) - 1;
 #pragma unroll
         for (int i = 0; i < kRowLoads; ++i) {
             const int key = kStepRows * i + lrow;
-            u4v x = v[i];
-            if (!WINDOW && first_draft >= 0 && (first_draft + key > 63 || !((used >> (first_draft + key)) & 1)))
-                x = u4v{0u, 0u, 0u, 0u};
-            put(buf, key, as_h8(k[i]), as_h8(x));
-        }
-    };
-    // Puts tile t, loaded into regs, into LDS as float16.  Every wave of the block calls it, and
-    // for records it holds a barrier.
-    auto place = [&](int t, int buf, u4v (&regs)[kLoads]) {
-        if constexpr (kQuant) {
-            if (t >= last) {  // drafts: straight from memory, once a call
-                const int most = tile_keys(t) - 1;
-                u4v k[kRowLoads], v[kRowLoads];
-#pragma unroll
-                for (int i = 0; i < kRowLoads; ++i) {
-                    const int64_t from = (grp * a.t + tile_base(t) + min(kStepRows * i + lrow, most)) * 16 + lchunk;
-                    k[i] = static_cast<const u4v*>(a.Kt)[from];
-                    v[i] = static_cast<const u4v*>(a.Vt)[from];
-                }
-                put_rows(t, buf, k, v);
-                return;
+            u4v k, v;
+            if constexpr (kQuant) {  // drafts: straight from memory, once a call
+                const int64_t from = (grp * a.t + first_draft + min(key, most)) * 16 + lchunk;
+                k = static_cast<const u4v*>(a.Kt)[from];
+                v = static_cast<const u4v*>(a.Vt)[from];
+            } else {
+                k = regs.k[i];
+                v = regs.v[i];
             }
-            // Records that are not there: codes of 0, not what the bytes of another part would mean.
-            const int have = tile_keys(t) * (kRecord / 16);
-            if (have < kChunks)
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i)
-                    if (kTaThreads * i + tid >= have) regs[i] = u4v{0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                if (kTaThreads * (i + 1) <= kChunks || kTaThreads * i + tid < kChunks)
-                    reinterpret_cast<u4v*>(rt)[kTaThreads * i + tid] = regs[i];
-            __syncthreads();
-            u2v kc[kRowLoads], vc[kRowLoads];
-            uint32_t ks[kRowLoads], vs[kRowLoads];
-#pragma unroll
-            for (int i = 0; i < kRowLoads; ++i) {
-                const unsigned char* p = rt + (kStepRows * i + lrow) * kRecord;
-                kc[i] = quant_load8<KB>(p + lchunk * KB);
-                vc[i] = quant_load8<VB>(p + quant_code_bytes(KB) + lchunk * VB);
-                ks[i] = p[quant_code_bytes(KB) + quant_code_bytes(VB) + (lchunk >> 2)];
-                vs[i] = p[quant_code_bytes(KB) + quant_code_bytes(VB) + 4 + (lchunk >> 2)];
-            }
-#pragma unroll
-            for (int i = 0; i < kRowLoads; ++i)
-                put(buf, kStepRows * i + lrow, quant_decode8<KB>(kc[i][0], kc[i][1], quant_scale_value(ks[i])),
-                    quant_decode8<VB>(vc[i][0], vc[i][1], quant_scale_value(vs[i])));
-        } else {
-            put_rows(t, buf, regs, regs + kRowLoads);
+            if (drafts && (first_draft + key > 63 || !((used >> (first_draft + key)) & 1))) v = u4v{0u, 0u, 0u, 0u};
+            put(buf, key, as_h8(k), as_h8(v));
         }
     };
 
@@ -196,37 +178,21 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
         }
     };
 
-    u4v regs[2][kLoads];
+    TileRegs<kRowLoads, KB, VB> regs[2];
     if (first < end) load(first, regs[0]);
     if (first + 1 < end) load(first + 1, regs[1]);
-    if constexpr (kQuant) {
-        // place() waits for every wave to be done with the tile before: at its own barrier, or,
-        // for drafts, at this one.
-        auto turn = [&](int t, u4v (&r)[kLoads]) {
-            if (t >= last) __syncthreads();
-            place(t, 0, r);
-            if (t + 2 < end) load(t + 2, r);
-            __syncthreads();
-            compute(t, 0);
-        };
-        for (int t = first; t < end; t += 2) {
-            turn(t, regs[0]);
-            if (t + 1 < end) turn(t + 1, regs[1]);
-        }
-    } else {
-        if (first < end) place(first, 0, regs[0]);
-        if (first + 2 < end) load(first + 2, regs[0]);
-        // Tile t lies in buffer b; r holds tile t + 1 and takes tile t + 3.
-        auto turn = [&](int t, int b, u4v (&r)[kLoads]) {
-            __syncthreads();
-            compute(t, b);
-            if (t + 1 < end) place(t + 1, b ^ 1, r);
-            if (t + 3 < end) load(t + 3, r);
-        };
-        for (int t = first; t < end; t += 2) {
-            turn(t, 0, regs[1]);
-            if (t + 1 < end) turn(t + 1, 1, regs[0]);
-        }
+    if (first < end) place(first, 0, regs[0]);
+    if (first + 2 < end) load(first + 2, regs[0]);
+    // Tile t lies in buffer b; r holds tile t + 1 and takes tile t + 3.
+    auto turn = [&](int t, int b, TileRegs<kRowLoads, KB, VB>& r) {
+        __syncthreads();
+        compute(t, b);
+        if (t + 1 < end) place(t + 1, b ^ 1, r);
+        if (t + 3 < end) load(t + 3, r);
+    };
+    for (int t = first; t < end; t += 2) {
+        turn(t, 0, regs[1]);
+        if (t + 1 < end) turn(t + 1, 1, regs[0]);
     }
 
     __syncthreads();
