@@ -351,6 +351,25 @@ void chunk_plan(ChunkArgs& a) {
     a.splits = (int32_t)(splits < 1 ? 1 : splits);
 }
 
+// Both forms' times in ns, fitted to 120 calls of 1 to 256 tokens, 1 to 128 (sequence, KV head)s
+// and windows of 512 to 16384 rows: 1 x 8 x 4 heads, 4096 rows, 16 tokens: 19 us here, 85 in the
+// prompt form; 128 tokens 39 and 89; 16 x 8 x 4, 4096 rows, 64 tokens 148 and 157, 128 tokens 232
+// and 172; 512 rows, 32 tokens 37 and 26.
+bool few_tokens(const ChunkArgs& a) {
+    if (a.t > 1024) return false;
+    const double groups = (double)a.batch * a.hkv, rows = (double)a.g * a.t, all = (double)(a.n + a.t);
+    auto tiles = [&](double tokens) {
+        const double keys = (double)a.sink + (double)a.window + tokens;
+        return (keys < all ? keys : all) / 64;
+    };
+    const double blocks = groups * a.g * ((a.t + 127) / 128);
+    // Two launches and the parts' way through memory; 64 rows of K and V, or the work on them.
+    const double few = 12000 + groups * rows + groups * tiles(a.t) * (rows > 92 ? 0.0586 * rows : 5.4);
+    // A tile's latency, or the blocks' work once they fill the chip.
+    const double prompt = 4000 + tiles(a.t < 128 ? a.t : 128) * (blocks > 325 ? 4.3 * blocks : 1400);
+    return few < prompt;
+}
+
 size_t chunk_part_bytes(const ChunkArgs& a) {
     return a.splits > 1 ? (size_t)a.batch * a.hkv * a.g * a.t * (size_t)a.splits * (kD + 2) * 4 : 0;
 }

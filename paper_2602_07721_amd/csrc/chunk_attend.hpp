@@ -46,9 +46,9 @@ hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s);
 hipError_t launch_tile_attend(const ChunkArgs& a, int block, int row_tiles, int64_t groups, const char* name,
                               hipStream_t s);
 
-// Whether the sliding window takes the few-token form: blocks of it share a sequence's keys,
-// blocks of the prompt form hold 128 tokens of a head.
-inline bool few_tokens(const ChunkArgs& a) { return a.t <= 16; }
+// Whether a sliding-window call takes the few-token form: its blocks share a sequence's keys,
+// those of the prompt form hold 128 tokens of one head and walk all of theirs.
+bool few_tokens(const ChunkArgs& a);
 
 // The prompt form of the sliding window (many new tokens): the same arguments, float16 out.
 hipError_t launch_prompt_attend(const ChunkArgs& a, hipStream_t s);

@@ -64,8 +64,9 @@ __global__ __launch_bounds__(kQuThreads) void quantize_rows_kernel(const uint4* 
     const int64_t r = quant_first_row(rows, row, (int)(grp / hkv)) + i;
     if (i >= t || r < 0 || r >= capacity) return;  // all 16 lanes of a row together
     const int lane = threadIdx.x & 63, l16 = lane & 15;
-    const uint4 k = K[(grp * src_capacity + i) * 16 + l16];
-    const uint4 v = V[(grp * src_capacity + i) * 16 + l16];
+    const u4v k4 = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(K) + (grp * src_capacity + i) * 16 + l16);
+    const u4v v4 = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(V) + (grp * src_capacity + i) * 16 + l16);
+    const uint4 k{k4[0],k4[1],k4[2],k4[3]}, v{v4[0],v4[1],v4[2],v4[3]};
     const uint32_t sk = block_scale<KB>(k), sv = block_scale<VB>(v);
     uint8_t* out = rec + (grp * capacity + r) * kRecord;
     store_codes<KB>(out, l16, quant_encode8<KB>(k, sk));

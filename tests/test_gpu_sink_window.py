@@ -87,17 +87,17 @@ def test_more_than_eight_kv_heads_and_sequences():
 
 
 def test_both_forms_agree():
-    # 16 tokens by the few-token form, the same among 40 by the prompt form.
-    b, hkv, g, pos, t = 2, 2, 4, 1000, 40
+    # 4 tokens by the form whose blocks share the keys, the same among 1100 by the other.
+    b, hkv, g, pos, t = 2, 2, 4, 1000, 1100
     r = np.random.default_rng(3)
     K, V, q = draw(r, b, hkv, pos + t, D), draw(r, b, hkv, pos + t, D), draw(r, b, hkv * g, t, D)
     cfg = _cfg(hkv, g)
     whole = pk.sink_window_attend(cfg, gpu(q), gpu(K), gpu(V), pos, 8, 300, SCALE).cpu().numpy()
-    part = pk.sink_window_attend(cfg, gpu(q[:, :, :16]), gpu(K), gpu(V), pos, 8, 300, SCALE).cpu().numpy()
+    part = pk.sink_window_attend(cfg, gpu(q[:, :, :4]), gpu(K), gpu(V), pos, 8, 300, SCALE).cpu().numpy()
     for s in range(b):
         for h in range(hkv * g):
             tol = tolerance(q[s, h], K[s, h // g], V[s, h // g], half_out=True)
-            check(whole[s, h, :16], part[s, h].astype(np.float64), 2 * tol, f"seq {s} head {h}")
+            check(whole[s, h, :4], part[s, h].astype(np.float64), 2 * tol, f"seq {s} head {h}")
 
 
 def test_captured_calls_replay():
@@ -128,3 +128,19 @@ def test_captured_calls_replay():
             call()
             torch.cuda.synchronize()
             assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("b,hkv,g,pos,t,window", [
+    (1, 2, 4, 3000, 1, 2048), (1, 1, 16, 3000, 2, 2048), (2, 1, 8, 4000, 8, 3000), (1, 2, 4, 4000, 40, 4000),
+    (1, 1, 7, 5000, 19, 4500), (1, 1, 2, 6000, 300, 4000), (9, 1, 1, 2500, 70, 2500), (1, 1, 1, 9000, 1000, 9000)])
+def test_long_windows_with_shared_keys(b, hkv, g, pos, t, window):
+    # Blocks share a sequence's keys: 16, 32, 64 and 128 rows of it a block, and more.
+    _run(b, hkv, g, pos, t, 100, window, seed=t)
+    _run(b, hkv, g, pos, t, 0, window, seed=t, starts=list(np.linspace(0, pos, b).astype(int)),
+         counts=[max(1, t - i) for i in range(b)])
+
+
+@pytest.mark.parametrize("b,hkv,g,pos,t,window", [(1, 2, 4, 200, 1, 64), (2, 4, 4, 300, 9, 30), (40, 8, 2, 64, 33, 500)])
+def test_short_windows_in_one_launch(b, hkv, g, pos, t, window):
+    _run(b, hkv, g, pos, t, 5, window, seed=t, starts=[(7 * i) % (pos + 1) for i in range(b)],
+         counts=[(5 * i) % (t + 1) for i in range(b)])
