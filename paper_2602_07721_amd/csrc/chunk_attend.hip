@@ -133,7 +133,7 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
         }
         const bool sink = WINDOW && st < sink_steps;
         r.base = sink ? st * kCaKeys : span.lo + (st - sink_steps) * kCaKeys;
-        r.valid = (sink ? span.sink_end : span.hi) - r.base;
+        r.valid = min((sink ? span.sink_end : span.hi) - r.base, kCaKeys);
         const int64_t at = grp * a.capacity + r.base;
         if constexpr (kQuant) {
             r.rec = a.rec + at * kRecord;

@@ -135,12 +135,13 @@ __device__ __forceinline__ void leave_idle(const ChunkArgs& a, const ChunkPlace&
 // Drafts that some token of the sequence sees, bit by bit; the others may hold anything.  Every
 // lane of the wave calls it.
 __device__ __forceinline__ uint64_t used_drafts(const ChunkArgs& a, int seq, int lane) {
-    if (!a.mask) return ~0ull;
+    const uint64_t there = ~0ull >> (64 - a.t);
+    if (!a.mask) return there;
     uint64_t used = lane < a.t ? (uint64_t)a.mask[(int64_t)seq * a.t + lane] : 0ull;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1)
         used |= (uint64_t)lane_xor((uint32_t)used, m, lane) | (uint64_t)lane_xor((uint32_t)(used >> 32), m, lane) << 32;
-    return used;
+    return used & there;
 }
 // Which of the drafts first, first + 1, ... (valid of them) token tok sees.
 __device__ __forceinline__ uint32_t draft_bits(const ChunkArgs& a, int seq, int tok, int first, int valid) {

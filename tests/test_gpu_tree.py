@@ -165,6 +165,52 @@ def test_a_long_cache_passes_32_bit_offsets():
     assert abs(out[0, 0, 0, 0] - want) <= 2 * (4 * np.sqrt(128) * 2.0 ** -24 * score + 2.0 ** -20)
 
 
+def test_a_long_quantised_cache_passes_32_bit_offsets():
+    # 127 million records of 272 bytes: records, their 16-byte pieces and bytes all pass 2^31.
+    n, t = 127_000_000, 2
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GB")
+    cfg = _cfg(1, 2)
+    cache = pk.QuantCache.empty(cfg, 1, n)
+    cache.rec.zero_()
+    r = np.random.default_rng(1)
+    q = draw(r, 1, 2, t, D)
+    k, v = np.zeros((1, 1, 1, D), np.float16), np.ones((1, 1, 1, D), np.float16)
+    k[0, 0, 0] = quant.round_trip((4 * q[0, 0, 0].astype(np.float32)).astype(np.float16), 8)
+    pk.quantize_rows(cfg, cache, gpu(k), gpu(v), 0, n - 3, 1)
+    Kt, Vt = torch.zeros((2, 1, 1, t, D), dtype=torch.float16, device="cuda")
+    for scale in (SCALE, 4 * SCALE):  # two kernels' worth of rows: 2 heads x 2 drafts, and 33 rows below
+        out = pk.quant_tree_attend(cfg, gpu(q), cache, Kt, Vt, n, scale).cpu().numpy()
+        score = scale * (k[0, 0, 0].astype(np.float64) * q[0, 0, 0]).sum()
+        want = np.exp(score) / (np.exp(score) + n - 1 + 1)
+        assert abs(out[0, 0, 0, 0] - want) <= 2 * (4 * np.sqrt(128) * 2.0 ** -24 * score + 2.0 ** -20) + n * 2.0 ** -33
+    cfg33 = _cfg(1, 3)
+    q33 = np.repeat(q[:, :1, :1], 33, axis=1).reshape(1, 3, 11, D)
+    Kt, Vt = torch.zeros((2, 1, 1, 11, D), dtype=torch.float16, device="cuda")
+    out = pk.quant_tree_attend(cfg33, gpu(q33), cache, Kt, Vt, n, 4 * SCALE).cpu().numpy()
+    assert np.abs(out[0, :, 0, 0] - want).max() <= 2 * (4 * np.sqrt(128) * 2.0 ** -24 * score + 2.0 ** -20) + n * 2.0 ** -33
+
+
+def test_mask_bits_past_the_drafts_are_ignored():
+    # The last draft is seen by nobody and holds NaN; bits t .. 63 are set in every word.
+    b, hkv, g, n, t = 1, 2, 4, 100, 5
+    r = np.random.default_rng(4)
+    q, K, V = draw(r, b, hkv * g, t, D), draw(r, b, hkv, n, D), draw(r, b, hkv, n, D)
+    Kt, Vt = draw(r, b, hkv, t, D), draw(r, b, hkv, t, D)
+    Kt[:, :, -1] = Vt[:, :, -1] = np.nan
+    see = random_tree(r, t)
+    see[:, -1] = False
+    words = mask_words(see) | np.int64(-1 << t)
+    for g_ in (g, 16):
+        qq = draw(r, b, hkv * g_, t, D)
+        out = pk.tree_attend(_cfg(hkv, g_), gpu(qq), gpu(K), gpu(V), gpu(Kt), gpu(Vt), n, SCALE, mask=gpu(words[None])).cpu().numpy()
+        for h in range(hkv * g_):
+            k_, v_ = np.concatenate([K[0, h // g_], Kt[0, h // g_, :-1]]), np.concatenate([V[0, h // g_], Vt[0, h // g_, :-1]])
+            vis = np.concatenate([np.ones((t, n), bool), see[:, :-1]], 1)
+            check(out[0, h], attend64(qq[0, h], k_, v_, vis), tolerance(qq[0, h], k_, v_), f"head {h}")
+
+
 def test_two_streams_and_their_own_workspaces():
     b, hkv, g, n, t = 2, 2, 4, 3000, 8
     r = np.random.default_rng(6)
