@@ -1,8 +1,8 @@
 // Attention of a few new tokens per sequence over a long cache, on matrix instructions.
 //
 // The g heads of a KV head times the t new tokens are M = g t rows over the same keys; a wave
-// holds 16 NQ of them.  Per wave and 32 keys:
-//   S^T = K Q^T    a lane holds 8 keys' scores of one row per tile of 16 rows,
+// holds 16 or 32 of them.  Per wave and 32 keys:
+//   S^T = K Q^T    a lane holds 8 or 16 keys' scores of one row,
 //   P              exp2 of the scores less the row's running maximum,
 //   O^T += V^T P^T the scores' own registers are the second operand: matrix instructions sum
 //                  over 32 keys in any order, as long as both operands agree on it.
@@ -32,14 +32,13 @@ constexpr int kCaWaves = 4;  // waves of a block
 
 // LDS of one wave: its V and its records, later its state.
 constexpr int kCaVBytes = kCaKeys * kD * 2;
-constexpr int ca_wave_lds(int nq, int record) {
-    const int v = kCaVBytes + kCaKeys * record, o = ca_state_bytes(nq);
+constexpr int ca_wave_lds(int rows, int record) {
+    const int v = kCaVBytes + kCaKeys * record, o = ca_state_bytes(rows);
     return v > o ? v : o;
 }
 
-// Registers of 32 keys of a wave, as loaded.  Float16 K: lane l holds key l % 16 of each half, of
-// the dims that step_dim names; V: 8 loads of 4 whole rows.  Records: the 32 of them as they
-// lie, 1 KB a load.
+// Registers of 32 keys of a wave, as loaded.  Float16 K: the operand that ChunkRows names; V: 8
+// loads of 4 whole rows.  Records: the 32 of them as they lie, 1 KB a load.
 template <int KB, int VB>
 struct StepRegs {
     static constexpr int kChunks = kCaKeys * quant_record_bytes(KB, VB) / 16;
@@ -48,15 +47,8 @@ struct StepRegs {
 template <>
 struct StepRegs<16, 16> {
     static constexpr int kChunks = 0;
-    u4v k[2][4], v[8];
+    u4v k[8], v[8];
 };
-
-// Dims of matrix step c that lane group l / 16 holds start here.  A quantised key's lane group
-// holds one whole block (one scale a lane); a float16 key's four lanes read 64 bytes in a row.
-template <bool QUANT>
-__device__ __forceinline__ int step_dim(int c, int grp) {
-    return QUANT ? 32 * grp + 8 * c : 32 * c + 8 * grp;
-}
 
 // A step's 32 keys: rows of a float16 cache, of the drafts or of a quantised cache, of which the
 // first `valid` exist.
@@ -69,24 +61,25 @@ struct StepRows {
     int drafts;  // < 0, or the number of the draft that key 0 is
 };
 
-template <int NQ, int KB, int VB, bool WINDOW>
+template <int R, int KB, int VB, bool WINDOW>
 __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArgs a, int row_tiles, int64_t groups) {
     constexpr bool kQuant = KB < 16;
     constexpr int kRecord = kQuant ? quant_record_bytes(KB, VB) : 0;
     constexpr int kChunks = StepRegs<KB, VB>::kChunks;
     constexpr int kLoads = (kChunks + 63) / 64;
-    constexpr int kWaveLds = ca_wave_lds(NQ, kRecord);
+    constexpr int kWaveLds = ca_wave_lds(R, kRecord);
     // Steps whose loads are in flight: two of records where the registers hold them (32 rows and
     // 8-bit codes do not leave room), one of float16 rows.
-    constexpr int kAhead = kQuant && (NQ == 1 || kLoads <= 5) ? 2 : 1;
+    constexpr int kAhead = kQuant && (R == 16 || kLoads <= 5) ? 2 : 1;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kCaWaves * kWaveLds];
 
     const ChunkPlace pl = chunk_place(a, row_tiles, groups);
     const int64_t grp = pl.grp;
     const int seq = pl.seq;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, lg = lane >> 4;
-    const int M = a.g * a.t, row0 = pl.tile * 16 * NQ;
+    using Rows = ChunkRows<R>;
+    constexpr int kHalves = Rows::kHalves, kSteps = Rows::kSteps;
+    const int M = a.g * a.t, row0 = pl.tile * R;
     const KeySpan span = key_span(a, seq, 0, a.t);
 
     // Steps of 32 keys: the sinks', the cached stretch's; this share's part of them, and the
@@ -97,28 +90,20 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
     const int first = min(pl.split * a.per, steps), last = closing ? steps : min(first + a.per, steps);
     const int draft_steps = (!WINDOW && closing) ? (a.t + kCaKeys - 1) / kCaKeys : 0;
     const int end = last + draft_steps;
-    if (first >= end && a.splits > 1) return leave_idle(a, pl, groups, row0, 16 * NQ);
+    if (first >= end && a.splits > 1) return leave_idle(a, pl, groups, row0, R);
 
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-    h8v qf[NQ][4];
-    int tok[NQ];  // token of this lane's row
+    const int row = min(row0 + Rows::row(lane), M - 1), tok = row % a.t;  // this lane's
+    const __half* qr = static_cast<const __half*>(a.q) + (grp * M + row) * kD;
+    h8v qf[kSteps];
 #pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-        const int r = min(row0 + 16 * x + col, M - 1);
-        tok[x] = r % a.t;
-        const __half* qr = static_cast<const __half*>(a.q) + (grp * M + r) * kD;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            qf[x][c] = query_part(*reinterpret_cast<const u4v*>(qr + step_dim<kQuant>(c, lg)), flip);
-    }
-    ChunkRows<NQ> rows;
-    rows.init(score_factor(a.scale));
+    for (int c = 0; c < kSteps; ++c)
+        qf[c] = query_part(*reinterpret_cast<const u4v*>(qr + Rows::template dim<kQuant>(c, lane)), flip);
+    Rows rows(score_factor(a.scale), lane);
 
     unsigned char* vt = lds + wave * kWaveLds;
     unsigned char* rt = vt + kCaVBytes;  // the step's records
-    // Where this lane's transposing reads begin: key 4 lg + col / 4 of a half, dims 16 d + 4 (col % 4).
-    const int tkey = 4 * lg + (col >> 2);
-    const unsigned char* tr = vt + tkey * 256 + ((col & 3) >> 1) * 16 + (col & 1) * 8;
+    const int vrow = lane >> 4, vchunk = lane & 15;  // of a load or a store of 4 rows of V
 
     auto rows_of = [&](int st) {
         StepRows r{};
@@ -153,13 +138,13 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                regs.v[i] = reinterpret_cast<const u4v*>(r.v + min(4 * i + lg, r.valid - 1) * kD)[col];
+                regs.v[i] = reinterpret_cast<const u4v*>(r.v + min(4 * i + vrow, r.valid - 1) * kD)[vchunk];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    regs.k[h][c] = *reinterpret_cast<const u4v*>(r.k + min(16 * h + col, r.valid - 1) * kD +
-                                                                 step_dim<false>(c, lg));
+                for (int c = 0; c < kSteps; ++c)
+                    regs.k[h * kSteps + c] = *reinterpret_cast<const u4v*>(
+                        r.k + min(Rows::key(h, lane), r.valid - 1) * kD + Rows::template dim<false>(c, lane));
         }
     };
     const uint64_t used = draft_steps > 0 ? used_drafts(a, seq, lane) : ~0ull;
@@ -190,48 +175,49 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
             uint32_t vs[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const unsigned char* p = rt + (4 * i + lg) * kRecord + quant_code_bytes(KB);
-                vc[i] = quant_load8<VB>(p + col * VB);
-                vs[i] = p[quant_code_bytes(VB) + 4 + (col >> 2)];
+                const unsigned char* p = rt + (4 * i + vrow) * kRecord + quant_code_bytes(KB);
+                vc[i] = quant_load8<VB>(p + vchunk * VB);
+                vs[i] = p[quant_code_bytes(VB) + 4 + (vchunk >> 2)];
             }
-            u4v kc[2][KB / 4];
-            float ks[2];
+            // 128 / kHalves bits of codes a step of 8 dims, and a scale for every 4 of them.
+            constexpr int kWords = kSteps * KB / 16;
+            u4v kc[kHalves][kWords];
+            float ks[kHalves][kSteps / 4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const unsigned char* p = rt + (16 * h + col) * kRecord;
+            for (int h = 0; h < kHalves; ++h) {
+                const unsigned char* p = rt + Rows::key(h, lane) * kRecord;
+                const int d0 = Rows::template dim<true>(0, lane);
 #pragma unroll
-                for (int c = 0; c < KB / 4; ++c) kc[h][c] = reinterpret_cast<const u4v*>(p + lg * (4 * KB))[c];
-                ks[h] = quant_scale_value(p[quant_code_bytes(KB) + quant_code_bytes(VB) + lg]);
+                for (int c = 0; c < kWords; ++c) kc[h][c] = reinterpret_cast<const u4v*>(p + d0 * KB / 8)[c];
+#pragma unroll
+                for (int c = 0; c < kSteps / 4; ++c)
+                    ks[h][c] = quant_scale_value(p[quant_code_bytes(KB) + quant_code_bytes(VB) + d0 / 32 + c]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                put_v(vt, 4 * i + lg, col, quant_decode8<VB>(vc[i][0], vc[i][1], quant_scale_value(vs[i])));
+                put_v(vt, 4 * i + vrow, vchunk, quant_decode8<VB>(vc[i][0], vc[i][1], quant_scale_value(vs[i])));
             wave_lds_order();
             rows.scores(qf, [&](int h, int c) {
                 if constexpr (KB == 8)
-                    return quant_decode8<8>(kc[h][c / 2][2 * (c % 2)], kc[h][c / 2][2 * (c % 2) + 1], ks[h]);
+                    return quant_decode8<8>(kc[h][c / 2][2 * (c % 2)], kc[h][c / 2][2 * (c % 2) + 1], ks[h][c / 4]);
                 else
-                    return quant_decode8<4>(kc[h][0][c], 0u, ks[h]);
+                    return quant_decode8<4>(kc[h][c / 4][c % 4], 0u, ks[h][c / 4]);
             });
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 u4v v = reg.v[i];
-                if (!WINDOW && cur.drafts >= 0 && !((used >> (cur.drafts + 4 * i + lg)) & 1)) v = u4v{0u, 0u, 0u, 0u};
-                put_v(vt, 4 * i + lg, col, as_h8(v));
+                if (!WINDOW && cur.drafts >= 0 && !((used >> (cur.drafts + 4 * i + vrow)) & 1)) v = u4v{0u, 0u, 0u, 0u};
+                put_v(vt, 4 * i + vrow, vchunk, as_h8(v));
             }
             wave_lds_order();
-            rows.scores(qf, [&](int h, int c) { return as_h8(reg.k[h][c]); });
+            rows.scores(qf, [&](int h, int c) { return as_h8(reg.k[h * kSteps + c]); });
             if (ahead < main_end) load(rows_of(ahead), reg);
         }
-        uint32_t w[NQ];
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            w[x] = bits_to(cur.valid - 1);
-            if constexpr (WINDOW) w[x] &= window_bits(span.start + tok[x], cur.base, (int)a.sink, (int)a.window);
-            else if (!kQuant && cur.drafts >= 0) w[x] = draft_bits(a, seq, tok[x], cur.drafts, cur.valid);
-        }
-        rows.accumulate(w, tr, tkey, lg);
+        uint32_t w = bits_to(cur.valid - 1);
+        if constexpr (WINDOW) w &= window_bits(span.start + tok, cur.base, (int)a.sink, (int)a.window);
+        else if (!kQuant && cur.drafts >= 0) w = draft_bits(a, seq, tok, cur.drafts, cur.valid);
+        rows.accumulate(w, vt, lane);
     };
 
     int st = first + wave;
@@ -252,27 +238,24 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
             wave_lds_order();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int key = 4 * i + lg;
-                u4v v = reinterpret_cast<const u4v*>(r.v + min(key, r.valid - 1) * kD)[col];
+                const int key = 4 * i + vrow;
+                u4v v = reinterpret_cast<const u4v*>(r.v + min(key, r.valid - 1) * kD)[vchunk];
                 if (!((used >> (r.drafts + key)) & 1)) v = u4v{0u, 0u, 0u, 0u};
-                put_v(vt, key, col, as_h8(v));
+                put_v(vt, key, vchunk, as_h8(v));
             }
             wave_lds_order();
             rows.scores(qf, [&](int h, int c) {
-                return as_h8(*reinterpret_cast<const u4v*>(r.k + min(16 * h + col, r.valid - 1) * kD +
-                                                           step_dim<true>(c, lg)));
+                return as_h8(*reinterpret_cast<const u4v*>(r.k + min(Rows::key(h, lane), r.valid - 1) * kD +
+                                                           Rows::template dim<true>(c, lane)));
             });
-            uint32_t w[NQ];
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) w[x] = draft_bits(a, seq, tok[x], r.drafts, r.valid);
-            rows.accumulate(w, tr, tkey, lg);
+            rows.accumulate(draft_bits(a, seq, tok, r.drafts, r.valid), vt, lane);
         }
     }
 
     __syncthreads();
-    rows.leave(vt, col, lg);
+    rows.leave(vt, lane);
     __syncthreads();
-    join_waves<NQ, kCaWaves, WINDOW>(a, pl, groups, row0, span.tokens, lds, kWaveLds, threadIdx.x >> 5, 2 * kCaWaves);
+    join_waves<R, kCaWaves, WINDOW>(a, pl, groups, row0, span.tokens, lds, kWaveLds, threadIdx.x >> 5, 2 * kCaWaves);
 }
 
 // Joins the shares' states of a row: 8 groups of 32 lanes take every eighth share, 4 dims a lane.
@@ -391,17 +374,17 @@ hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s) {
         };
         auto rows = [&](auto k16, auto k32) { block == 16 ? go(k16) : go(k32); };
         if (a.window > 0)
-            rows(chunk_attend_kernel<1, 16, 16, true>, chunk_attend_kernel<2, 16, 16, true>);
+            rows(chunk_attend_kernel<16, 16, 16, true>, chunk_attend_kernel<32, 16, 16, true>);
         else if (!a.rec)
-            rows(chunk_attend_kernel<1, 16, 16, false>, chunk_attend_kernel<2, 16, 16, false>);
+            rows(chunk_attend_kernel<16, 16, 16, false>, chunk_attend_kernel<32, 16, 16, false>);
         else if (a.k_bits == 8 && a.v_bits == 8)
-            rows(chunk_attend_kernel<1, 8, 8, false>, chunk_attend_kernel<2, 8, 8, false>);
+            rows(chunk_attend_kernel<16, 8, 8, false>, chunk_attend_kernel<32, 8, 8, false>);
         else if (a.k_bits == 8)
-            rows(chunk_attend_kernel<1, 8, 4, false>, chunk_attend_kernel<2, 8, 4, false>);
+            rows(chunk_attend_kernel<16, 8, 4, false>, chunk_attend_kernel<32, 8, 4, false>);
         else if (a.v_bits == 8)
-            rows(chunk_attend_kernel<1, 4, 8, false>, chunk_attend_kernel<2, 4, 8, false>);
+            rows(chunk_attend_kernel<16, 4, 8, false>, chunk_attend_kernel<32, 4, 8, false>);
         else
-            rows(chunk_attend_kernel<1, 4, 4, false>, chunk_attend_kernel<2, 4, 4, false>);
+            rows(chunk_attend_kernel<16, 4, 4, false>, chunk_attend_kernel<32, 4, 4, false>);
         e = hipGetLastError();
     }
     if (e != hipSuccess || a.splits == 1) return e;

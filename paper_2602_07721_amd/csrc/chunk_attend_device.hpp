@@ -83,14 +83,14 @@ __device__ __forceinline__ KeySpan key_span(const ChunkArgs& a, int seq, int i0,
     return s;
 }
 
-// ---- few new tokens: a wave's 16 NQ rows over steps of 32 keys
+// ---- few new tokens: a wave's 16 or 32 rows over steps of 32 keys
 
 constexpr int kCaKeys = 32;      // keys of a step
 constexpr float kCaUp = 8.f;     // P is held scaled by 2^8 ...
 constexpr float kCaSlack = 7.f;  // ... and grows by up to 2^7 before the maximum is raised
 constexpr int kCaRow = kD + 4;   // floats of an output row in LDS (spreads the rows over the banks)
 // LDS of a wave's outputs [row][kCaRow], maxima and sums.
-constexpr int ca_state_bytes(int nq) { return 16 * nq * (kCaRow + 2) * 4; }
+constexpr int ca_state_bytes(int rows) { return rows * (kCaRow + 2) * 4; }
 
 // What a block works on: tile `tile` of the rows of (sequence, KV head) grp, share `split` of its keys.
 struct ChunkPlace {
@@ -155,133 +155,208 @@ __device__ __forceinline__ void put_v(unsigned char* vt, int key, int chunk, h8v
     *reinterpret_cast<h8v*>(vt + key * 256 + ((chunk ^ (2 * (key & 7))) << 4)) = v;
 }
 
-// The softmax of NQ tiles of 16 rows.  Lane l = col + 16 lg: row col of each tile.
-template <int NQ>
-struct ChunkRows {
-    // A row's running maximum m as nm = 8 - m (P = 2^(c2 s + nm); infinite before the first key),
-    // its sum over this lane's keys, its outputs: dims 16 d + 4 lg + i.
-    float nm[NQ], sum[NQ], c2;
-    f4v o[NQ][8];
-    // A step's scores: keys 16 h + 4 lg + i.
-    f4v s[NQ][2];
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) s4v* lds_s4v;
 
-    __device__ __forceinline__ void init(float factor) {
-        c2 = factor;
+// A wave's rows: their softmax, and how matrix instructions split them over the lanes.  R rows
+// and 32 keys a step: S^T = K Q^T in kHalves blocks of keys and kSteps steps of dims, O^T +=
+// V^T P^T with the scores' registers as the second operand.  32 rows take instructions of 32 x
+// 32, which occupy the issue of the vector units half as long as those of 16 x 16.
+template <int R>
+struct ChunkRows;
+
+// P of two neighbouring scores of a row as two float16 values each: hi, and what hi leaves.
+__device__ __forceinline__ void split_p(float s0, float s1, float c2, float base, float& sum, h8v& hi, h8v& lo, int at) {
+    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s0, c2, base));
+    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s1, c2, base));
+    sum += p0 + p1;
+    // Two values an instruction; p - hi is exact.
+    const h2v ph = __builtin_convertvector((f2v{p0, p1}), h2v);
+    const h2v pl = __builtin_convertvector((f2v{__builtin_fmaf((float)ph[0], -1.f, p0),
+                                                __builtin_fmaf((float)ph[1], -1.f, p1)}), h2v);
+    hi[at] = ph[0];
+    hi[at + 1] = ph[1];
+    lo[at] = pl[0];
+    lo[at + 1] = pl[1];
+}
+
+// 16 rows.  Lane l = col + 16 lg: row col, keys 16 h + 4 lg + i, outputs of dims 16 d + 4 lg + i.
+template <>
+struct ChunkRows<16> {
+    static constexpr int kHalves = 2, kSteps = 4;
+    // The running maximum m as nm = 8 - m (P = 2^(c2 s + nm); infinite before the first key), the
+    // sum over this lane's keys.
+    float nm = __builtin_huge_valf(), sum = 0.f, c2;
+    f4v o[8], s[2];
+    int lg, tkey;
+
+    __device__ __forceinline__ ChunkRows(float factor, int lane) : c2(factor), lg(lane >> 4), tkey(4 * (lane >> 4) + ((lane & 15) >> 2)) {
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            nm[x] = __builtin_huge_valf();
-            sum[x] = 0.f;
+        for (int d = 0; d < 8; ++d) o[d] = f4v{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ static int row(int lane) { return lane & 15; }
+    // This lane's part of step c of a key (of the row's query): key(lane) of half h, 8 dims from
+    // dim() on.  BLOCKS: as a quantised key's lane group likes it, one block of 32 dims each.
+    template <bool BLOCKS>
+    __device__ __forceinline__ static int dim(int c, int lane) {
+        return BLOCKS ? 32 * (lane >> 4) + 8 * c : 32 * c + 8 * (lane >> 4);
+    }
+    __device__ __forceinline__ static int key(int h, int lane) { return 16 * h + (lane & 15); }
+
+    template <class F>
+    __device__ __forceinline__ void scores(const h8v (&qf)[kSteps], F&& kpart) {
 #pragma unroll
-            for (int d = 0; d < 8; ++d) o[x][d] = f4v{0.f, 0.f, 0.f, 0.f};
-        }
+        for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kpart(h, c), qf[c],
+                                                              c == 0 ? f4v{0.f, 0.f, 0.f, 0.f} : s[h], 0, 0, 0);
     }
 
-    // S^T = K Q^T of 32 keys: kpart(h, c) gives the operand of half h, matrix step c.
-    template <class F>
-    __device__ __forceinline__ void scores(const h8v (&qf)[NQ][4], F&& kpart) {
+    // With the step's V in LDS at vt; bits of w: the keys that the row sees.
+    __device__ __forceinline__ void accumulate(uint32_t w, const unsigned char* vt, int lane) {
+        if (__builtin_expect(!__all(w == ~0u), 0)) {
+            const uint32_t b = w >> (4 * lg);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(b & (1u << (16 * h + i)))) s[h][i] = -__builtin_huge_valf();
+        }
+        float top = -__builtin_huge_valf();
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const h8v kf = kpart(h, c);
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, s[h][i]);
+        top *= c2;
+        if (__any(top > -__builtin_huge_valf() && !(top + nm <= kCaUp + kCaSlack))) {
+            const float to = kCaUp - rows_max(top);  // inf where the row saw nothing in this step
+            if (to < nm) {
+                const float c = __builtin_amdgcn_exp2f(to - nm);  // 0 before the first key
+                nm = to;
+                sum *= c;
 #pragma unroll
-                for (int x = 0; x < NQ; ++x)
-                    s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                        kf, qf[x][c], c == 0 ? f4v{0.f, 0.f, 0.f, 0.f} : s[x][h], 0, 0, 0);
-            }
-    }
-
-    // O^T += V^T P^T from the scores and the step's V in LDS; bits of w[x]: the keys row tile x
-    // sees.  tkey = 4 lg + col / 4 and tr = where this lane's transposing reads of V begin.
-    __device__ __forceinline__ void accumulate(const uint32_t (&w)[NQ], const unsigned char* tr, int tkey, int lg) {
-        bool all_seen = true, raise = false;
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) all_seen &= w[x] == ~0u;
-        if (!__all(all_seen)) {
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) {
-                const uint32_t b = w[x] >> (4 * lg);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!(b & (1u << (16 * h + i)))) s[x][h][i] = -__builtin_huge_valf();
+                for (int d = 0; d < 8; ++d) o[d] *= c;
             }
         }
-        float top[NQ];
+        const float base = nm < __builtin_huge_valf() ? nm : 0.f;
+        h8v hi, lo;
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            top[x] = -__builtin_huge_valf();
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top[x] = fmaxf(top[x], s[x][h][i]);
-            top[x] *= c2;
-            raise |= top[x] > -__builtin_huge_valf() && !(top[x] + nm[x] <= kCaUp + kCaSlack);
-        }
-        if (__any(raise)) {
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) {
-                const float to = kCaUp - rows_max(top[x]);  // inf where the row saw nothing in this step
-                if (to < nm[x]) {
-                    const float c = __builtin_amdgcn_exp2f(to - nm[x]);  // 0 before the first key
-                    nm[x] = to;
-                    sum[x] *= c;
-#pragma unroll
-                    for (int d = 0; d < 8; ++d) o[x][d] *= c;
-                }
-            }
-        }
-        h8v hi[NQ], lo[NQ];
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            const float base = nm[x] < __builtin_huge_valf() ? nm[x] : 0.f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][h][i], c2, base));
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][h][i + 1], c2, base));
-                    sum[x] += p0 + p1;
-                    // Two values an instruction; p - hi is exact.
-                    const h2v ph = __builtin_convertvector((f2v{p0, p1}), h2v);
-                    const h2v pl = __builtin_convertvector((f2v{__builtin_fmaf((float)ph[0], -1.f, p0),
-                                                                __builtin_fmaf((float)ph[1], -1.f, p1)}), h2v);
-                    hi[x][4 * h + i] = ph[0];
-                    hi[x][4 * h + i + 1] = ph[1];
-                    lo[x][4 * h + i] = pl[0];
-                    lo[x][4 * h + i + 1] = pl[1];
-                }
-        }
+            for (int i = 0; i < 4; i += 2) split_p(s[h][i], s[h][i + 1], c2, base, sum, hi, lo, 4 * h + i);
+        const int col = lane & 15;
+        const unsigned char* tr = vt + tkey * 256 + ((col & 3) >> 1) * 16 + (col & 1) * 8;
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
-            typedef __attribute__((address_space(3))) s4v* lds_s4;
             const unsigned char* at = tr + ((d ^ (tkey & 7)) << 5);
-            const s4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at));
-            const s4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + 16 * 256));
-            const h8v vf = join_h4(v0, v1);
+            const h8v vf = join_h4(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(at)),
+                                   __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(at + 16 * 256)));
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, hi, o[d], 0, 0, 0);
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, lo, o[d], 0, 0, 0);
+        }
+    }
+
+    // Leaves the state in ca_state_bytes(16) of LDS.
+    __device__ __forceinline__ void leave(unsigned char* to, int lane) const {
+        float* so = reinterpret_cast<float*>(to);
+        const float l = rows_sum(sum);
+        const int r = lane & 15;
+        if (lg == 0) {
+            so[16 * kCaRow + r] = nm;
+            so[16 * (kCaRow + 1) + r] = l;
+        }
 #pragma unroll
-            for (int x = 0; x < NQ; ++x) {
-                o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, hi[x], o[x][d], 0, 0, 0);
-                o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, lo[x], o[x][d], 0, 0, 0);
+        for (int d = 0; d < 8; ++d) *reinterpret_cast<f4v*>(so + r * kCaRow + 16 * d + 4 * lg) = o[d];
+    }
+};
+
+// 32 rows.  Lane l = col + 32 half: row col, keys 8 (i / 4) + 4 half + i % 4, outputs of dims
+// 32 d + 8 (i / 4) + 4 half + i % 4.
+template <>
+struct ChunkRows<32> {
+    static constexpr int kHalves = 1, kSteps = 8;
+    float nm = __builtin_huge_valf(), sum = 0.f, c2;
+    f16v o[4], s;
+    int half, tkey, tchunk;
+
+    __device__ __forceinline__ ChunkRows(float factor, int lane)
+        : c2(factor), half(lane >> 5), tkey(4 * (lane >> 5) + ((lane & 15) >> 2)),
+          tchunk(2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    }
+    __device__ __forceinline__ static int row(int lane) { return lane & 31; }
+    template <bool BLOCKS>
+    __device__ __forceinline__ static int dim(int c, int lane) {
+        return BLOCKS ? 64 * (lane >> 5) + 8 * c : 16 * c + 8 * (lane >> 5);
+    }
+    __device__ __forceinline__ static int key(int, int lane) { return lane & 31; }
+
+    template <class F>
+    __device__ __forceinline__ void scores(const h8v (&qf)[kSteps], F&& kpart) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < kSteps; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kpart(0, c), qf[c], s, 0, 0, 0);
+    }
+
+    __device__ __forceinline__ void accumulate(uint32_t w, const unsigned char* vt, int lane) {
+        if (__builtin_expect(!__all(w == ~0u), 0)) {
+            const uint32_t b = w >> (4 * half);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(b & (1u << (8 * (i / 4) + i % 4)))) s[i] = -__builtin_huge_valf();
+        }
+        float top = -__builtin_huge_valf();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+        top *= c2;
+        if (__any(top > -__builtin_huge_valf() && !(top + nm <= kCaUp + kCaSlack))) {
+            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            const float to = kCaUp - fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            if (to < nm) {
+                const float c = __builtin_amdgcn_exp2f(to - nm);
+                nm = to;
+                sum *= c;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) o[d] *= c;
+            }
+        }
+        const float base = nm < __builtin_huge_valf() ? nm : 0.f;
+        const unsigned char* tr = vt + tkey * 256 + (lane & 1) * 8;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            h8v hi, lo;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) split_p(s[8 * k + i], s[8 * k + i + 1], c2, base, sum, hi, lo, i);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const unsigned char* at = tr + 16 * k * 256 + (((4 * d + tchunk) ^ (2 * tkey)) << 4);
+                const h8v vf = join_h4(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(at)),
+                                       __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(at + 8 * 256)));
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, hi, o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo, o[d], 0, 0, 0);
             }
         }
     }
 
-    // Leaves the state in ca_state_bytes(NQ) of LDS.
-    __device__ __forceinline__ void leave(unsigned char* to, int col, int lg) const {
+    __device__ __forceinline__ void leave(unsigned char* to, int lane) const {
         float* so = reinterpret_cast<float*>(to);
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            const float l = rows_sum(sum[x]);
-            const int r = 16 * x + col;
-            if (lg == 0) {
-                so[16 * NQ * kCaRow + r] = nm[x];
-                so[16 * NQ * (kCaRow + 1) + r] = l;
-            }
-#pragma unroll
-            for (int d = 0; d < 8; ++d) *reinterpret_cast<f4v*>(so + r * kCaRow + 16 * d + 4 * lg) = o[x][d];
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+        const int r = lane & 31;
+        if (half == 0) {
+            so[32 * kCaRow + r] = nm;
+            so[32 * (kCaRow + 1) + r] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
         }
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<f4v*>(so + r * kCaRow + 32 * d + 8 * j + 4 * half) =
+                    f4v{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
     }
 };
 
@@ -298,28 +373,27 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int d
     }
 }
 
-// Joins the states that WAVES waves left `stride` bytes apart for rows [row0, row0 + 16 NQ) of
+// Joins the states that WAVES waves left `stride` bytes apart for rows [row0, row0 + R) of
 // group grp, and writes the rows, or the share's part of them.  32 lanes a row, 4 dims a lane;
 // `sub` of `subs` such sets of lanes.
-template <int NQ, int WAVES, bool WINDOW>
+template <int R, int WAVES, bool WINDOW>
 __device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace& pl, int64_t groups, int row0, int tokens,
                                            const unsigned char* states, int stride, int sub, int subs) {
-    constexpr int kRows = 16 * NQ;
     const int M = a.g * a.t, d4 = threadIdx.x & 31;
     const float* of = reinterpret_cast<const float*>(states);
-    for (int r = sub; r < kRows; r += subs) {
+    for (int r = sub; r < R; r += subs) {
         if (row0 + r >= M) break;
         float top = __builtin_huge_valf();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fminf(top, of[w * (stride / 4) + kRows * kCaRow + r]);
+        for (int w = 0; w < WAVES; ++w) top = fminf(top, of[w * (stride / 4) + R * kCaRow + r]);
         float l = 0.f;
         f4v acc{0.f, 0.f, 0.f, 0.f};
         if (top < __builtin_huge_valf())
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 const float* ow = of + w * (stride / 4);
-                const float c = __builtin_amdgcn_exp2f(top - ow[kRows * kCaRow + r]);
-                l += c * ow[kRows * (kCaRow + 1) + r];
+                const float c = __builtin_amdgcn_exp2f(top - ow[R * kCaRow + r]);
+                l += c * ow[R * (kCaRow + 1) + r];
                 acc += c * *reinterpret_cast<const f4v*>(ow + r * kCaRow + 4 * d4);
             }
         const int64_t row = pl.grp * M + row0 + r;

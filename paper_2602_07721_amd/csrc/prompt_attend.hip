@@ -25,7 +25,6 @@ __device__ __forceinline__ void to_lds(const u4v* from, u4v* lds) {
                                      (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);
 }
 
-typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int kPaThreads = 256;
 constexpr int kPaTokens = 128;  // tokens of a block

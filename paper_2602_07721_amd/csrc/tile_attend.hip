@@ -32,7 +32,8 @@ struct TileRegs<N, 16, 16> {
 
 template <int SETS, int KB, int VB, bool WINDOW>
 __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a, int row_tiles, int64_t groups) {
-    constexpr int NQ = 2;
+    constexpr int R = 32;  // rows of a wave
+    using Rows = ChunkRows<R>;
     constexpr bool kQuant = KB < 16;
     constexpr int kRecord = kQuant ? quant_record_bytes(KB, VB) : 0;
     constexpr int kParts = kTaWaves / SETS;      // waves that share a set's keys
@@ -40,7 +41,7 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
     constexpr int kTile = kCaKeys * kParts * kSub;  // keys of a tile
     constexpr int kRowLoads = kTile * 16 / kTaThreads;  // 16-byte pieces of K (of V) a thread holds
     constexpr int kTileBytes = kTile * kD * 2;
-    constexpr int kUse = 4 * kTileBytes, kState = ca_state_bytes(NQ);  // two buffers of K and V
+    constexpr int kUse = 4 * kTileBytes, kState = ca_state_bytes(R);  // two buffers of K and V
     constexpr int kLds = kUse > kTaWaves * kState ? kUse : kTaWaves * kState;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kLds];
 
@@ -49,8 +50,7 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
     const int seq = pl.seq;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = wave % kParts, set = wave / kParts;
-    const int col = lane & 15, lg = lane >> 4;
-    const int M = a.g * a.t, row0 = (pl.tile * SETS + set) * 16 * NQ;
+    const int M = a.g * a.t, row0 = (pl.tile * SETS + set) * R;
     const KeySpan span = key_span(a, seq, 0, a.t);
 
     // Tiles: the sinks', the cached stretch's; this share's part of them, and the drafts behind
@@ -61,21 +61,15 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
     const bool closing = pl.split == a.splits - 1;  // takes what is left, and the drafts
     const int first = min(pl.split * per, tiles), last = closing ? tiles : min(first + per, tiles);
     const int end = last + ((!WINDOW && closing) ? (a.t + kTile - 1) / kTile : 0);
-    if (first >= end && a.splits > 1) return leave_idle(a, pl, groups, pl.tile * SETS * 16 * NQ, SETS * 16 * NQ);
+    if (first >= end && a.splits > 1) return leave_idle(a, pl, groups, pl.tile * SETS * R, SETS * R);
 
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-    h8v qf[NQ][4];
-    int tok[NQ];
+    const int row = min(row0 + Rows::row(lane), M - 1), tok = row % a.t;  // this lane's
+    const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) + (grp * M + row) * kD);
+    h8v qf[Rows::kSteps];
 #pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-        const int r = min(row0 + 16 * x + col, M - 1);
-        tok[x] = r % a.t;
-        const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) + (grp * M + r) * kD);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) qf[x][c] = query_part(qr[4 * c + lg], flip);
-    }
-    ChunkRows<NQ> rows;
-    rows.init(score_factor(a.scale));
+    for (int c = 0; c < Rows::kSteps; ++c) qf[c] = query_part(qr[Rows::dim<false>(c, lane) / 8], flip);
+    Rows rows(score_factor(a.scale), lane);
 
     // Of a tile: cache row (or draft) of its first key, and how many of its keys there are.
     auto tile_base = [&](int t) {
@@ -152,10 +146,6 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
         }
     };
 
-    // Where this lane's reads of a tile begin: its K operands and its transposing reads of V.
-    const int tkey = 4 * lg + (col >> 2);
-    const unsigned char* kr = kt + (part * kSub * kCaKeys + col) * 256;
-    const unsigned char* tr = vt + (part * kSub * kCaKeys + tkey) * 256 + ((col & 3) >> 1) * 16 + (col & 1) * 8;
     auto compute = [&](int t, int buf) {
         if (row0 >= M) return;
 #pragma unroll 1
@@ -163,18 +153,15 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
             const int at = (part * kSub + sub) * kCaKeys;
             const int base = tile_base(t) + at, valid = tile_keys(t) - at;
             if (valid <= 0) return;
-            const unsigned char* ks = kr + buf * kTileBytes + sub * kCaKeys * 256;
-            rows.scores(qf, [&](int h, int c) {
-                return *reinterpret_cast<const h8v*>(ks + 16 * h * 256 + (((4 * c + lg) ^ col) << 4));
+            const int from = buf * kTileBytes + at * 256, key = Rows::key(0, lane);
+            rows.scores(qf, [&](int, int c) {
+                return *reinterpret_cast<const h8v*>(kt + from + key * 256 +
+                                                     (((Rows::dim<false>(c, lane) / 8) ^ (key & 15)) << 4));
             });
-            uint32_t w[NQ];
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) {
-                w[x] = bits_to(valid - 1);
-                if constexpr (WINDOW) w[x] &= window_bits(span.start + tok[x], base, (int)a.sink, (int)a.window);
-                else if (t >= last) w[x] = draft_bits(a, seq, tok[x], base, valid);
-            }
-            rows.accumulate(w, tr + buf * kTileBytes + sub * kCaKeys * 256, tkey, lg);
+            uint32_t w = bits_to(valid - 1);
+            if constexpr (WINDOW) w &= window_bits(span.start + tok, base, (int)a.sink, (int)a.window);
+            else if (t >= last) w = draft_bits(a, seq, tok, base, valid);
+            rows.accumulate(w, vt + from, lane);
         }
     };
 
@@ -196,9 +183,9 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
     }
 
     __syncthreads();
-    rows.leave(lds + wave * kState, col, lg);
+    rows.leave(lds + wave * kState, lane);
     __syncthreads();
-    join_waves<NQ, kParts, WINDOW>(a, pl, groups, row0, span.tokens, lds + set * kParts * kState, kState,
+    join_waves<R, kParts, WINDOW>(a, pl, groups, row0, span.tokens, lds + set * kParts * kState, kState,
                                    (tid >> 5) % (2 * kParts), 2 * kParts);
 }
 
