@@ -461,6 +461,8 @@ typedef struct pariskv_quant_cache {
     int32_t host_mapped; /* 0 or 1 */
 } pariskv_quant_cache;
 
+#define PARISKV_MAX_QUANT_ROWS (1 << 27) /* rows of a (sequence, KV head) written or read in one call */
+
 /* Bytes of one record; 0 for other numbers of bits.  Host only. */
 size_t pariskv_quant_record_bytes(int32_t k_bits, int32_t v_bits);
 
@@ -468,7 +470,8 @@ size_t pariskv_quant_record_bytes(int32_t k_bits, int32_t v_bits);
  * (device float16 [batch][Hkv][src_capacity][D]) into t rows of the cache, from
  * `row` on, or, with rows (device int32 [batch]) non-NULL, from rows[b] on in
  * sequence b; then rows that fall outside [0, capacity) are not written.
- * Errors: INVALID, CAPACITY (row + t > capacity, rows NULL), HIP. */
+ * Errors: INVALID, UNSUPPORTED (t > PARISKV_MAX_QUANT_ROWS), CAPACITY (row + t >
+ * capacity, rows NULL), HIP. */
 int pariskv_quantize_rows(const pariskv_config* cfg, const pariskv_quant_cache* cache, const void* K,
                           const void* V, int64_t src_capacity, int64_t src_row, int64_t row,
                           const int32_t* rows, int64_t t, int32_t batch, void* stream);
@@ -477,7 +480,7 @@ int pariskv_quantize_rows(const pariskv_config* cfg, const pariskv_quant_cache* 
  * [dst_row, dst_row + t) of K and V (device float16 [batch][Hkv][dst_capacity][D]).
  * With rows, destination rows whose cache row falls outside [0, capacity) are
  * left as they were.
- * Errors: INVALID, CAPACITY (row + t > capacity, rows NULL), HIP. */
+ * Errors: those of pariskv_quantize_rows. */
 int pariskv_dequantize_rows(const pariskv_config* cfg, const pariskv_quant_cache* cache, int64_t row,
                             const int32_t* rows, int64_t t, void* K, void* V, int64_t dst_capacity,
                             int64_t dst_row, int32_t batch, void* stream);
@@ -509,7 +512,8 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
 /* Verification of drafted tokens (t of every sequence, 1 = a dense decode step):
  * token i attends the sequence's cached rows and the drafted tokens that its
  * mask names, its ancestors in the tree of drafts and itself,
- *   o_i = sum_j softmax_j(scale <k_j, q_i>) v_j.
+ *   o_i = sum_j softmax_j(scale <k_j, q_i>) v_j
+ * in float32 (scores have to be finite there).
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D], the cached rows
  *   n       cached rows of every sequence, 0..kv_capacity; with lens (device
@@ -558,7 +562,7 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
  *           aligned; overwritten, so calls that overlap need one each
  * t = 0 does nothing.
  * Errors: INVALID (also pos + t > kv_capacity, window < 1), UNSUPPORTED (more
- * than 2^31-1 blocks), WORKSPACE, HIP. */
+ * than 2^24 - 1 blocks of 128 tokens of a query head), WORKSPACE, HIP. */
 int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const void* K, const void* V,
                                int64_t kv_capacity, int64_t pos, const int32_t* starts, int64_t t,
                                const int32_t* counts, int64_t sink, int64_t window, int32_t batch, float scale,

@@ -887,6 +887,9 @@ static int check_quant_rows(const pariskv_config* cfg, const pariskv_quant_cache
     if (t < 0 || at < 0 || at > kv_capacity - t)
         return fail(PARISKV_ERR_INVALID, "K/V rows [%lld, %lld + %lld) outside [0, %lld)", (long long)at, (long long)at,
                     (long long)t, (long long)kv_capacity);
+    // A launch has at most 2^32 - 1 threads, 16 a row.
+    if (t > PARISKV_MAX_QUANT_ROWS)
+        return fail(PARISKV_ERR_UNSUPPORTED, "%lld rows in one call, above %d", (long long)t, PARISKV_MAX_QUANT_ROWS);
     if (!rows && row < 0) return fail(PARISKV_ERR_INVALID, "row %lld < 0", (long long)row);
     if (!rows && row > cache->capacity - t)
         return fail(PARISKV_ERR_CAPACITY, "rows [%lld, %lld + %lld) exceed cache capacity %lld", (long long)row,
@@ -1082,7 +1085,8 @@ static int check_sink_window_sizes(const pariskv_config* cfg, int32_t batch, int
     if (sink < 0 || window < 1)
         return fail(PARISKV_ERR_INVALID, "sink %lld < 0 or window %lld < 1", (long long)sink, (long long)window);
     const int64_t heads = (int64_t)batch * cfg->n_kv_heads * cfg->q_per_kv;
-    if (heads * ((t + 127) / 128) > INT32_MAX)
+    // A launch has at most 2^32 - 1 threads, and a block of 256 takes 128 tokens of a head.
+    if (heads * ((t + 127) / 128) > UINT32_MAX / 256)
         return fail(PARISKV_ERR_UNSUPPORTED, "%lld query heads x %lld tokens", (long long)heads, (long long)t);
     return PARISKV_OK;
 }

@@ -51,7 +51,8 @@ def test_record_bytes():
     (dict(cache=None), pk.ERR_INVALID), (dict(K=0), pk.ERR_INVALID), (dict(V=FAKE + 2), pk.ERR_INVALID),
     (dict(kv_cap=0), pk.ERR_INVALID), (dict(at=-1), pk.ERR_INVALID), (dict(at=41), pk.ERR_INVALID),
     (dict(t=-1), pk.ERR_INVALID), (dict(row=-1), pk.ERR_INVALID), (dict(row=91), pk.ERR_CAPACITY),
-    (dict(rows=FAKE + 2), pk.ERR_INVALID), (dict(batch=0), pk.ERR_INVALID), (dict(batch=10000), pk.ERR_UNSUPPORTED)])
+    (dict(rows=FAKE + 2), pk.ERR_INVALID), (dict(batch=0), pk.ERR_INVALID), (dict(batch=10000), pk.ERR_UNSUPPORTED),
+    (dict(t=2 ** 27 + 1, kv_cap=2 ** 28, cache=_cache(cap=2 ** 28)), pk.ERR_UNSUPPORTED)])
 def test_row_copies_refuse(change, code):
     a = dict(cache=_cache(), K=FAKE, V=FAKE, kv_cap=50, at=0, row=0, rows=0, t=10, batch=1)
     a.update(change)
@@ -131,7 +132,7 @@ def test_tree_attend_refuses_caches():
     (dict(q=0), pk.ERR_INVALID), (dict(K=FAKE + 8), pk.ERR_INVALID), (dict(out=0), pk.ERR_INVALID),
     (dict(starts=FAKE + 2), pk.ERR_INVALID), (dict(counts=FAKE + 2), pk.ERR_INVALID), (dict(ws=0), pk.ERR_WORKSPACE),
     (dict(ws_bytes=0), pk.ERR_WORKSPACE), (dict(batch=0), pk.ERR_INVALID),
-    (dict(batch=8000, t=2 ** 23, cap=2 ** 29), pk.ERR_UNSUPPORTED)])
+    (dict(batch=8000, pos=0, t=262 * 128 + 1, cap=2 ** 29), pk.ERR_UNSUPPORTED)])
 def test_sink_window_attend_refuses(change, code):
     a = dict(q=FAKE, K=FAKE, cap=100, pos=96, starts=0, t=4, counts=0, sink=4, window=32, batch=1, scale=0.1, out=FAKE,
              ws=FAKE, ws_bytes=1 << 20)
