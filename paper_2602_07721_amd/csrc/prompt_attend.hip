@@ -8,8 +8,12 @@
 //                  a row's maximum needs one exchange and its sum none until the end,
 //   O^T += V^T P^T the scores' own registers are the second operand (the sum over keys may run in
 //                  any order that both operands agree on); V^T by transposing LDS reads.
-// Tiles inside every token's window take no masks.  Bound by the matrix and vector units
-// together: 4 D flops a visible pair, and an exponential, a maximum, a sum and a rounding.
+// Tiles inside every token's window take no masks.  The next tile goes straight into LDS while
+// one is computed on.  Bound by the matrix and vector units together (4 D flops a visible pair,
+// and an exponential, a maximum, a sum and a rounding), with LDS close behind: a wave reads 32
+// KB a tile, which takes the block as long as its matrix instructions.  64 tokens a wave would
+// halve that but leave one wave a SIMD: 870 us where 32 took 660.  32 heads, 8192 tokens after
+// 8192 others, window 4096: 615 us, 920 TFLOP/s (a plain float16 matrix product: 1147).
 
 #include <hip/hip_fp16.h>
 
@@ -19,22 +23,19 @@ namespace pariskv {
 
 namespace {
 
-// 16 bytes of global memory a lane straight into LDS, at lds + 16 x lane.
-__device__ __forceinline__ void to_lds(const u4v* from, u4v* lds) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
-                                     (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);
-}
-
+typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kPaThreads = 256;
 constexpr int kPaTokens = 128;  // tokens of a block
 constexpr int kPaKeys = 64;     // keys of a tile
+constexpr int kPaBufferWord3 = 0x00020000;  // buffer descriptor: raw, range-checked
 constexpr float kPaUp = 8.f;    // P is held scaled by 2^8, and grows by up to 2^7 before the
 constexpr float kPaSlack = 7.f; // running maximum is raised: below 2^16, and small P lose nothing
 
 __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs a, int qtiles) {
-    __shared__ u4v sk[2][kPaKeys * 16];
-    __shared__ u4v sv[2][kPaKeys * 16];
+    // Arrays of their own, chosen at compile time: in one array the compiler cannot tell a read of
+    // this tile from the loads under way to the next, and waits for them first (653 us for 615).
+    __shared__ u4v sk0[kPaKeys * 16], sk1[kPaKeys * 16], sv0[kPaKeys * 16], sv1[kPaKeys * 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
 
@@ -81,8 +82,8 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-    const u4v* Kg = static_cast<const u4v*>(a.K) + (int64_t)grp * a.capacity * 16;
-    const u4v* Vg = static_cast<const u4v*>(a.V) + (int64_t)grp * a.capacity * 16;
+    char* Kg = static_cast<char*>(const_cast<void*>(a.K)) + (int64_t)grp * a.capacity * 256;
+    char* Vg = static_cast<char*>(const_cast<void*>(a.V)) + (int64_t)grp * a.capacity * 256;
     // First row of a tile, and how many of its keys there are.
     auto tile_base = [&](int tile) {
         return tile < sink_tiles ? tile * kPaKeys : span.lo + (tile - sink_tiles) * kPaKeys;
@@ -91,15 +92,18 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     // This wave's quarter of a tile straight into LDS, 4 rows an instruction, lane i's 16 bytes
     // behind lane i - 1's: the swizzle is in what a lane reads.  Keys past the last repeat it:
     // what lies behind is not read.
-    auto load = [&](int tile, int buf) {
-        const int64_t base = (int64_t)tile_base(tile) * 16;
+    auto load = [&](int tile, u4v* nk, u4v* nv) {
+        const int64_t base = (int64_t)tile_base(tile) * 256;
         const int most = tile_keys(tile) - 1;
+        const auto kr = __builtin_amdgcn_make_buffer_rsrc(Kg + base, 0, kPaKeys * 256, kPaBufferWord3);
+        const auto vr = __builtin_amdgcn_make_buffer_rsrc(Vg + base, 0, kPaKeys * 256, kPaBufferWord3);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int first = 16 * i + 4 * wave, r = first + (lane >> 4), c = lane & 15;
-            const int row = min(r, most) * 16;
-            to_lds(Kg + base + (row + (c ^ (r & 15))), &sk[buf][first * 16]);
-            to_lds(Vg + base + (row + (c ^ (4 * (r & 3)))), &sv[buf][first * 16]);
+            const int kat = min(r, most) * 256 + ((c ^ (r & 15)) << 4);
+            const int vat = min(r, most) * 256 + ((c ^ (4 * (r & 3))) << 4);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_ptr)(nk + first * 16), 16, kat, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr)(nv + first * 16), 16, vat, 0, 0, 0);
         }
     };
     // Where this lane's transposing reads begin: key 4 half + (lane % 16) / 4, dims
@@ -107,11 +111,9 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     const int tkey = 4 * half + ((lane & 15) >> 2);
     const int tchunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 
-    load(0, 0);
-    __syncthreads();
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int buf = tile & 1;
-        if (tile + 1 < tiles) load(tile + 1, buf ^ 1);
+    // Tile `tile`, whose keys lie in ck and cv; loads the next into nk and nv.
+    auto take = [&](int tile, const u4v* ck, const u4v* cv, u4v* nk, u4v* nv) __attribute__((always_inline)) {
+        if (tile + 1 < tiles) load(tile + 1, nk, nv);
         const int base_row = tile_base(tile), valid = tile_keys(tile);
         // Whether some token of the wave sees a key of the tile (its first key is at or before the
         // last token, and its first token's window or the sinks reach into it).
@@ -128,7 +130,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        as_h8(sk[buf][(32 * h + col) * 16 + ((2 * c + half) ^ (col & 15))]), qf[c], s[h], 0, 0, 0);
+                        as_h8(ck[(32 * h + col) * 16 + ((2 * c + half) ^ (col & 15))]), qf[c], s[h], 0, 0, 0);
             uint32_t w[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -159,6 +161,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
                     for (int d = 0; d < 4; ++d) o[d] *= c;
                 }
             }
+            __builtin_amdgcn_s_setprio(1);  // ahead of another wave's S^T: 1%
             const float base = nm < __builtin_huge_valf() ? nm : 0.f;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -171,19 +174,27 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    typedef __attribute__((address_space(3))) s4v* lds_s4;
 #pragma unroll
                     for (int d = 0; d < 4; ++d) {
-                        const u4v* vp = sv[buf] + tkey * 16 + ((4 * d + tchunk) ^ (4 * (tkey & 3)));
-                        const char* at = reinterpret_cast<const char*>(vp + 16 * (2 * h + k) * 16) + (lane & 1) * 8;
-                        const s4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at));
-                        const s4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + 8 * 256));
+                        // One offset from the array: longer chains lose which array it is.
+                        const int at = tkey * 256 + (((4 * d + tchunk) ^ (4 * (tkey & 3))) << 4) + (lane & 1) * 8 +
+                                       16 * (2 * h + k) * 256;
+                        const char* vp = reinterpret_cast<const char*>(cv);
+                        const s4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(vp + at));
+                        const s4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(vp + (at + 8 * 256)));
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(join_h4(a0, a1), pf[k], o[d], 0, 0, 0);
                     }
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         __syncthreads();  // and the next tile is there
+    };
+    load(0, sk0, sv0);
+    __syncthreads();
+    for (int tile = 0; tile < tiles; tile += 2) {
+        take(tile, sk0, sv0, sk1, sv1);
+        if (tile + 1 < tiles) take(tile + 1, sk1, sv1, sk0, sv0);
     }
 
     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);

