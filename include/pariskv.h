@@ -522,7 +522,8 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
  *           (not in the cache: which of them stay is known after verification)
  *   mask    device int64 [batch][t]: bit j of word i lets token i attend draft
  *           j (bits from t on are ignored); NULL: a chain, drafts j <= i.
- *           Drafts that no token of their sequence attends may hold anything.
+ *           A draft's values, whatever they are (infinities, NaNs), reach only
+ *           the tokens that attend it.
  *   out     device float [batch][Hq][t][D]; zero where a token attends nothing
  *   workspace  device, >= pariskv_tree_workspace(...) bytes, 256-byte aligned;
  *           overwritten, so calls that overlap need one each
@@ -551,7 +552,9 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
  * or j > p - window (window >= pos + t: plain causal attention).
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D]: row j holds position j,
- *           the new tokens' rows among them
+ *           the new tokens' rows among them.  Rows that no new token of the
+ *           sequence attends may hold anything; one that holds infinities or
+ *           NaNs and that some new token attends may reach others of them, too
  *   pos     position of the first new token; with starts (device int32 [batch],
  *           or NULL) that of sequence b is min(max(starts[b], 0), pos)
  *   counts  device int32 [batch] or NULL: sequence b has min(max(counts[b], 0),

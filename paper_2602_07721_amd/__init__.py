@@ -807,7 +807,7 @@ def tree_attend(cfg, q, K, V, K_tree, V_tree, n, scale, mask=None, lens=None, ou
     """Attention of t <= 64 drafted tokens per sequence, q [batch][Hq][t][D], over the n cached rows of K, V
     [batch][Hkv][kv_capacity][D] (or lens[b] of them, int32 [batch]) and the drafts' own rows K_tree, V_tree
     [batch][Hkv][t][D]: token i attends draft j when bit j of mask[b, i] (int64 [batch][t]) is set, without a mask when
-    j <= i.  Returns out [batch][Hq][t][D] float32."""
+    j <= i.  Drafts reach only the tokens that attend them.  Returns out [batch][Hq][t][D] float32."""
     dev = []
     (qp, ktp, vtp, mp, lp, op, wp), batch, t, out, workspace = _tree_args(cfg, q, K_tree, V_tree, n, mask, lens, out,
                                                                           workspace, dev, stream)
@@ -843,7 +843,8 @@ def sink_window_attend(cfg, q, K, V, pos, sink, window, scale, starts=None, coun
     """Attention of t new tokens per sequence, q [batch][Hq][t][D] at positions pos .. pos + t - 1, over the cache rows
     (row = position) of K, V [batch][Hkv][kv_capacity][D] that each sees: j <= p with j < sink or j > p - window.
     starts (int32 [batch], at most pos) gives each sequence's first position, counts (int32 [batch]) how many of its t
-    tokens there are; rows of out behind them are left as they were.  Returns out [batch][Hq][t][D] float16."""
+    tokens there are; rows of out behind them are left as they were.  A row that some token attends and that is not
+    finite may reach the others.  Returns out [batch][Hq][t][D] float16."""
     torch = _torch()
     dev = []
     qp, batch, t = _tokens_arg(cfg, q, dev)

@@ -61,8 +61,9 @@ struct StepRows {
     int drafts;  // < 0, or the number of the draft that key 0 is
 };
 
+// 16 rows of float16 keys: 3 blocks a CU.
 template <int R, int KB, int VB, bool WINDOW>
-__global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArgs a, int row_tiles, int64_t groups) {
+__global__ __launch_bounds__(64 * kCaWaves, R == 16 && KB == 16 ? 3 : 2) void chunk_attend_kernel(ChunkArgs a, int row_tiles, int64_t groups) {
     constexpr bool kQuant = KB < 16;
     constexpr int kRecord = kQuant ? quant_record_bytes(KB, VB) : 0;
     constexpr int kChunks = StepRegs<KB, VB>::kChunks;
@@ -147,8 +148,7 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
                         r.k + min(Rows::key(h, lane), r.valid - 1) * kD + Rows::template dim<false>(c, lane));
         }
     };
-    const uint64_t used = draft_steps > 0 ? used_drafts(a, seq, lane) : ~0ull;
-
+    bool odd = false;  // a draft's V has values that are not finite
     // Quantised kernels take the drafts, which are float16, in a loop of their own.
     const int main_end = kQuant ? last : end;
     StepRegs<KB, VB> regs[kAhead];
@@ -205,10 +205,15 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
             });
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u4v v = reg.v[i];
-                if (!WINDOW && cur.drafts >= 0 && !((used >> (cur.drafts + 4 * i + vrow)) & 1)) v = u4v{0u, 0u, 0u, 0u};
-                put_v(vt, 4 * i + vrow, vchunk, as_h8(v));
+            for (int i = 0; i < 8; ++i) put_v(vt, 4 * i + vrow, vchunk, as_h8(reg.v[i]));
+            if (!WINDOW && cur.drafts >= 0) {
+                uint32_t m = 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) note_odd(reg.v[i], m);
+                if (__builtin_expect(__any(m & kOddBits), 0)) {
+                    odd = true;
+                    clean_v(vt, lane);
+                }
             }
             wave_lds_order();
             rows.scores(qf, [&](int h, int c) { return as_h8(reg.k[h * kSteps + c]); });
@@ -235,13 +240,18 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
     if constexpr (kQuant) {
         for (int ds = st - last; ds < draft_steps; ds += kCaWaves) {
             const StepRows r = rows_of(last + ds);
+            uint32_t m = 0u;
             wave_lds_order();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int key = 4 * i + vrow;
-                u4v v = reinterpret_cast<const u4v*>(r.v + min(key, r.valid - 1) * kD)[vchunk];
-                if (!((used >> (r.drafts + key)) & 1)) v = u4v{0u, 0u, 0u, 0u};
+                const u4v v = reinterpret_cast<const u4v*>(r.v + min(key, r.valid - 1) * kD)[vchunk];
+                note_odd(v, m);
                 put_v(vt, key, vchunk, as_h8(v));
+            }
+            if (__builtin_expect(__any(m & kOddBits), 0)) {
+                odd = true;
+                clean_v(vt, lane);
             }
             wave_lds_order();
             rows.scores(qf, [&](int h, int c) {
@@ -253,7 +263,7 @@ __global__ __launch_bounds__(64 * kCaWaves, 2) void chunk_attend_kernel(ChunkArg
     }
 
     __syncthreads();
-    rows.leave(vt, lane);
+    rows.leave(vt, lane, odd);
     __syncthreads();
     join_waves<R, kCaWaves, WINDOW>(a, pl, groups, row0, span.tokens, lds, kWaveLds, threadIdx.x >> 5, 2 * kCaWaves);
 }
@@ -268,6 +278,7 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
     const int d4 = threadIdx.x & 31, sub = threadIdx.x >> 5;
     const float2* state = part_state(a, groups, row);
     const f4v* part = reinterpret_cast<const f4v*>(a.part) + (int64_t)row * a.splits * (kD / 4) + d4;
+    const bool odd = __builtin_signbit(state[a.splits - 1].y);  // the last share's: the drafts are its
     float top = __builtin_huge_valf(), l = 0.f;
     f4v acc{0.f, 0.f, 0.f, 0.f};
     for (int s = sub; s < a.splits; s += kCcGroups) {
@@ -276,7 +287,7 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
         if (st.x == __builtin_huge_valf()) continue;  // saw no key; its outputs may not have been written
         const float to = fminf(top, st.x);
         const float c0 = __builtin_amdgcn_exp2f(to - top), c1 = __builtin_amdgcn_exp2f(to - st.x);
-        l = l * c0 + st.y * c1;
+        l = l * c0 + __builtin_fabsf(st.y) * c1;
         acc = acc * c0 + v * c1;
         top = to;
     }
@@ -292,6 +303,8 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
     for (int i = 0; i < kCcGroups; ++i) top = fminf(top, snm[i]);
     l = 0.f;
     acc = f4v{0.f, 0.f, 0.f, 0.f};
+    f4v other = acc;
+    if (!WINDOW && odd) other = other_part(a, row, d4);
     if (top < __builtin_huge_valf())
 #pragma unroll
         for (int i = 0; i < kCcGroups; ++i) {
@@ -304,7 +317,7 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
         const uint32_t M = (uint32_t)(a.g * a.t);
         real = (int)(row % M % (uint32_t)a.t) < a.counts[row / M / (uint32_t)a.hkv];
     }
-    store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, real);
+    store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, other, real);
 }
 
 }  // namespace

@@ -132,27 +132,58 @@ __device__ __forceinline__ void leave_idle(const ChunkArgs& a, const ChunkPlace&
         part_state(a, groups, pl.grp * M + r)[pl.split] = float2{__builtin_huge_valf(), 0.f};
 }
 
-// Drafts that some token of the sequence sees, bit by bit; the others may hold anything.  Every
-// lane of the wave calls it.
-__device__ __forceinline__ uint64_t used_drafts(const ChunkArgs& a, int seq, int lane) {
-    const uint64_t there = ~0ull >> (64 - a.t);
-    if (!a.mask) return there;
-    uint64_t used = lane < a.t ? (uint64_t)a.mask[(int64_t)seq * a.t + lane] : 0ull;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1)
-        used |= (uint64_t)lane_xor((uint32_t)used, m, lane) | (uint64_t)lane_xor((uint32_t)(used >> 32), m, lane) << 32;
-    return used & there;
-}
 // Which of the drafts first, first + 1, ... (valid of them) token tok sees.
 __device__ __forceinline__ uint32_t draft_bits(const ChunkArgs& a, int seq, int tok, int first, int valid) {
     const uint64_t m = a.mask ? (uint64_t)a.mask[(int64_t)seq * a.t + tok] : ~0ull >> (63 - tok);
     return first > 63 ? 0u : (uint32_t)(m >> first) & bits_to(valid - 1);
 }
 
+// Draft values that are not finite.  A draft that a token does not see has a weight of 0 there, but
+// 0 times infinity is not 0, and a branch of the tree that overflows must not spoil the others.
+// So the products get such values as 0, and the rows that see them have them added at the end:
+// infinities and NaNs come out of any weight as they are.
+//
+// Sets bits of kOddBits in m if one of v's 8 values is such a value (all ones in its exponent).
+constexpr uint32_t kOddBits = 0x80008000u;
+__device__ __forceinline__ void note_odd(u4v v, uint32_t& m) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m |= (v[i] & 0x7c007c00u) + 0x04000400u;
+}
+__device__ __forceinline__ u4v finite_part(u4v v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((v[i] & 0x7c00u) == 0x7c00u) v[i] &= 0xffff0000u;
+        if ((v[i] & 0x7c000000u) == 0x7c000000u) v[i] &= 0xffffu;
+    }
+    return v;
+}
+// What finite_part left out of the drafts that row `row` sees, dims 4 d4 on.
+__device__ __forceinline__ f4v other_part(const ChunkArgs& a, int64_t row, int d4) {
+    const int64_t M = (int64_t)a.g * a.t, grp = row / M;
+    const int tok = (int)(row % M) % a.t;
+    const uint64_t m = a.mask ? (uint64_t)a.mask[grp / a.hkv * a.t + tok] : ~0ull >> (63 - tok);
+    const h4v* v = static_cast<const h4v*>(a.Vt) + grp * a.t * (kD / 4) + d4;
+    f4v sum{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < a.t; ++j) {
+        const h4v x = v[j * (kD / 4)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += ((m >> j) & 1) && !__builtin_isfinite((float)x[i]) ? (float)x[i] : 0.f;
+    }
+    return sum;
+}
+
 // 16 bytes of key `key`'s V (chunk `chunk` of 16) in a tile of V in LDS.  The XOR spreads the 16
 // rows of a transposing read over all banks.
 __device__ __forceinline__ void put_v(unsigned char* vt, int key, int chunk, h8v v) {
     *reinterpret_cast<h8v*>(vt + key * 256 + ((chunk ^ (2 * (key & 7))) << 4)) = v;
+}
+
+// The finite parts of a step's V that this wave has put into LDS.
+__device__ __forceinline__ void clean_v(unsigned char* vt, int lane) {
+    wave_lds_order();
+    u4v* at = reinterpret_cast<u4v*>(vt) + lane;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) at[64 * i] = finite_part(at[64 * i]);
 }
 
 typedef float f16v __attribute__((ext_vector_type(16)));
@@ -190,7 +221,8 @@ struct ChunkRows<16> {
     f4v o[8], s[2];
     int lg, tkey;
 
-    __device__ __forceinline__ ChunkRows(float factor, int lane) : c2(factor), lg(lane >> 4), tkey(4 * (lane >> 4) + ((lane & 15) >> 2)) {
+    __device__ __forceinline__ ChunkRows(float factor, int lane)
+        : c2(factor), lg(lane >> 4), tkey(4 * (lane >> 4) + ((lane & 15) >> 2)) {
 #pragma unroll
         for (int d = 0; d < 8; ++d) o[d] = f4v{0.f, 0.f, 0.f, 0.f};
     }
@@ -257,14 +289,14 @@ struct ChunkRows<16> {
         }
     }
 
-    // Leaves the state in ca_state_bytes(16) of LDS.
-    __device__ __forceinline__ void leave(unsigned char* to, int lane) const {
+    // Leaves the state in ca_state_bytes(16) of LDS; the sums' signs say `odd`.
+    __device__ __forceinline__ void leave(unsigned char* to, int lane, bool odd) const {
         float* so = reinterpret_cast<float*>(to);
         const float l = rows_sum(sum);
         const int r = lane & 15;
         if (lg == 0) {
             so[16 * kCaRow + r] = nm;
-            so[16 * (kCaRow + 1) + r] = l;
+            so[16 * (kCaRow + 1) + r] = odd ? -l : l;
         }
 #pragma unroll
         for (int d = 0; d < 8; ++d) *reinterpret_cast<f4v*>(so + r * kCaRow + 16 * d + 4 * lg) = o[d];
@@ -343,13 +375,14 @@ struct ChunkRows<32> {
         }
     }
 
-    __device__ __forceinline__ void leave(unsigned char* to, int lane) const {
+    __device__ __forceinline__ void leave(unsigned char* to, int lane, bool odd) const {
         float* so = reinterpret_cast<float*>(to);
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
         const int r = lane & 31;
         if (half == 0) {
             so[32 * kCaRow + r] = nm;
-            so[32 * (kCaRow + 1) + r] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+            const float l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+            so[32 * (kCaRow + 1) + r] = odd ? -l : l;
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d)
@@ -360,22 +393,24 @@ struct ChunkRows<32> {
     }
 };
 
-// 4 dims of an output row: float32, or float16 where the prompt's next product reads it.  Rows
-// of tokens that are not there are left as they were.
+// 4 dims of an output row, acc times inv and `other`: float32, or float16 where the prompt's next
+// product reads it.  Rows of tokens that are not there are left as they were.
 template <bool WINDOW>
-__device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int d4, float inv, f4v acc, bool real) {
+__device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int d4, float inv, f4v acc, f4v other,
+                                          bool real) {
     acc *= inv;
     if constexpr (WINDOW) {
         const h4v h{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
         if (real) static_cast<h4v*>(a.out)[row * (kD / 4) + d4] = h;
     } else {
-        static_cast<f4v*>(a.out)[row * (kD / 4) + d4] = acc;
+        static_cast<f4v*>(a.out)[row * (kD / 4) + d4] = acc + other;
     }
 }
 
 // Joins the states that WAVES waves left `stride` bytes apart for rows [row0, row0 + R) of
 // group grp, and writes the rows, or the share's part of them.  32 lanes a row, 4 dims a lane;
-// `sub` of `subs` such sets of lanes.
+// `sub` of `subs` such sets of lanes.  A negative sum says that a draft holds values that are not
+// finite, in a wave's state and in a share's part.
 template <int R, int WAVES, bool WINDOW>
 __device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace& pl, int64_t groups, int row0, int tokens,
                                            const unsigned char* states, int stride, int sub, int subs) {
@@ -387,22 +422,27 @@ __device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace&
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) top = fminf(top, of[w * (stride / 4) + R * kCaRow + r]);
         float l = 0.f;
+        bool odd = false;
         f4v acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) odd |= __builtin_signbit(of[w * (stride / 4) + R * (kCaRow + 1) + r]);
         if (top < __builtin_huge_valf())
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 const float* ow = of + w * (stride / 4);
                 const float c = __builtin_amdgcn_exp2f(top - ow[R * kCaRow + r]);
-                l += c * ow[R * (kCaRow + 1) + r];
+                l += c * __builtin_fabsf(ow[R * (kCaRow + 1) + r]);
                 acc += c * *reinterpret_cast<const f4v*>(ow + r * kCaRow + 4 * d4);
             }
         const int64_t row = pl.grp * M + row0 + r;
         if (a.splits > 1) {
             const int64_t at = row * a.splits + pl.split;
             reinterpret_cast<f4v*>(a.part)[at * (kD / 4) + d4] = acc;
-            if (d4 == 0) part_state(a, groups, row)[pl.split] = float2{top, l};
+            if (d4 == 0) part_state(a, groups, row)[pl.split] = float2{top, odd ? -l : l};
         } else {
-            store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, (row0 + r) % a.t < tokens);
+            f4v other{0.f, 0.f, 0.f, 0.f};
+            if (!WINDOW && odd) other = other_part(a, row, d4);
+            store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, other, (row0 + r) % a.t < tokens);
         }
     }
 }

@@ -120,8 +120,8 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
             }
         }
     };
-    const uint64_t used = end > last ? used_drafts(a, seq, lane) : ~0ull;
-    // Puts tile t, loaded into regs, into buffer buf as float16; drafts that nobody sees count as 0.
+    uint32_t odd = 0u;  // kOddBits: a draft's V has values that are not finite
+    // Puts tile t, loaded into regs, into buffer buf as float16.
     auto place = [&](int t, int buf, const TileRegs<kRowLoads, KB, VB>& regs) {
         const bool drafts = !WINDOW && t >= last;
         if (kQuant && !drafts) {
@@ -145,7 +145,10 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
                 k = regs.k[i];
                 v = regs.v[i];
             }
-            if (drafts && (first_draft + key > 63 || !((used >> (first_draft + key)) & 1))) v = u4v{0u, 0u, 0u, 0u};
+            if (drafts) {
+                note_odd(v, odd);
+                v = finite_part(v);
+            }
             put(buf, key, as_h8(k), as_h8(v));
         }
     };
@@ -186,8 +189,9 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
         if (t + 1 < end) turn(t + 1, 1, regs[0]);
     }
 
-    __syncthreads();
-    rows.leave(lds + wave * kState, lane);
+    const bool any_odd = !WINDOW && __syncthreads_or((odd & kOddBits) != 0u);
+    if (WINDOW) __syncthreads();
+    rows.leave(lds + wave * kState, lane, any_odd);
     __syncthreads();
     join_waves<R, kParts, WINDOW>(a, pl, groups, row0, span.tokens, lds + set * kParts * kState, kState,
                                    (tid >> 5) % (2 * kParts), 2 * kParts);

@@ -86,6 +86,49 @@ def test_masks_with_empty_rows_and_unseen_drafts(n, t):
         assert not out[:, :, -1].any()
 
 
+@pytest.mark.parametrize("bits", [None, (8, 8), (4, 4)])
+@pytest.mark.parametrize("n", [100, 3000])  # one share of the keys, several
+@pytest.mark.parametrize("g,t", [(1, 8), (4, 8), (4, 16), (4, 31), (2, 64)])
+def test_drafts_that_are_not_finite_reach_only_tokens_that_see_them(g, t, n, bits):
+    print(f"[tree] not finite: g {g} t {t} n {n} bits {bits}", flush=True)
+    b, hkv = 2, 2
+    r = np.random.default_rng(g + t + n)
+    cfg = _cfg(hkv, g)
+    K, V, q = draw(r, b, hkv, n, D), draw(r, b, hkv, n, D), draw(r, b, hkv * g, t, D)
+    Kt, Vt = draw(r, b, hkv, t, D), draw(r, b, hkv, t, D)
+    see = np.stack([random_tree(r, t) for _ in range(b)])
+    odd, lost = t // 2, t - 2  # a draft with such values, one whose score is NaN
+    bad = Vt.copy()
+    bad[:, :, odd, 3], bad[:, :, odd, 70], bad[:, :, odd, 127] = np.inf, -np.inf, np.nan
+    bad[:, :, odd + 1, 3] = np.inf
+    Vt[~np.isfinite(bad)] = 0
+    badk = Kt.copy()
+    badk[:, :, lost, 9] = np.nan
+    Kt[:, :, lost] = 0
+    mask = gpu(mask_words(see))
+    if bits:
+        cache = pk.QuantCache.empty(cfg, b, n, *bits)
+        pk.quantize_rows(cfg, cache, gpu(K), gpu(V), 0, 0, n)
+        K, V = quant.round_trip(K, bits[0]), quant.round_trip(V, bits[1])
+        out = pk.quant_tree_attend(cfg, gpu(q), cache, gpu(badk), gpu(bad), n, SCALE, mask=mask).cpu().numpy()
+    else:
+        out = pk.tree_attend(cfg, gpu(q), gpu(K), gpu(V), gpu(badk), gpu(bad), n, SCALE, mask=mask).cpu().numpy()
+    for s in range(b):
+        dead, visible = see[s, :, lost], np.concatenate([np.ones((t, n), bool), see[s]], 1)
+        for h in range(hkv * g):
+            x, rows = out[s, h], bad[s, h // g].astype(np.float32)
+            assert np.isnan(x[dead]).all()
+            # Of the drafts that a token sees, the sum of such values of each dim (inf, -inf or NaN), else 0.
+            odds = np.stack([np.where(np.isfinite(rows[m]), 0, rows[m]).sum(0) for m in see[s]])
+            hit = (odds != 0) & ~dead[:, None]
+            assert np.array_equal(x[hit], odds[hit], equal_nan=True)
+            k_ = np.concatenate([K[s, h // g], Kt[s, h // g]]).astype(np.float64)
+            v_ = np.concatenate([V[s, h // g], Vt[s, h // g]]).astype(np.float64)
+            fine = ~hit & ~dead[:, None]
+            want = attend64(q[s, h], k_, v_, visible)
+            check(x[fine], want[fine], tolerance(q[s, h], k_, v_), f"seq {s} head {h}")
+
+
 @pytest.mark.parametrize("t", [1, 32, 64])
 def test_chain_without_a_mask(t):
     _run(2, 2, 3, 300, t, mask="chain", seed=t)
