@@ -552,9 +552,8 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
  * or j > p - window (window >= pos + t: plain causal attention).
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D]: row j holds position j,
- *           the new tokens' rows among them.  Rows that no new token of the
- *           sequence attends may hold anything; one that holds infinities or
- *           NaNs and that some new token attends may reach others of them, too
+ *           the new tokens' rows among them.  A row's values, whatever they are
+ *           (infinities, NaNs), reach only the tokens that attend it
  *   pos     position of the first new token; with starts (device int32 [batch],
  *           or NULL) that of sequence b is min(max(starts[b], 0), pos)
  *   counts  device int32 [batch] or NULL: sequence b has min(max(counts[b], 0),

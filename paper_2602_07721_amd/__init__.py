@@ -843,8 +843,7 @@ def sink_window_attend(cfg, q, K, V, pos, sink, window, scale, starts=None, coun
     """Attention of t new tokens per sequence, q [batch][Hq][t][D] at positions pos .. pos + t - 1, over the cache rows
     (row = position) of K, V [batch][Hkv][kv_capacity][D] that each sees: j <= p with j < sink or j > p - window.
     starts (int32 [batch], at most pos) gives each sequence's first position, counts (int32 [batch]) how many of its t
-    tokens there are; rows of out behind them are left as they were.  A row that some token attends and that is not
-    finite may reach the others.  Returns out [batch][Hq][t][D] float16."""
+    tokens there are; rows of out behind them are left as they were.  Returns out [batch][Hq][t][D] float16."""
     torch = _torch()
     dev = []
     qp, batch, t = _tokens_arg(cfg, q, dev)

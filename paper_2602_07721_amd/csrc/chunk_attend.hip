@@ -148,7 +148,7 @@ __global__ __launch_bounds__(64 * kCaWaves, R == 16 && KB == 16 ? 3 : 2) void ch
                         r.k + min(Rows::key(h, lane), r.valid - 1) * kD + Rows::template dim<false>(c, lane));
         }
     };
-    bool odd = false;  // a draft's V has values that are not finite
+    bool odd = false;  // whether some V there had values that are not finite
     // Quantised kernels take the drafts, which are float16, in a loop of their own.
     const int main_end = kQuant ? last : end;
     StepRegs<KB, VB> regs[kAhead];
@@ -156,6 +156,9 @@ __global__ __launch_bounds__(64 * kCaWaves, R == 16 && KB == 16 ? 3 : 2) void ch
     auto take = [&](int st, StepRegs<KB, VB>& reg) {
         const StepRows cur = rows_of(st);
         const int ahead = st + kAhead * kCaWaves;
+        uint32_t w = bits_to(cur.valid - 1);
+        if constexpr (WINDOW) w &= window_bits(span.start + tok, cur.base, (int)a.sink, (int)a.window);
+        else if (!kQuant && cur.drafts >= 0) w = draft_bits(a, seq, tok, cur.drafts, cur.valid);
         wave_lds_order();  // the step before has read its V
         if constexpr (kQuant) {
             // Records that are not there: codes of 0, not what the bytes of another part would mean.
@@ -206,7 +209,7 @@ __global__ __launch_bounds__(64 * kCaWaves, R == 16 && KB == 16 ? 3 : 2) void ch
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) put_v(vt, 4 * i + vrow, vchunk, as_h8(reg.v[i]));
-            if (!WINDOW && cur.drafts >= 0) {
+            if (WINDOW ? !__all(w == ~0u) : cur.drafts >= 0) {
                 uint32_t m = 0u;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) note_odd(reg.v[i], m);
@@ -219,9 +222,6 @@ __global__ __launch_bounds__(64 * kCaWaves, R == 16 && KB == 16 ? 3 : 2) void ch
             rows.scores(qf, [&](int h, int c) { return as_h8(reg.k[h * kSteps + c]); });
             if (ahead < main_end) load(rows_of(ahead), reg);
         }
-        uint32_t w = bits_to(cur.valid - 1);
-        if constexpr (WINDOW) w &= window_bits(span.start + tok, cur.base, (int)a.sink, (int)a.window);
-        else if (!kQuant && cur.drafts >= 0) w = draft_bits(a, seq, tok, cur.drafts, cur.valid);
         rows.accumulate(w, vt, lane);
     };
 
@@ -278,13 +278,14 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
     const int d4 = threadIdx.x & 31, sub = threadIdx.x >> 5;
     const float2* state = part_state(a, groups, row);
     const f4v* part = reinterpret_cast<const f4v*>(a.part) + (int64_t)row * a.splits * (kD / 4) + d4;
-    const bool odd = __builtin_signbit(state[a.splits - 1].y);  // the last share's: the drafts are its
+    bool odd = false;
     float top = __builtin_huge_valf(), l = 0.f;
     f4v acc{0.f, 0.f, 0.f, 0.f};
     for (int s = sub; s < a.splits; s += kCcGroups) {
         const float2 st = state[s];
         const f4v v = part[s * (kD / 4)];
         if (st.x == __builtin_huge_valf()) continue;  // saw no key; its outputs may not have been written
+        odd |= __builtin_signbit(st.y);
         const float to = fminf(top, st.x);
         const float c0 = __builtin_amdgcn_exp2f(to - top), c1 = __builtin_amdgcn_exp2f(to - st.x);
         l = l * c0 + __builtin_fabsf(st.y) * c1;
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
     so[sub][d4] = acc;
     if (d4 == 0) {
         snm[sub] = top;
-        sl[sub] = l;
+        sl[sub] = odd ? -l : l;
     }
     __syncthreads();
     if (sub != 0) return;
@@ -303,13 +304,14 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
     for (int i = 0; i < kCcGroups; ++i) top = fminf(top, snm[i]);
     l = 0.f;
     acc = f4v{0.f, 0.f, 0.f, 0.f};
-    f4v other = acc;
-    if (!WINDOW && odd) other = other_part(a, row, d4);
+    odd = false;
+#pragma unroll
+    for (int i = 0; i < kCcGroups; ++i) odd |= __builtin_signbit(sl[i]);
     if (top < __builtin_huge_valf())
 #pragma unroll
         for (int i = 0; i < kCcGroups; ++i) {
             const float c = __builtin_amdgcn_exp2f(top - snm[i]);
-            l += c * sl[i];
+            l += c * __builtin_fabsf(sl[i]);
             acc += c * so[i][d4];
         }
     bool real = true;
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
         const uint32_t M = (uint32_t)(a.g * a.t);
         real = (int)(row % M % (uint32_t)a.t) < a.counts[row / M / (uint32_t)a.hkv];
     }
-    store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, other, real);
+    store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, odd, real);
 }
 
 }  // namespace

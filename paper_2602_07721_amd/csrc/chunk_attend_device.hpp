@@ -138,9 +138,10 @@ __device__ __forceinline__ uint32_t draft_bits(const ChunkArgs& a, int seq, int 
     return first > 63 ? 0u : (uint32_t)(m >> first) & bits_to(valid - 1);
 }
 
-// Draft values that are not finite.  A draft that a token does not see has a weight of 0 there, but
-// 0 times infinity is not 0, and a branch of the tree that overflows must not spoil the others.
-// So the products get such values as 0, and the rows that see them have them added at the end:
+// Values of V that are not finite.  A key that a token does not see has a weight of 0 there, but 0
+// times infinity is not 0, and a draft or a row that overflowed must not spoil tokens that do not
+// see it.  So where not every token sees every key (drafts; the ends of windows) the products get
+// such values as 0, and the rows that see them have them added at the end, if there were any:
 // infinities and NaNs come out of any weight as they are.
 //
 // Sets bits of kOddBits in m if one of v's 8 values is such a value (all ones in its exponent).
@@ -157,17 +158,29 @@ __device__ __forceinline__ u4v finite_part(u4v v) {
     }
     return v;
 }
-// What finite_part left out of the drafts that row `row` sees, dims 4 d4 on.
-__device__ __forceinline__ f4v other_part(const ChunkArgs& a, int64_t row, int d4) {
-    const int64_t M = (int64_t)a.g * a.t, grp = row / M;
-    const int tok = (int)(row % M) % a.t;
-    const uint64_t m = a.mask ? (uint64_t)a.mask[grp / a.hkv * a.t + tok] : ~0ull >> (63 - tok);
-    const h4v* v = static_cast<const h4v*>(a.Vt) + grp * a.t * (kD / 4) + d4;
-    f4v sum{0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < a.t; ++j) {
-        const h4v x = v[j * (kD / 4)];
+// Adds x's values that are not finite to sum.
+__device__ __forceinline__ void add_odd(f4v& sum, h4v x) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += ((m >> j) & 1) && !__builtin_isfinite((float)x[i]) ? (float)x[i] : 0.f;
+    for (int i = 0; i < 4; ++i) sum[i] += __builtin_isfinite((float)x[i]) ? 0.f : (float)x[i];
+}
+// Such values of the keys that row `row` sees, dims 4 d4 on: of all its drafts, or of the cache
+// rows of its window and sinks.
+template <bool WINDOW>
+__device__ __forceinline__ f4v odd_part(const ChunkArgs& a, int64_t row, int d4) {
+    const int64_t M = (int64_t)a.g * a.t, grp = row / M;
+    const int tok = (int)(row % M) % a.t, seq = (int)(grp / a.hkv);
+    f4v sum{0.f, 0.f, 0.f, 0.f};
+    if constexpr (WINDOW) {
+        const h4v* v = static_cast<const h4v*>(a.V) + grp * a.capacity * (kD / 4) + d4;
+        const int p = key_span(a, seq, 0, a.t).start + tok;
+        const int lo = max(0, p - (int)a.window + 1), sinks = min((int)a.sink, lo);
+        for (int j = 0; j < sinks; ++j) add_odd(sum, v[(int64_t)j * (kD / 4)]);
+        for (int j = lo; j <= p; ++j) add_odd(sum, v[(int64_t)j * (kD / 4)]);
+    } else {
+        const uint64_t m = a.mask ? (uint64_t)a.mask[(int64_t)seq * a.t + tok] : ~0ull >> (63 - tok);
+        const h4v* v = static_cast<const h4v*>(a.Vt) + grp * a.t * (kD / 4) + d4;
+        for (int j = 0; j < a.t; ++j)
+            if ((m >> j) & 1) add_odd(sum, v[j * (kD / 4)]);
     }
     return sum;
 }
@@ -393,24 +406,25 @@ struct ChunkRows<32> {
     }
 };
 
-// 4 dims of an output row, acc times inv and `other`: float32, or float16 where the prompt's next
-// product reads it.  Rows of tokens that are not there are left as they were.
+// 4 dims of an output row: float32, or float16 where the prompt's next product reads it.  Rows of
+// tokens that are not there are left as they were.
 template <bool WINDOW>
-__device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int d4, float inv, f4v acc, f4v other,
+__device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int d4, float inv, f4v acc, bool odd,
                                           bool real) {
     acc *= inv;
+    if (odd && real) acc += odd_part<WINDOW>(a, row, d4);
     if constexpr (WINDOW) {
         const h4v h{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
         if (real) static_cast<h4v*>(a.out)[row * (kD / 4) + d4] = h;
     } else {
-        static_cast<f4v*>(a.out)[row * (kD / 4) + d4] = acc + other;
+        static_cast<f4v*>(a.out)[row * (kD / 4) + d4] = acc;
     }
 }
 
 // Joins the states that WAVES waves left `stride` bytes apart for rows [row0, row0 + R) of
 // group grp, and writes the rows, or the share's part of them.  32 lanes a row, 4 dims a lane;
-// `sub` of `subs` such sets of lanes.  A negative sum says that a draft holds values that are not
-// finite, in a wave's state and in a share's part.
+// `sub` of `subs` such sets of lanes.  A negative sum says that odd_part has something
+// to add, in a wave's state and in a share's part.
 template <int R, int WAVES, bool WINDOW>
 __device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace& pl, int64_t groups, int row0, int tokens,
                                            const unsigned char* states, int stride, int sub, int subs) {
@@ -440,9 +454,7 @@ __device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace&
             reinterpret_cast<f4v*>(a.part)[at * (kD / 4) + d4] = acc;
             if (d4 == 0) part_state(a, groups, row)[pl.split] = float2{top, odd ? -l : l};
         } else {
-            f4v other{0.f, 0.f, 0.f, 0.f};
-            if (!WINDOW && odd) other = other_part(a, row, d4);
-            store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, other, (row0 + r) % a.t < tokens);
+            store_row<WINDOW>(a, row, d4, l > 0.f ? 1.f / l : 0.f, acc, odd, (row0 + r) % a.t < tokens);
         }
     }
 }

@@ -36,6 +36,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     // Arrays of their own, chosen at compile time: in one array the compiler cannot tell a read of
     // this tile from the loads under way to the next, and waits for them first (653 us for 615).
     __shared__ u4v sk0[kPaKeys * 16], sk1[kPaKeys * 16], sv0[kPaKeys * 16], sv1[kPaKeys * 16];
+    __shared__ int again;  // whether a wave has outputs that are not finite
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
 
@@ -70,17 +71,8 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     const int p = span.start + tok;
     const int wave_first = span.start + min(i0 + 32 * wave, i1 - 1);
     const int wave_last = span.start + min(i0 + 32 * wave + 31, i1 - 1);
-    const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) + (head * a.t + tok) * kD);
-    h8v qf[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) qf[c] = query_part(qr[2 * c + half], flip);
-
-    float nm = __builtin_huge_valf(), sum = 0.f;
+    float nm, sum;
     f16v o[4];
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
     char* Kg = static_cast<char*>(const_cast<void*>(a.K)) + (int64_t)grp * a.capacity * 256;
     char* Vg = static_cast<char*>(const_cast<void*>(a.V)) + (int64_t)grp * a.capacity * 256;
@@ -106,11 +98,42 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
             __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr)(nv + first * 16), 16, vat, 0, 0, 0);
         }
     };
+    // Tiles [full0, full1) are those of the stretch whose keys every token of the block sees.
+    const int first_p = span.start + i0, last_p = span.start + i1 - 1;
+    const int full0 = sink_tiles + (max(0, last_p - window + 1 - span.lo) + kPaKeys - 1) / kPaKeys;
+    const int full1 = sink_tiles + max(0, first_p + 1 - span.lo) / kPaKeys;
+    auto partly = [&](int tile) {
+        return __builtin_expect(tile >= full1 || (tile < full0 && tile >= span.sink_end / kPaKeys), 0);
+    };
+    // Values of V that are not finite (see finite_part).  Looking for them in every other tile costs
+    // 6% with a window of 512; so the outputs are looked at instead (1 to 2%), and a block that has
+    // such ones takes its tiles once more, carefully: each wave takes those values out of its
+    // quarter of a tile before the others see it.
+    bool careful = false, odd = false;
+    auto clean = [&](int tile, u4v* nv) {
+        if (!careful || !partly(tile)) return;
+        uint32_t m = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) note_odd(nv[(16 * i + 4 * wave) * 16 + lane], m);
+        if (!__any(m & kOddBits)) return;
+        odd = true;
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            u4v* at = nv + (16 * i + 4 * wave) * 16 + lane;
+            *at = finite_part(*at);
+        }
+    };
     // Where this lane's transposing reads begin: key 4 half + (lane % 16) / 4, dims
     // 16 (lane / 16 % 2) + 4 (lane % 4).
     const int tkey = 4 * half + ((lane & 15) >> 2);
     const int tchunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 
+    load(0, sk0, sv0);
+    if (tid == 0) again = 0;  // seen at the first barrier
+    const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) + (head * a.t + tok) * kD);
+    h8v qf[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) qf[c] = query_part(qr[2 * c + half], flip);
     // Tile `tile`, whose keys lie in ck and cv; loads the next into nk and nv.
     auto take = [&](int tile, const u4v* ck, const u4v* cv, u4v* nk, u4v* nv) __attribute__((always_inline)) {
         if (tile + 1 < tiles) load(tile + 1, nk, nv);
@@ -131,18 +154,19 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
                 for (int h = 0; h < 2; ++h)
                     s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                         as_h8(ck[(32 * h + col) * 16 + ((2 * c + half) ^ (col & 15))]), qf[c], s[h], 0, 0, 0);
-            uint32_t w[2];
+            if (partly(tile)) {
+                uint32_t w[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                w[h] = bits_to(valid - 1 - 32 * h) & window_bits(p, base_row + 32 * h, sink, window);
-            if (__builtin_expect(!__all((w[0] & w[1]) == ~0u), 0)) {
+                for (int h = 0; h < 2; ++h)
+                    w[h] = bits_to(valid - 1 - 32 * h) & window_bits(p, base_row + 32 * h, sink, window);
+                if (!__all((w[0] & w[1]) == ~0u))
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t b = w[h] >> (4 * half);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t b = w[h] >> (4 * half);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(b & (1u << (8 * (i / 4) + i % 4)))) s[h][i] = -__builtin_huge_valf();
-                }
+                        for (int i = 0; i < 16; ++i)
+                            if (!(b & (1u << (8 * (i / 4) + i % 4)))) s[h][i] = -__builtin_huge_valf();
+                    }
             }
             float top = -__builtin_huge_valf();
 #pragma unroll
@@ -188,13 +212,53 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
             }
         }
         __builtin_amdgcn_s_setprio(0);
+        if (tile + 1 < tiles) clean(tile + 1, nv);
         __syncthreads();  // and the next tile is there
     };
-    load(0, sk0, sv0);
-    __syncthreads();
-    for (int tile = 0; tile < tiles; tile += 2) {
-        take(tile, sk0, sv0, sk1, sv1);
-        if (tile + 1 < tiles) take(tile + 1, sk1, sv1, sk0, sv0);
+    for (;; careful = true) {
+        nm = __builtin_huge_valf();
+        sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        if (careful) {
+            load(0, sk0, sv0);
+            clean(0, sv0);
+        }
+        __syncthreads();
+        for (int tile = 0; tile < tiles; tile += 2) {
+            take(tile, sk0, sv0, sk1, sv1);
+            if (tile + 1 < tiles) take(tile + 1, sk1, sv1, sk0, sv0);
+        }
+        if (careful) break;
+        float m = 0.f;  // maximum() hands a NaN on
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) m = __builtin_elementwise_maximum(m, __builtin_fabsf(o[d][i]));
+        if (__any(!(m < __builtin_huge_valf()))) again = 1;
+        __syncthreads();
+        if (!again) break;
+    }
+    if (careful && __syncthreads_or(odd)) {
+#pragma unroll 1
+        for (int tile = 0; tile < tiles; ++tile) {
+            if (!partly(tile)) continue;
+#pragma unroll 1
+            for (int key = 0; key < min(tile_keys(tile), kPaKeys); ++key) {
+                const int j = tile_base(tile) + key;
+                if (j > p || (j >= sink && j <= p - window)) continue;
+                const h4v* v = reinterpret_cast<const h4v*>(Vg + (int64_t)j * 256) + half;
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    f4v part{0.f, 0.f, 0.f, 0.f};
+                    add_odd(part, v[2 * c]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[c / 4][4 * (c % 4) + i] += part[i];
+                }
+            }
+        }
     }
 
     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);

@@ -120,7 +120,14 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
             }
         }
     };
-    uint32_t odd = 0u;  // kOddBits: a draft's V has values that are not finite
+    uint32_t odd = 0u;  // kOddBits: some V there had values that are not finite
+    // Whether some token does not see some key of tile t.
+    auto partly = [&](int t) {
+        const int base = tile_base(t), end = base + kTile - 1;
+        if (!WINDOW) return t >= last;
+        return tile_keys(t) < kTile || end > span.start ||
+               (end >= (int)a.sink && base <= span.start + span.tokens - 1 - (int)a.window);
+    };
     // Puts tile t, loaded into regs, into buffer buf as float16.
     auto place = [&](int t, int buf, const TileRegs<kRowLoads, KB, VB>& regs) {
         const bool drafts = !WINDOW && t >= last;
@@ -133,6 +140,7 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
             return;
         }
         const int first_draft = tile_base(t), most = tile_keys(t) - 1;
+        const bool some = partly(t);
 #pragma unroll
         for (int i = 0; i < kRowLoads; ++i) {
             const int key = kStepRows * i + lrow;
@@ -145,7 +153,7 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
                 k = regs.k[i];
                 v = regs.v[i];
             }
-            if (drafts) {
+            if (some) {
                 note_odd(v, odd);
                 v = finite_part(v);
             }
@@ -189,8 +197,7 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
         if (t + 1 < end) turn(t + 1, 1, regs[0]);
     }
 
-    const bool any_odd = !WINDOW && __syncthreads_or((odd & kOddBits) != 0u);
-    if (WINDOW) __syncthreads();
+    const bool any_odd = __syncthreads_or((odd & kOddBits) != 0u);
     rows.leave(lds + wave * kState, lane, any_odd);
     __syncthreads();
     join_waves<R, kParts, WINDOW>(a, pl, groups, row0, span.tokens, lds + set * kParts * kState, kState,

@@ -144,3 +144,40 @@ def test_long_windows_with_shared_keys(b, hkv, g, pos, t, window):
 def test_short_windows_in_one_launch(b, hkv, g, pos, t, window):
     _run(b, hkv, g, pos, t, 5, window, seed=t, starts=[(7 * i) % (pos + 1) for i in range(b)],
          counts=[(5 * i) % (t + 1) for i in range(b)])
+
+
+@pytest.mark.parametrize("b,hkv,g,pos,t,sink,window", [
+    (1, 1, 4, 3000, 4, 40, 2000), (1, 2, 4, 3000, 8, 40, 2000), (2, 1, 4, 3000, 16, 40, 2000),
+    (1, 1, 4, 3000, 40, 0, 2000), (64, 8, 4, 120, 4, 5, 60), (64, 8, 4, 120, 8, 0, 60),  # few tokens
+    (1, 2, 2, 500, 300, 40, 100), (2, 1, 2, 0, 500, 3, 64), (1, 1, 2, 0, 200, 0, 1000)])  # prompt form
+def test_rows_that_are_not_finite_reach_only_tokens_that_see_them(b, hkv, g, pos, t, sink, window):
+    print(f"[sink] not finite: batch {b} hkv {hkv} g {g} pos {pos} t {t} sink {sink} window {window}", flush=True)
+    r = np.random.default_rng(pos + t)
+    n = pos + t
+    K, V, q = draw(r, b, hkv, n, D), draw(r, b, hkv, n, D), draw(r, b, hkv * g, t, D)
+    # Rows that some tokens see and some do not: the last token's own, one in the middle, the
+    # first token's oldest, and a row behind the sinks.
+    values = {n - 1: np.inf, pos + t // 2: np.nan, max(sink, pos - window + 1): -np.inf, sink: np.inf}
+    bad = V.copy()
+    for i, (j, x) in enumerate(values.items()):
+        bad[:, :, j, 5 + 30 * i] = bad[:, :, j, 127] = x
+    odd = ~np.isfinite(bad)
+    V[odd] = 0
+    lost, badk = pos + t // 3, K.copy()  # a row whose scores are NaN
+    badk[:, :, lost, 77], K[:, :, lost] = np.nan, 0
+    got = pk.sink_window_attend(_cfg(hkv, g), gpu(q), gpu(badk), gpu(bad), pos, sink, window, SCALE).cpu().numpy()
+    p, j = np.arange(pos, n)[:, None], np.arange(n)[None]
+    visible = (j <= p) & ((j < sink) | (j > p - window))
+    assert not visible[:, list(values)].all(0).all(), "some of the rows are hidden from some token"
+    dead = visible[:, lost]
+    for s in range(0, b, 21):
+        for h in range(hkv * g):
+            x, v = got[s, h].astype(np.float32), bad[s, h // g].astype(np.float32)
+            assert np.isnan(x[dead]).all()
+            odds = np.stack([np.where(np.isfinite(v[m]), 0, v[m]).sum(0) for m in visible])
+            hit = (odds != 0) & ~dead[:, None]
+            assert np.array_equal(x[hit], odds[hit], equal_nan=True)
+            k_, v_ = K[s, h // g], V[s, h // g]
+            fine = ~hit & ~dead[:, None]
+            want = attend64(q[s, h], k_, v_, visible)
+            check(got[s, h][fine], want[fine], tolerance(q[s, h], k_, v_, half_out=True), f"seq {s} head {h}")
