@@ -349,10 +349,10 @@ void chunk_plan(ChunkArgs& a) {
     a.splits = (int32_t)(splits < 1 ? 1 : splits);
 }
 
-// Both forms' times in ns, fitted to 120 calls of 1 to 256 tokens, 1 to 128 (sequence, KV head)s
-// and windows of 512 to 16384 rows: 1 x 8 x 4 heads, 4096 rows, 16 tokens: 19 us here, 85 in the
-// prompt form; 128 tokens 39 and 89; 16 x 8 x 4, 4096 rows, 64 tokens 148 and 157, 128 tokens 232
-// and 172; 512 rows, 32 tokens 37 and 26.
+// Both forms' times in ns, fitted to 165 calls of 1 to 512 tokens, 1 to 128 (sequence, KV head)s
+// and windows of 512 to 16384 rows: 1 x 8 x 4 heads, 4096 rows, 16 tokens: 20 us here, 78 in the
+// prompt form; 128 tokens 39 and 83; 16 x 8 x 4, 4096 rows, 32 tokens 88 and 125, 64 tokens 144 and
+// 130, 128 tokens 235 and 147; 512 rows, 32 tokens 37 and 25.
 bool few_tokens(const ChunkArgs& a) {
     if (a.t > 1024) return false;
     const double groups = (double)a.batch * a.hkv, rows = (double)a.g * a.t, all = (double)(a.n + a.t);
