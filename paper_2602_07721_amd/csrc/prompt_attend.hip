@@ -13,7 +13,7 @@
 // and an exponential, a maximum, a sum and a rounding), with LDS close behind: a wave reads 32
 // KB a tile, which takes the block as long as its matrix instructions.  64 tokens a wave would
 // halve that but leave one wave a SIMD: 870 us where 32 took 660.  32 heads, 8192 tokens after
-// 8192 others, window 4096: 615 us, 920 TFLOP/s (a plain float16 matrix product: 1147).
+// 8192 others, window 4096: 544 us, 1042 TFLOP/s (a plain float16 matrix product: 1147).
 
 #include <hip/hip_fp16.h>
 
@@ -34,7 +34,7 @@ constexpr float kPaSlack = 7.f; // running maximum is raised: below 2^16, and sm
 
 __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs a, int qtiles) {
     // Arrays of their own, chosen at compile time: in one array the compiler cannot tell a read of
-    // this tile from the loads under way to the next, and waits for them first (653 us for 615).
+    // this tile from the loads under way to the next, and waits for them first (653 us for 615 under a trace).
     __shared__ u4v sk0[kPaKeys * 16], sk1[kPaKeys * 16], sv0[kPaKeys * 16], sv1[kPaKeys * 16];
     __shared__ int again;  // whether a wave has outputs that are not finite
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -8,9 +8,10 @@
 // 128K float16 rows: 1317 us so, 920 with the sets in blocks of their own, 757 here, 93% of the
 // rate of a plain read).  Records are taken apart once for all rows.  Two tiles are in flight in
 // registers while one is computed on, and two blocks share a CU: one computes while the other
-// waits at its barrier.  128 rows are bound by the matrix and vector units and by the power they
-// draw: 31 drafts x 4 heads over the same rows take 1108 us (750 TFLOP/s of matrix
-// instructions), and 804 us where all values are 0.
+// waits at its barrier.
+// 128 rows are bound by the matrix and vector units and by the power they draw: 31 drafts x 4 heads
+// over the same rows take 1070 to 1200 us from card to card (700 to 780 TFLOP/s of matrix
+// instructions), and 805 us where all values are 0.
 
 #include <hip/hip_fp16.h>
 
@@ -176,7 +177,9 @@ __global__ __launch_bounds__(kTaThreads, 2) void tile_attend_kernel(ChunkArgs a,
             uint32_t w = bits_to(valid - 1);
             if constexpr (WINDOW) w &= window_bits(span.start + tok, base, (int)a.sink, (int)a.window);
             else if (t >= last) w = draft_bits(a, seq, tok, base, valid);
+            __builtin_amdgcn_s_setprio(1);  // ahead of another wave's S^T: 2 to 5%
             rows.accumulate(w, vt + from, lane);
+            __builtin_amdgcn_s_setprio(0);
         }
     };
 
