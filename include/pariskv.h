@@ -513,7 +513,8 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
  * token i attends the sequence's cached rows and the drafted tokens that its
  * mask names, its ancestors in the tree of drafts and itself,
  *   o_i = sum_j softmax_j(scale <k_j, q_i>) v_j
- * in float32 (scores have to be finite there).
+ * in float32 (scores have to be finite there; one that is NaN, by the query or
+ * by a key that the token sees, makes the token's output NaN).
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D], the cached rows
  *   n       cached rows of every sequence, 0..kv_capacity; with lens (device
@@ -549,7 +550,8 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
 /* Attention of t new tokens per sequence -- a prompt, a chunk of one, or a
  * single token -- over a sliding window and the first tokens, which stay
  * visible: the token at position p attends the cache rows j <= p with j < sink
- * or j > p - window (window >= pos + t: plain causal attention).
+ * or j > p - window (window >= pos + t: plain causal attention).  A score that
+ * is NaN, by the query or by a key that the token sees, makes its output NaN.
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D]: row j holds position j,
  *           the new tokens' rows among them.  A row's values, whatever they are

@@ -224,6 +224,13 @@ __device__ __forceinline__ void split_p(float s0, float s1, float c2, float base
     lo[at + 1] = pl[1];
 }
 
+// The maximum that a row's state is left with.  Maxima pass NaNs over, sums and outputs do not: a row
+// whose scores are all NaN has an infinite nm, as one that saw no key, but a sum that is NaN.  Any
+// finite nm keeps such a state in the joins, which then hand the NaNs on.
+__device__ __forceinline__ float left_maximum(float nm, float sum) {
+    return sum != sum && nm == __builtin_huge_valf() ? 0.f : nm;
+}
+
 // 16 rows.  Lane l = col + 16 lg: row col, keys 16 h + 4 lg + i, outputs of dims 16 d + 4 lg + i.
 template <>
 struct ChunkRows<16> {
@@ -305,10 +312,10 @@ struct ChunkRows<16> {
     // Leaves the state in ca_state_bytes(16) of LDS; the sums' signs say `odd`.
     __device__ __forceinline__ void leave(unsigned char* to, int lane, bool odd) const {
         float* so = reinterpret_cast<float*>(to);
-        const float l = rows_sum(sum);
+        const float l = __builtin_fabsf(rows_sum(sum));
         const int r = lane & 15;
         if (lg == 0) {
-            so[16 * kCaRow + r] = nm;
+            so[16 * kCaRow + r] = left_maximum(nm, l);
             so[16 * (kCaRow + 1) + r] = odd ? -l : l;
         }
 #pragma unroll
@@ -393,8 +400,8 @@ struct ChunkRows<32> {
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
         const int r = lane & 31;
         if (half == 0) {
-            so[32 * kCaRow + r] = nm;
-            const float l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+            const float l = __builtin_fabsf(__uint_as_float(x[0]) + __uint_as_float(x[1]));
+            so[32 * kCaRow + r] = left_maximum(nm, l);
             so[32 * (kCaRow + 1) + r] = odd ? -l : l;
         }
 #pragma unroll
