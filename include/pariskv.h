@@ -487,14 +487,15 @@ int pariskv_dequantize_rows(const pariskv_config* cfg, const pariskv_quant_cache
 
 /* pariskv_sparse_attend over the rows of a quantised cache: the attention over
  * the float16 values the records stand for, in float32.  Entries of idx outside
- * [0, capacity) are skipped; out is zero when no entry is left.
+ * [0, capacity) are skipped; out is zero when no entry is left, NaN when the
+ * score of one that is left is NaN.
  * Errors: INVALID, UNSUPPORTED (k > 4096), HIP. */
 int pariskv_quant_attend(const pariskv_config* cfg, const void* q, const pariskv_quant_cache* cache,
                          const int32_t* idx, int32_t k, int32_t batch, float scale, float* out, void* stream);
 
 /* pariskv_tiered_attend with the retrieval rows in a quantised cache (entry j
  * attends its row win->retr_begin + idx[j]) and Sink + Local + Update Buffer
- * rows in the float16 window cache K_win, V_win.
+ * rows in the float16 window cache K_win, V_win; NaN scores as above.
  * Errors: those of pariskv_tiered_attend. */
 int pariskv_quant_tiered_attend(const pariskv_config* cfg, const void* q, const void* K_win, const void* V_win,
                                 int64_t win_capacity, const pariskv_quant_cache* cache, const int32_t* idx,

@@ -40,15 +40,17 @@ struct QaState {
         float mn = m;
 #pragma unroll
         for (int u = 0; u < N; ++u) mn = there[u] ? fmaxf(mn, s[u]) : mn;
-        if (mn == -__builtin_huge_valf()) return;
-        const float c = __expf(m - mn);  // m = -inf before the first row: c = 0
+        // m = -inf before the first row: c = 0.  Rows whose scores are NaN leave the maximum as it is,
+        // and make the sum NaN.
+        const float from = mn > -__builtin_huge_valf() ? mn : 0.f;
+        const float c = __expf(m - from);
         l *= c;
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[d] *= c;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             if (!there[u]) continue;  // its values may be anything
-            const float p = __expf(s[u] - mn);
+            const float p = __expf(s[u] - from);
             l += p;
 #pragma unroll
             for (int d = 0; d < 8; ++d) acc[d] += p * v[u][d];
@@ -173,15 +175,14 @@ __global__ __launch_bounds__(kQaThreads) void quant_attend_kernel(
         float M = -__builtin_huge_valf(), L = 0.f, O = 0.f;
 #pragma unroll
         for (int w = 0; w < kQaWaves; ++w) M = fmaxf(M, sm.m[w]);
-        if (M > -__builtin_huge_valf()) {
+        const float from = M > -__builtin_huge_valf() ? M : 0.f;
 #pragma unroll
-            for (int w = 0; w < kQaWaves; ++w) {
-                const float c = __expf(sm.m[w] - M);
-                L += sm.l[w] * c;
-                O += sm.acc[w][tid] * c;
-            }
+        for (int w = 0; w < kQaWaves; ++w) {
+            const float c = __expf(sm.m[w] - from);
+            L += sm.l[w] * c;
+            O += sm.acc[w][tid] * c;
         }
-        out[row * kD + tid] = L > 0.f ? O / L : 0.f;
+        out[row * kD + tid] = L == 0.f ? 0.f : O / L;  // NaN where some score was
     }
 }
 

@@ -117,3 +117,41 @@ def test_a_nan_key_in_the_first_row_of_a_prompt(t):
 def test_a_token_whose_own_key_is_nan_and_alone_in_its_share(g):
     # Rows 0 .. 127 in one share of the keys, the token's own in the next.
     _window(2, 1, g, 3000, 1, 0, 4000, nan_keys=(128, 256), starts=(128, 256))
+
+
+@pytest.mark.parametrize("kb,vb", [(8, 8), (4, 4)])
+@pytest.mark.parametrize("k", [1, 16, 64, 65, 300])
+@pytest.mark.parametrize("what", ["query", "window row", "only row"])
+def test_listed_rows(what, k, kb, vb):
+    print(f"[nan listed] {what} k {k} bits {kb} {vb}", flush=True)
+    b, hkv, g, n = 2, 2, 4, 400
+    r = np.random.default_rng(k)
+    cfg, win = _cfg(hkv, g), pk.Window(3, 3, n, n + 9)
+    K, V, q = draw(r, b, hkv, n, D), draw(r, b, hkv, n, D), draw(r, b, hkv * g, D)
+    Kw, Vw = draw(r, b, hkv, 16, D), draw(r, b, hkv, 16, D)
+    idx = np.stack([np.sort(r.permutation(n - 3)[:k]) for _ in range(b * hkv * g)]).reshape(b, hkv * g, k).astype(np.int32)
+    if what == "query":
+        q[:, 1::2] = np.nan
+    else:
+        Kw[:, 1, 5, 40] = np.nan  # slot 5 of one KV head: a Local row
+    if what == "only row":
+        idx[:] = -1
+        win = pk.Window(0, 0, n - 11, n - 10)
+        Kw[:, 1, (n - 11) % 16, 40] = np.nan
+    cache = pk.QuantCache.empty(cfg, b, n, kb, vb)
+    pk.quantize_rows(cfg, cache, gpu(K), gpu(V), 0, 0, n)
+    K, V = quant.round_trip(K, kb), quant.round_trip(V, vb)
+    plain = pk.quant_attend(cfg, gpu(q), cache, gpu(idx), SCALE).cpu().numpy()
+    tiered = pk.quant_tiered_attend(cfg, gpu(q), gpu(Kw), gpu(Vw), cache, gpu(idx), win, SCALE).cpu().numpy()
+    slots = [pk.window_slot(x, win.sink_len, 16) for x in
+             list(range(win.sink_len)) + list(range(win.dense_begin, win.dense_end))]
+    for s in range(b):
+        for h in range(hkv * g):
+            rows = idx[s, h][idx[s, h] >= 0]
+            for got, first, dense in ((plain, 0, []), (tiered, win.retr_begin, slots)):
+                k_ = np.concatenate([K[s, h // g, first + rows], Kw[s, h // g, dense].astype(np.float64)])
+                v_ = np.concatenate([V[s, h // g, first + rows], Vw[s, h // g, dense].astype(np.float64)])
+                if len(k_) == 0:
+                    assert not got[s, h].any()
+                    continue
+                _compare(got[s, h][None], q[s, h][None], k_, v_, np.ones((1, len(k_)), bool), False, f"seq {s} head {h}")
