@@ -553,6 +553,10 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
  * visible: the token at position p attends the cache rows j <= p with j < sink
  * or j > p - window (window >= pos + t: plain causal attention).  A score that
  * is NaN, by the query or by a key that the token sees, makes its output NaN.
+ * Scores and sums are float32, also where many tokens' weights are rounded to
+ * float16 (and summed as rounded): an output is then within 2^-11 of the largest
+ * |v| that its token sees before it is rounded itself, within 2^-20 otherwise,
+ * plus twice the float32 rounding of the scores.
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D]: row j holds position j,
  *           the new tokens' rows among them.  A row's values, whatever they are
