@@ -506,8 +506,10 @@ int pariskv_quant_tiered_attend(const pariskv_config* cfg, const void* q, const 
 
 #define PARISKV_MAX_TREE 64 /* largest number of drafted tokens of a sequence */
 
-/* Bytes of the workspace that pariskv_tree_attend and pariskv_quant_tree_attend
- * need for these sizes (at least 256; 0 on invalid input). */
+/* Bytes of a workspace for pariskv_tree_attend and pariskv_quant_tree_attend with
+ * these sizes and every smaller batch, n and t (at least 256, below 70 MB; 0 on
+ * invalid input): one sized for the longest call serves them all.  A call of
+ * given sizes may need less, and is refused only below what it needs. */
 size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t n, int32_t t);
 
 /* Verification of drafted tokens (t of every sequence, 1 = a dense decode step):
@@ -543,8 +545,10 @@ int pariskv_quant_tree_attend(const pariskv_config* cfg, const void* q, const pa
                               const int32_t* lens, int32_t t, int32_t batch, float scale, float* out,
                               void* workspace, size_t ws_bytes, void* stream);
 
-/* Bytes of the workspace that pariskv_sink_window_attend needs for these sizes
- * (at least 256; 0 on invalid input). */
+/* Bytes of a workspace for pariskv_sink_window_attend with these sizes and every
+ * smaller batch, pos, t, sink and window (at least 256, below 70 MB; 0 on invalid
+ * input).  A call of given sizes may need less, and is refused only below what it
+ * needs. */
 size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, int64_t pos, int64_t t,
                                      int64_t sink, int64_t window);
 

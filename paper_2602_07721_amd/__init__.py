@@ -786,7 +786,8 @@ def _workspace_arg(workspace, size, q, dev, stream):
 
 
 def tree_workspace_size(cfg, batch, n, t):
-    """Bytes of the workspace of tree_attend and quant_tree_attend (0 on invalid sizes)."""
+    """Bytes of a workspace for tree_attend and quant_tree_attend with these sizes and all smaller ones (0 on invalid
+    sizes)."""
     return int(lib().pariskv_tree_workspace(cfg.c(), int(batch), int(n), int(t)))
 
 
@@ -834,7 +835,7 @@ def quant_tree_attend(cfg, q, cache, K_tree, V_tree, n, scale, mask=None, lens=N
 
 
 def sink_window_workspace_size(cfg, batch, pos, t, sink, window):
-    """Bytes of the workspace of sink_window_attend (0 on invalid sizes)."""
+    """Bytes of a workspace for sink_window_attend with these sizes and all smaller ones (0 on invalid sizes)."""
     return int(lib().pariskv_sink_window_workspace(cfg.c(), int(batch), int(pos), int(t), int(sink), int(window)))
 
 

@@ -976,11 +976,12 @@ static int check_tree_sizes(const pariskv_config* cfg, int32_t batch, int64_t n,
     return PARISKV_OK;
 }
 
+static size_t workspace_bytes(size_t bytes) { return bytes < 256 ? 256 : (bytes + 255) / 256 * 256; }
+
 // Plans a few-token call; bytes of its workspace.
 static size_t chunk_workspace(ChunkArgs& a) {
     chunk_plan(a);
-    const size_t bytes = chunk_part_bytes(a);
-    return bytes < 256 ? 256 : (bytes + 255) / 256 * 256;
+    return workspace_bytes(chunk_part_bytes(a));
 }
 
 static int check_workspace(const void* workspace, size_t ws_bytes, size_t need) {
@@ -999,7 +1000,7 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
     a.g = cfg->q_per_kv;
     a.t = t;
     a.n = n;
-    return chunk_workspace(a);
+    return workspace_bytes(chunk_part_bound(a));
 }
 
 static int tree_impl(const pariskv_config* cfg, const void* q, const void* K, const void* V,
@@ -1108,7 +1109,7 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
     if (check_sink_window_sizes(cfg, batch, pos, t, sink, window) != PARISKV_OK) return 0;
     ChunkArgs a{};
     sink_window_shape(cfg, batch, pos, t, sink, window, &a);
-    return t > 0 && few_tokens(a) ? chunk_workspace(a) : 256;
+    return workspace_bytes(chunk_part_bound(a));
 }
 
 int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const void* K, const void* V,

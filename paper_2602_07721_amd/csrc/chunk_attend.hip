@@ -29,6 +29,8 @@ namespace pariskv {
 namespace {
 
 constexpr int kCaWaves = 4;  // waves of a block
+constexpr int kCaMaxShares = 256;  // of a sequence's keys
+constexpr int kFewTokens = 1024;   // the few-token form of the sliding window takes no more
 
 // LDS of one wave: its V and its records, later its state.
 constexpr int kCaVBytes = kCaKeys * kD * 2;
@@ -328,19 +330,25 @@ __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs
 // register of a SIMD), more by tile_attend.hip, whose waves share the keys' tiles.
 static int chunk_block_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
+static int64_t chunk_steps(const ChunkArgs& a) {
+    if (a.window == 0) return (a.n + kCaKeys - 1) / kCaKeys;
+    const int64_t near = a.window + a.t - 1, all = a.n + a.t, sinks = a.sink < a.n ? a.sink : a.n;
+    return (sinks + kCaKeys - 1) / kCaKeys + ((near < all ? near : all) + kCaKeys - 1) / kCaKeys;
+}
+
+// Shares of the keys that `blocks` blocks of `block` rows are cut into at most: about two rounds of
+// the blocks that the chip holds at a time (2 a CU).
+static int64_t chunk_rounds(int64_t block) { return block <= 32 ? 1024 : 512; }
+static int64_t chunk_shares(int64_t block, int64_t blocks) {
+    const int64_t splits = (chunk_rounds(block) + blocks - 1) / blocks;
+    return splits > kCaMaxShares ? kCaMaxShares : splits;
+}
+
 void chunk_plan(ChunkArgs& a) {
     const int64_t groups = (int64_t)a.batch * a.hkv, rows = (int64_t)a.g * a.t;
-    const int64_t block = chunk_block_rows(rows), blocks = groups * ((rows + block - 1) / block);
-    int64_t steps = (a.n + kCaKeys - 1) / kCaKeys;
-    if (a.window > 0) {
-        const int64_t near = a.window + a.t - 1, all = a.n + a.t, sinks = a.sink < a.n ? a.sink : a.n;
-        steps = (sinks + kCaKeys - 1) / kCaKeys + ((near < all ? near : all) + kCaKeys - 1) / kCaKeys;
-    }
-    // About two rounds of the blocks that the chip holds at a time (2 a CU); a share is a multiple
-    // of 4 steps, one for every wave.
-    const int64_t want = block <= 32 ? 1024 : 512;
-    int64_t splits = (want + blocks - 1) / blocks;
-    if (splits > 256) splits = 256;
+    const int64_t block = chunk_block_rows(rows), steps = chunk_steps(a);
+    int64_t splits = chunk_shares(block, groups * ((rows + block - 1) / block));
+    // A share is a multiple of 4 steps, one for every wave.
     int64_t per = (steps + splits - 1) / splits;
     per = (per + kCaWaves - 1) / kCaWaves * kCaWaves;
     if (per < kCaWaves) per = kCaWaves;
@@ -354,7 +362,7 @@ void chunk_plan(ChunkArgs& a) {
 // prompt form; 128 tokens 39 and 83; 16 x 8 x 4, 4096 rows, 32 tokens 88 and 125, 64 tokens 144 and
 // 130, 128 tokens 235 and 147; 512 rows, 32 tokens 37 and 25.
 bool few_tokens(const ChunkArgs& a) {
-    if (a.t > 1024) return false;
+    if (a.t > kFewTokens) return false;
     const double groups = (double)a.batch * a.hkv, rows = (double)a.g * a.t, all = (double)(a.n + a.t);
     auto tiles = [&](double tokens) {
         const double keys = (double)a.sink + (double)a.window + tokens;
@@ -368,8 +376,33 @@ bool few_tokens(const ChunkArgs& a) {
     return few < prompt;
 }
 
-size_t chunk_part_bytes(const ChunkArgs& a) {
-    return a.splits > 1 ? (size_t)a.batch * a.hkv * a.g * a.t * (size_t)a.splits * (kD + 2) * 4 : 0;
+static size_t part_bytes(int64_t rows, int64_t splits) { return splits > 1 ? (size_t)rows * splits * (kD + 2) * 4 : 0; }
+
+size_t chunk_part_bytes(const ChunkArgs& a) { return part_bytes((int64_t)a.batch * a.hkv * a.g * a.t, a.splits); }
+
+// Fewer keys, tokens or sequences can take more shares (rounding a share to whole steps leaves fewer
+// of more keys), so this is the largest of them all.  For every number of blocks that the rows of a
+// (sequence, KV head) make, the most tokens that make it; there, for every number of shares, the
+// most sequences that are cut into it.
+size_t chunk_part_bound(ChunkArgs a) {
+    const int64_t most = a.window > 0 && a.t > kFewTokens ? kFewTokens : a.t, batch = a.batch;
+    size_t bytes = 0;
+    for (int64_t t = 1; t <= most; t = a.t + 1) {
+        const int64_t block = chunk_block_rows(a.g * t), tiles = (a.g * t + block - 1) / block;
+        const int64_t full = tiles * block / a.g;
+        a.t = (int32_t)(full < most ? full : most);
+        const int64_t shares = (chunk_steps(a) + kCaWaves - 1) / kCaWaves, blocks = a.hkv * tiles;
+        for (int64_t b = 1; b <= batch; ++b) {
+            int64_t splits = chunk_shares(block, b * blocks);
+            if (shares < splits) splits = shares;
+            if (splits <= 1) break;
+            const int64_t same = (chunk_rounds(block) - 1) / (blocks * (splits - 1));
+            b = same < batch ? same : batch;
+            const size_t need = part_bytes(b * a.hkv * a.g * a.t, splits);
+            if (need > bytes) bytes = need;
+        }
+    }
+    return bytes;
 }
 
 hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s) {

@@ -41,6 +41,8 @@ struct ChunkArgs {
 // Sets splits and per from the call's sizes alone (not from lens and counts).
 void chunk_plan(ChunkArgs& a);
 size_t chunk_part_bytes(const ChunkArgs& a);
+// Bytes that this call and every smaller one need (batch, n, t, sink or window smaller).
+size_t chunk_part_bound(ChunkArgs a);
 hipError_t launch_chunk_attend(const ChunkArgs& a, hipStream_t s);
 // Its first kernel for blocks of 64 or 128 rows (tile_attend.hip).
 hipError_t launch_tile_attend(const ChunkArgs& a, int block, int row_tiles, int64_t groups, const char* name,
