@@ -275,44 +275,45 @@ constexpr int kCcGroups = 8;
 template <bool WINDOW>
 __global__ __launch_bounds__(32 * kCcGroups) void chunk_combine_kernel(ChunkArgs a, int64_t groups) {
     __shared__ f4v so[kCcGroups][32];
-    __shared__ float snm[kCcGroups], sl[kCcGroups];
+    __shared__ float sr[kCcGroups], sl[kCcGroups];
     const uint32_t row = blockIdx.x;
     const int d4 = threadIdx.x & 31, sub = threadIdx.x >> 5;
     const float2* state = part_state(a, groups, row);
     const f4v* part = reinterpret_cast<const f4v*>(a.part) + (int64_t)row * a.splits * (kD / 4) + d4;
+    const float c2 = score_factor(a.scale);
     bool odd = false;
-    float top = __builtin_huge_valf(), l = 0.f;
+    float top = -__builtin_huge_valf(), l = 0.f;
     f4v acc{0.f, 0.f, 0.f, 0.f};
     for (int s = sub; s < a.splits; s += kCcGroups) {
         const float2 st = state[s];
         const f4v v = part[s * (kD / 4)];
-        if (st.x == __builtin_huge_valf()) continue;  // saw no key; its outputs may not have been written
+        if (st.x == -__builtin_huge_valf()) continue;  // saw no key; its outputs may not have been written
         odd |= __builtin_signbit(st.y);
-        const float to = fminf(top, st.x);
-        const float c0 = __builtin_amdgcn_exp2f(to - top), c1 = __builtin_amdgcn_exp2f(to - st.x);
+        const float to = fmaxf(top, st.x);
+        const float c0 = rescale(top, to, c2), c1 = rescale(st.x, to, c2);
         l = l * c0 + __builtin_fabsf(st.y) * c1;
         acc = acc * c0 + v * c1;
         top = to;
     }
     so[sub][d4] = acc;
     if (d4 == 0) {
-        snm[sub] = top;
+        sr[sub] = top;
         sl[sub] = odd ? -l : l;
     }
     __syncthreads();
     if (sub != 0) return;
-    top = __builtin_huge_valf();
+    top = -__builtin_huge_valf();
 #pragma unroll
-    for (int i = 0; i < kCcGroups; ++i) top = fminf(top, snm[i]);
+    for (int i = 0; i < kCcGroups; ++i) top = fmaxf(top, sr[i]);
     l = 0.f;
     acc = f4v{0.f, 0.f, 0.f, 0.f};
     odd = false;
 #pragma unroll
     for (int i = 0; i < kCcGroups; ++i) odd |= __builtin_signbit(sl[i]);
-    if (top < __builtin_huge_valf())
+    if (top > -__builtin_huge_valf())
 #pragma unroll
         for (int i = 0; i < kCcGroups; ++i) {
-            const float c = __builtin_amdgcn_exp2f(top - snm[i]);
+            const float c = rescale(sr[i], top, c2);
             l += c * __builtin_fabsf(sl[i]);
             acc += c * so[i][d4];
         }

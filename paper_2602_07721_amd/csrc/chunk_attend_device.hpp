@@ -45,6 +45,34 @@ __device__ __forceinline__ float score_factor(float scale) {
     return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f);
 }
 
+// A row's weights are P = 2^(c2 (s - r) + kUp): s its scores, c2 their factor, and r one of them, near
+// the largest so far (-infinity before the first).  r is raised only when a weight would pass 2^kSlack
+// times that of r, so P stays below 2^16.  P is taken as 2^(c2 s + nm) with nm = kUp - c2 r, one
+// instruction a score.  Where nm is so large that its rounding would show, r is subtracted from the
+// scores first: nm is a NaN there, which sends every step through the path that raises r.  So the
+// differences of finite scores decide, however large both are.
+constexpr float kUp = 8.f;
+constexpr float kSlack = 7.f;
+constexpr float kLargeNm = 8388608.f;  // 2^23: float32 has steps of 1/2 to 1 there
+__device__ __forceinline__ float nm_of(float r, float c2) { return __builtin_fmaf(-r, c2, kUp); }
+// What sums and outputs of a state at r are multiplied by when they move to `to` >= r.
+__device__ __forceinline__ float rescale(float r, float to, float c2) { return __builtin_amdgcn_exp2f((r - to) * c2); }
+// Sums and outputs taken with nm are 2^(c2 r + nm - kUp) of those at r: what they are multiplied by
+// for that (1 where nm is not what they were taken with, or nothing was).
+__device__ __forceinline__ float at_r(float r, float nm, float c2) {
+    const float x = __builtin_fmaf(-r, c2, kUp - nm);
+    return __builtin_fabsf(nm) < kLargeNm ? __builtin_amdgcn_exp2f(x) : 1.f;
+}
+// Raises a row's r to m, the largest score it has met, and gives what its state is multiplied by.
+__device__ __forceinline__ float raise(float m, float c2, float& r, float& nm) {
+    const float to = nm_of(m, c2);
+    const bool small = __builtin_fabsf(nm) < kLargeNm && __builtin_fabsf(to) < kLargeNm;
+    const float c = small ? __builtin_amdgcn_exp2f(to - nm) : rescale(r, m, c2);
+    r = m;
+    nm = __builtin_fabsf(to) < kLargeNm ? to : __builtin_nanf("");
+    return c;
+}
+
 // Bits 0..x of a word (none for x < 0).
 __device__ __forceinline__ uint32_t bits_to(int x) { return x < 0 ? 0u : x >= 31 ? ~0u : (2u << x) - 1u; }
 
@@ -86,10 +114,8 @@ __device__ __forceinline__ KeySpan key_span(const ChunkArgs& a, int seq, int i0,
 // ---- few new tokens: a wave's 16 or 32 rows over steps of 32 keys
 
 constexpr int kCaKeys = 32;      // keys of a step
-constexpr float kCaUp = 8.f;     // P is held scaled by 2^8 ...
-constexpr float kCaSlack = 7.f;  // ... and grows by up to 2^7 before the maximum is raised
 constexpr int kCaRow = kD + 4;   // floats of an output row in LDS (spreads the rows over the banks)
-// LDS of a wave's outputs [row][kCaRow], maxima and sums.
+// LDS of a wave's outputs [row][kCaRow], references r and sums.
 constexpr int ca_state_bytes(int rows) { return rows * (kCaRow + 2) * 4; }
 
 // What a block works on: tile `tile` of the rows of (sequence, KV head) grp, share `split` of its keys.
@@ -121,7 +147,7 @@ __device__ __forceinline__ ChunkPlace chunk_place(const ChunkArgs& a, uint32_t r
     return p;
 }
 
-// The maximum and sum of a row's part in the workspace (behind all rows' outputs).
+// The reference r and the sum of a row's part in the workspace (behind all rows' outputs).
 __device__ __forceinline__ float2* part_state(const ChunkArgs& a, int64_t groups, int64_t row) {
     return reinterpret_cast<float2*>(a.part + groups * a.g * a.t * a.splits * kD) + row * a.splits;
 }
@@ -129,7 +155,7 @@ __device__ __forceinline__ float2* part_state(const ChunkArgs& a, int64_t groups
 __device__ __forceinline__ void leave_idle(const ChunkArgs& a, const ChunkPlace& pl, int64_t groups, int row0, int rows) {
     const int M = a.g * a.t;
     for (int r = row0 + (int)threadIdx.x; r < min(row0 + rows, M); r += (int)blockDim.x)
-        part_state(a, groups, pl.grp * M + r)[pl.split] = float2{__builtin_huge_valf(), 0.f};
+        part_state(a, groups, pl.grp * M + r)[pl.split] = float2{-__builtin_huge_valf(), 0.f};
 }
 
 // Which of the drafts first, first + 1, ... (valid of them) token tok sees.
@@ -224,20 +250,19 @@ __device__ __forceinline__ void split_p(float s0, float s1, float c2, float base
     lo[at + 1] = pl[1];
 }
 
-// The maximum that a row's state is left with.  Maxima pass NaNs over, sums and outputs do not: a row
-// whose scores are all NaN has an infinite nm, as one that saw no key, but a sum that is NaN.  Any
-// finite nm keeps such a state in the joins, which then hand the NaNs on.
-__device__ __forceinline__ float left_maximum(float nm, float sum) {
-    return sum != sum && nm == __builtin_huge_valf() ? 0.f : nm;
+// The r that a row's state is left with.  Maxima pass NaNs over, sums and outputs do not: a row whose
+// scores are all NaN has the r of one that saw no key, but a sum that is NaN.  Any finite r keeps
+// such a state in the joins, which then hand the NaNs on.
+__device__ __forceinline__ float left_r(float r, float sum) {
+    return sum != sum && r == -__builtin_huge_valf() ? 0.f : r;
 }
 
 // 16 rows.  Lane l = col + 16 lg: row col, keys 16 h + 4 lg + i, outputs of dims 16 d + 4 lg + i.
 template <>
 struct ChunkRows<16> {
     static constexpr int kHalves = 2, kSteps = 4;
-    // The running maximum m as nm = 8 - m (P = 2^(c2 s + nm); infinite before the first key), the
-    // sum over this lane's keys.
-    float nm = __builtin_huge_valf(), sum = 0.f, c2;
+    // The reference score, nm (infinite before the first key), the sum over this lane's keys.
+    float r = -__builtin_huge_valf(), nm = __builtin_huge_valf(), sum = 0.f, c2;
     f4v o[8], s[2];
     int lg, tkey;
 
@@ -280,18 +305,23 @@ struct ChunkRows<16> {
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, s[h][i]);
-        top *= c2;
-        if (__any(top > -__builtin_huge_valf() && !(top + nm <= kCaUp + kCaSlack))) {
-            const float to = kCaUp - rows_max(top);  // inf where the row saw nothing in this step
-            if (to < nm) {
-                const float c = __builtin_amdgcn_exp2f(to - nm);  // 0 before the first key
-                nm = to;
+        float base = nm < __builtin_huge_valf() ? nm : 0.f;
+        if (__builtin_expect(__any(top > -__builtin_huge_valf() && !(__builtin_fmaf(top, c2, nm) <= kUp + kSlack)), 0)) {
+            const float m = rows_max(top);  // -inf where the row saw nothing in this step
+            if (m > r) {
+                const float c = raise(m, c2, r, nm);  // 0 before the first key
                 sum *= c;
 #pragma unroll
                 for (int d = 0; d < 8; ++d) o[d] *= c;
+                base = nm;
+            }
+            if (__builtin_expect(__any(nm != nm), 0)) {
+                const float off = nm != nm ? r : 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[h] -= off;
+                base = nm != nm ? kUp : base;
             }
         }
-        const float base = nm < __builtin_huge_valf() ? nm : 0.f;
         h8v hi, lo;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -312,14 +342,14 @@ struct ChunkRows<16> {
     // Leaves the state in ca_state_bytes(16) of LDS; the sums' signs say `odd`.
     __device__ __forceinline__ void leave(unsigned char* to, int lane, bool odd) const {
         float* so = reinterpret_cast<float*>(to);
-        const float l = __builtin_fabsf(rows_sum(sum));
-        const int r = lane & 15;
+        const float fix = at_r(r, nm, c2), l = __builtin_fabsf(rows_sum(sum)) * fix;
+        const int row = lane & 15;
         if (lg == 0) {
-            so[16 * kCaRow + r] = left_maximum(nm, l);
-            so[16 * (kCaRow + 1) + r] = odd ? -l : l;
+            so[16 * kCaRow + row] = left_r(r, l);
+            so[16 * (kCaRow + 1) + row] = odd ? -l : l;
         }
 #pragma unroll
-        for (int d = 0; d < 8; ++d) *reinterpret_cast<f4v*>(so + r * kCaRow + 16 * d + 4 * lg) = o[d];
+        for (int d = 0; d < 8; ++d) *reinterpret_cast<f4v*>(so + row * kCaRow + 16 * d + 4 * lg) = o[d] * fix;
     }
 };
 
@@ -328,7 +358,7 @@ struct ChunkRows<16> {
 template <>
 struct ChunkRows<32> {
     static constexpr int kHalves = 1, kSteps = 8;
-    float nm = __builtin_huge_valf(), sum = 0.f, c2;
+    float r = -__builtin_huge_valf(), nm = __builtin_huge_valf(), sum = 0.f, c2;
     f16v o[4], s;
     int half, tkey, tchunk;
 
@@ -365,19 +395,23 @@ struct ChunkRows<32> {
         float top = -__builtin_huge_valf();
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
-        top *= c2;
-        if (__any(top > -__builtin_huge_valf() && !(top + nm <= kCaUp + kCaSlack))) {
+        float base = nm < __builtin_huge_valf() ? nm : 0.f;
+        if (__builtin_expect(__any(top > -__builtin_huge_valf() && !(__builtin_fmaf(top, c2, nm) <= kUp + kSlack)), 0)) {
             const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            const float to = kCaUp - fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-            if (to < nm) {
-                const float c = __builtin_amdgcn_exp2f(to - nm);
-                nm = to;
+            const float m = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            if (m > r) {
+                const float c = raise(m, c2, r, nm);
                 sum *= c;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) o[d] *= c;
+                base = nm;
+            }
+            if (__builtin_expect(__any(nm != nm), 0)) {
+                const float off = nm != nm ? r : 0.f;
+                s -= off;
+                base = nm != nm ? kUp : base;
             }
         }
-        const float base = nm < __builtin_huge_valf() ? nm : 0.f;
         const unsigned char* tr = vt + tkey * 256 + (lane & 1) * 8;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -398,18 +432,19 @@ struct ChunkRows<32> {
     __device__ __forceinline__ void leave(unsigned char* to, int lane, bool odd) const {
         float* so = reinterpret_cast<float*>(to);
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
-        const int r = lane & 31;
+        const int row = lane & 31;
+        const float fix = at_r(r, nm, c2);
         if (half == 0) {
-            const float l = __builtin_fabsf(__uint_as_float(x[0]) + __uint_as_float(x[1]));
-            so[32 * kCaRow + r] = left_maximum(nm, l);
-            so[32 * (kCaRow + 1) + r] = odd ? -l : l;
+            const float l = __builtin_fabsf(__uint_as_float(x[0]) + __uint_as_float(x[1])) * fix;
+            so[32 * kCaRow + row] = left_r(r, l);
+            so[32 * (kCaRow + 1) + row] = odd ? -l : l;
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<f4v*>(so + r * kCaRow + 32 * d + 8 * j + 4 * half) =
-                    f4v{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+                *reinterpret_cast<f4v*>(so + row * kCaRow + 32 * d + 8 * j + 4 * half) =
+                    f4v{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]} * fix;
     }
 };
 
@@ -437,21 +472,22 @@ __device__ __forceinline__ void join_waves(const ChunkArgs& a, const ChunkPlace&
                                            const unsigned char* states, int stride, int sub, int subs) {
     const int M = a.g * a.t, d4 = threadIdx.x & 31;
     const float* of = reinterpret_cast<const float*>(states);
+    const float c2 = score_factor(a.scale);
     for (int r = sub; r < R; r += subs) {
         if (row0 + r >= M) break;
-        float top = __builtin_huge_valf();
+        float top = -__builtin_huge_valf();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fminf(top, of[w * (stride / 4) + R * kCaRow + r]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, of[w * (stride / 4) + R * kCaRow + r]);
         float l = 0.f;
         bool odd = false;
         f4v acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) odd |= __builtin_signbit(of[w * (stride / 4) + R * (kCaRow + 1) + r]);
-        if (top < __builtin_huge_valf())
+        if (top > -__builtin_huge_valf())
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 const float* ow = of + w * (stride / 4);
-                const float c = __builtin_amdgcn_exp2f(top - ow[R * kCaRow + r]);
+                const float c = rescale(ow[R * kCaRow + r], top, c2);
                 l += c * __builtin_fabsf(ow[R * (kCaRow + 1) + r]);
                 acc += c * *reinterpret_cast<const f4v*>(ow + r * kCaRow + 4 * d4);
             }

@@ -37,8 +37,6 @@ constexpr int kPaThreads = 256;
 constexpr int kPaTokens = 128;  // tokens of a block
 constexpr int kPaKeys = 64;     // keys of a tile
 constexpr int kPaBufferWord3 = 0x00020000;  // buffer descriptor: raw, range-checked
-constexpr float kPaUp = 8.f;    // P is held scaled by 2^8, and grows by up to 2^7 before the
-constexpr float kPaSlack = 7.f; // running maximum is raised, which keeps it below 2^16
 
 __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs a, int qtiles) {
     // Arrays of their own, chosen at compile time: in one array the compiler cannot tell a read of
@@ -79,7 +77,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
     const int p = span.start + tok;
     const int wave_first = span.start + min(i0 + 32 * wave, i1 - 1);
     const int wave_last = span.start + min(i0 + 32 * wave + 31, i1 - 1);
-    float nm, sum;
+    float r, nm, sum;
     float one = 1.f;  // kept from the compiler: x * one + sum stays one instruction that takes a float16 x
     asm("" : "+s"(one));
     f16v o[4];
@@ -183,20 +181,26 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[h][i]);
-            top *= c2;
-            if (__builtin_expect(__any(top > -__builtin_huge_valf() && !(top + nm <= kPaUp + kPaSlack)), 0)) {
+            float base = nm < __builtin_huge_valf() ? nm : 0.f;
+            if (__builtin_expect(__any(top > -__builtin_huge_valf() &&
+                                       !(__builtin_fmaf(top, c2, nm) <= kUp + kSlack)), 0)) {
                 const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                const float to = kPaUp - fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-                if (to < nm) {
-                    const float c = __builtin_amdgcn_exp2f(to - nm);
-                    nm = to;
+                const float m = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+                if (m > r) {
+                    const float c = raise(m, c2, r, nm);
                     sum *= c;
 #pragma unroll
                     for (int d = 0; d < 4; ++d) o[d] *= c;
+                    base = nm;
+                }
+                if (__builtin_expect(__any(nm != nm), 0)) {
+                    const float off = nm != nm ? r : 0.f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) s[h] -= off;
+                    base = nm != nm ? kUp : base;
                 }
             }
             __builtin_amdgcn_s_setprio(1);  // ahead of another wave's S^T: 1%
-            const float base = nm < __builtin_huge_valf() ? nm : 0.f;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 h8v pf[2];
@@ -230,6 +234,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void prompt_attend_kernel(ChunkArgs 
         __syncthreads();  // and the next tile is there
     };
     for (;; careful = true) {
+        r = -__builtin_huge_valf();
         nm = __builtin_huge_valf();
         sum = 0.f;
 #pragma unroll
