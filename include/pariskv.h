@@ -519,7 +519,8 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
  * in float32 (scores have to be finite there; one that is NaN, by the query or
  * by a key that the token sees, makes the token's output NaN).
  *   q       device float16 [batch][Hq][t][D]
- *   K, V    device float16 [batch][Hkv][kv_capacity][D], the cached rows
+ *   K, V    device float16 [batch][Hkv][kv_capacity][D], the cached rows.  An
+ *           infinity or NaN in a value leaves its dim of out infinite or NaN
  *   n       cached rows of every sequence, 0..kv_capacity; with lens (device
  *           int32 [batch], or NULL) sequence b has min(max(lens[b], 0), n)
  *   K_tree, V_tree  device float16 [batch][Hkv][t][D], the drafts' own rows
@@ -527,7 +528,7 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
  *   mask    device int64 [batch][t]: bit j of word i lets token i attend draft
  *           j (bits from t on are ignored); NULL: a chain, drafts j <= i.
  *           A draft's values, whatever they are (infinities, NaNs), reach only
- *           the tokens that attend it.
+ *           the tokens that attend it, whose dim is then infinite or NaN.
  *   out     device float [batch][Hq][t][D]; zero where a token attends nothing
  *   workspace  device, >= pariskv_tree_workspace(...) bytes, 256-byte aligned;
  *           overwritten, so calls that overlap need one each
@@ -564,7 +565,9 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D]: row j holds position j,
  *           the new tokens' rows among them.  A row's values, whatever they are
- *           (infinities, NaNs), reach only the tokens that attend it
+ *           (infinities, NaNs), reach only the tokens that attend it, whose dim
+ *           is then infinite or NaN (which of the two an infinity gives is not
+ *           specified)
  *   pos     position of the first new token; with starts (device int32 [batch],
  *           or NULL) that of sequence b is min(max(starts[b], 0), pos)
  *   counts  device int32 [batch] or NULL: sequence b has min(max(counts[b], 0),

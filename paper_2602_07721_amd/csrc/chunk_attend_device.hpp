@@ -167,8 +167,10 @@ __device__ __forceinline__ uint32_t draft_bits(const ChunkArgs& a, int seq, int 
 // Values of V that are not finite.  A key that a token does not see has a weight of 0 there, but 0
 // times infinity is not 0, and a draft or a row that overflowed must not spoil tokens that do not
 // see it.  So where not every token sees every key (drafts; the ends of windows) the products get
-// such values as 0, and the rows that see them have them added at the end, if there were any:
-// infinities and NaNs come out of any weight as they are.
+// such values as 0, and the rows that see them have them added at the end, if there were any.
+// Where every token sees the key the products take them as they are, and an infinity may come out
+// as NaN (a weight's second part may be 0 or negative): either way the dim is not finite for the
+// tokens that see the key, and for no others.
 //
 // Sets bits of kOddBits in m if one of v's 8 values is such a value (all ones in its exponent).
 constexpr uint32_t kOddBits = 0x80008000u;
