@@ -517,7 +517,9 @@ size_t pariskv_tree_workspace(const pariskv_config* cfg, int32_t batch, int64_t 
  * mask names, its ancestors in the tree of drafts and itself,
  *   o_i = sum_j softmax_j(scale <k_j, q_i>) v_j
  * in float32 (scores have to be finite there; one that is NaN, by the query or
- * by a key that the token sees, makes the token's output NaN).
+ * by a key that the token sees, makes the token's output NaN), within 2^-20 of the
+ * largest |v|, twice the float32 rounding of the scores and 2^-33 a row that the
+ * token sees, for weights that are nothing beside the largest.
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D], the cached rows.  An
  *           infinity or NaN in a value leaves its dim of out infinite or NaN
@@ -559,9 +561,10 @@ size_t pariskv_sink_window_workspace(const pariskv_config* cfg, int32_t batch, i
  * or j > p - window (window >= pos + t: plain causal attention).  A score that
  * is NaN, by the query or by a key that the token sees, makes its output NaN.
  * Scores and sums are float32, also where many tokens' weights are rounded to
- * float16 (and summed as rounded): an output is then within 2^-11 of the largest
- * |v| that its token sees before it is rounded itself, within 2^-20 otherwise,
- * plus twice the float32 rounding of the scores.
+ * float16 (and summed as rounded): before it is rounded itself, an output is then
+ * within 2^-11 of the largest |v| that its token sees, otherwise within 2^-20;
+ * twice the float32 rounding of the scores and 2^-33 a row that the token sees,
+ * for weights that are nothing beside the largest, come on top.
  *   q       device float16 [batch][Hq][t][D]
  *   K, V    device float16 [batch][Hkv][kv_capacity][D]: row j holds position j,
  *           the new tokens' rows among them.  A row's values, whatever they are

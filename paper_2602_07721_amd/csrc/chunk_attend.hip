@@ -7,9 +7,11 @@
 //   O^T += V^T P^T the scores' own registers are the second operand: matrix instructions sum
 //                  over 32 keys in any order, as long as both operands agree on it.
 // Float32 results from float16 instructions: products are exact and summed in float32; P is
-// split into two float16 values (their sum is P to 2^-22 of it), two instructions instead of
-// one.  The maximum is raised only when a score exceeds it by 2^7, so that P, scaled by 2^8,
-// stays below 2^16 and small P lose nothing.
+// split into two float16 values, two instructions instead of one, which leave 2^-22 of it or
+// 2^-25, half their smallest step.  P is at least 2^8 for the largest weight, so that is 2^-33 of
+// the largest weight, for a key that weighs less than 2^-11 of it; n such keys shift an output by
+// up to n 2^-33 of the largest |v|.  The reference score is raised only when a weight passes 2^7
+// times its own, so P stays below 2^16.
 //
 // Here, up to 32 rows: bound by HBM, so each wave walks keys of its own, nothing is shared and
 // nothing waits.  Float16 K goes from HBM to registers as the operand it is.  V^T needs a
