@@ -12,10 +12,13 @@
 //
 // Record of one token and KV head, quant_record_bytes() long: the K codes in order of their
 // dims (two 4-bit codes a byte, the even dim low), the V codes, 4 bytes s + 127 of K's
-// blocks, 4 of V's, zeros up to a multiple of 16 bytes.  One record instead of four arrays
-// keeps a retrieved row's bytes together (a gathered row of two 8-bit halves touches 3.1
-// cache lines of 128 bytes on average, 4 with the scales apart) and a range of rows one
-// stretch of memory.
+// blocks, 4 of V's, zeros up to a multiple of 16 bytes.  A gathered record touches 3 cache lines of
+// 128 bytes (8/8 bits: 272 bytes at any multiple of 16 end within three), 2.5 on average (8/4: 208)
+// or 2 (4/4: 144).  With the 8 scale bytes of a row in an array of their own it would be as many, 3
+// (8/8) and 2 (4/4), or more, 3 (8/4); one record keeps a range of rows one stretch of memory, to
+// write, to stream and to move between HBM and the host.  What it costs: 16 of its bytes hold 8 of
+// scales, and over the host link, with the scales left in HBM, the codes alone would be 1 line
+// instead of 2 (4/4) or 2 instead of 3 (8/8).
 #pragma once
 
 #include <hip/hip_runtime.h>
