@@ -363,7 +363,9 @@ void chunk_plan(ChunkArgs& a) {
 // Both forms' times in ns, fitted to 165 calls of 1 to 512 tokens, 1 to 128 (sequence, KV head)s
 // and windows of 512 to 16384 rows: 1 x 8 x 4 heads, 4096 rows, 16 tokens: 20 us here, 78 in the
 // prompt form; 128 tokens 39 and 83; 16 x 8 x 4, 4096 rows, 32 tokens 88 and 125, 64 tokens 144 and
-// 130, 128 tokens 235 and 147; 512 rows, 32 tokens 37 and 25.
+// 130, 128 tokens 235 and 147; 512 rows, 32 tokens 37 and 25.  Over 135 other calls the choice is
+// 0.5% behind the faster form on average, more than 5% in 4, 31% at worst (2 x 7 heads, 1024 tokens,
+// 4096 rows: 107 us here, 81 in the prompt form).
 bool few_tokens(const ChunkArgs& a) {
     if (a.t > kFewTokens) return false;
     const double groups = (double)a.batch * a.hkv, rows = (double)a.g * a.t, all = (double)(a.n + a.t);

@@ -21,7 +21,8 @@
 // and an exponential, a maximum, a sum and a rounding), with LDS close behind: a wave reads 32
 // KB a tile, which takes the block as long as its matrix instructions.  64 tokens a wave would
 // halve that but leave one wave a SIMD: 870 us where 32 took 660.  32 heads, 8192 tokens after
-// 8192 others, window 4096: 544 us, 1042 TFLOP/s (a plain float16 matrix product: 1147).
+// 8192 others, window 4096: 541 to 574 us from card to card, 990 to 1050 TFLOP/s (a plain float16
+// matrix product: 1147).
 
 #include <hip/hip_fp16.h>
 
