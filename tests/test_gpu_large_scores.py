@@ -20,10 +20,12 @@ def _want(q, K, V, visible, scale, half_out):
     s = np.where(visible, scale * (q.astype(np.float64) @ K.astype(np.float64).T), -np.inf)
     top = s.max(1, keepdims=True)
     best = s == top
-    A = abs(scale) * (np.abs(q.astype(np.float64)) @ np.abs(K.astype(np.float64)).T).max()
-    # A score is off by at most (4 sqrt(128) 2^-24 + 2^-22) A (see tolerance()): a key that is 2 such errors and 30 below
-    # the top weighs less than e^-30.
-    clear = (np.where(best, -np.inf, s).max(1) < top[:, 0] - 30 - 2 * (4 * np.sqrt(128) * 2.0 ** -24 + 2.0 ** -22) * A)
+    # A score is off by at most (4 sqrt(128) 2^-24 + 2^-22) of A = |scale| sum |q k| (see tolerance()): a key that is both
+    # its own and the top's such error and 30 below the top weighs less than e^-30.
+    off = (4 * np.sqrt(128) * 2.0 ** -24 + 2.0 ** -22) * abs(scale) * (
+        np.abs(q.astype(np.float64)) @ np.abs(K.astype(np.float64)).T)
+    lowest = np.where(best, s - off, np.inf).min(1)
+    clear = np.where(best, -np.inf, s + off).max(1) < lowest - 30
     assert clear.mean() > 0.9, "the inputs leave the choice open"
     w = best / best.sum(1, keepdims=True)
     return w @ V.astype(np.float64), (2.0 ** -19 + (2.0 ** -10 if half_out else 0.0)) * np.abs(V).max(), clear
@@ -108,3 +110,24 @@ def test_listed_rows(qsize, ksize, scale):
         rows = idx[0, h]
         _check(out[0, h][None], q[0, h][None], K[0, h // g, rows], V[0, h // g, rows], np.ones((1, k), bool), scale,
                False, f"head {h}")
+
+
+@pytest.mark.parametrize("order", ["none", "grows", "falls"])
+@pytest.mark.parametrize("t", [3, 8, 16, 31, 1100])
+def test_scores_far_below_zero(t, order):
+    # Every score is negative and large: the weights are those of the least negative ones.
+    print(f"[large] below zero t {t} {order}", flush=True)
+    hkv, g, n = 2, 4, 2500
+    r = np.random.default_rng(t)
+    cfg = _cfg(hkv, g)
+    K = -np.abs(_rows(r, 1, hkv, n + t, 12000.0, order)) - np.float16(2000)
+    V = draw(r, 1, hkv, n + t, D)
+    q = (np.abs(draw(r, 1, hkv * g, t, D).clip(-4, 4).astype(np.float32)) * 8000 + 100).astype(np.float16)
+    see = np.concatenate([np.ones((t, n), bool), np.tril(np.ones((t, t), bool))], 1)
+    outs = [(pk.sink_window_attend(cfg, gpu(q), gpu(K), gpu(V), n, 0, n + t, SCALE), True)]
+    if t <= pk.MAX_TREE:
+        Kt, Vt = (np.ascontiguousarray(x[:, :, n:]) for x in (K, V))
+        outs.append((pk.tree_attend(cfg, gpu(q), gpu(K), gpu(V), gpu(Kt), gpu(Vt), n, SCALE), False))
+    for out, half in outs:
+        for h in range(hkv * g):
+            _check(out.cpu().numpy()[0, h], q[0, h], K[0, h // g], V[0, h // g], see, SCALE, half, f"head {h}")
