@@ -587,6 +587,128 @@ int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const v
                                const int32_t* counts, int64_t sink, int64_t window, int32_t batch, float scale,
                                void* out, void* workspace, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------- paged K/V cache */
+
+/* K/V rows of many sequences in one pool, so that a sequence takes memory by the
+ * page and not by the longest of them.
+ *   K, V  device float16 [n_pages][Hkv][page_size][D], 16-byte aligned
+ * A sequence's table names its pages: its row r is row r % page_size of page
+ * table[r / page_size].  A slot is page * page_size + row in the page.  At most
+ * 2^30 - 1 slots, and 2^31 - 1 with the KV heads.  A dense cache [batch][Hkv]
+ * [capacity][D] is one of `batch` pages of `capacity` rows. */
+typedef struct pariskv_pages {
+    void* K;
+    void* V;
+    int64_t n_pages;
+    int32_t page_size; /* any number >= 1 */
+} pariskv_pages;
+
+/* A step of a batch of sequences, all arrays in device memory, int32, 4-byte
+ * aligned.  Read (and the table and the free pages written in place): */
+typedef struct pariskv_page_step {
+    int32_t* table;      /* [batch][table_width]: the pages of each sequence      */
+    int64_t table_width; /* 1..2^30-1                                             */
+    int32_t* free_pages; /* [n_pages], a stack: the free pages are its first      */
+    int64_t n_pages;     /*   *n_free entries (taken as 0..n_pages)               */
+    int32_t page_size;
+    const int32_t* n_free;
+    const int32_t* lens;   /* [batch] rows of each sequence (taken as 0..room of its
+                              table)                                              */
+    const int32_t* counts; /* [batch] rows that it gets (its new tokens), or, below
+                              0, that it gives back from its end (at most all)    */
+    int32_t batch;         /* 1..65535                                            */
+    int64_t t;             /* entries of slots and positions, 0..2^24             */
+    /* written: */
+    int32_t* new_lens;  /* [batch] rows afterwards; may be lens                   */
+    int32_t* new_free;  /* [1] free pages afterwards; may be n_free               */
+    int32_t* offsets;   /* [batch + 1] sequence b's tokens are offsets[b] up to
+                           offsets[b + 1] of the step's, packed in the order of the
+                           sequences (granted or not); at most t                  */
+    int32_t* granted;   /* [batch] counts[b], or 0 (see below); may be counts     */
+    int32_t* slots;     /* [t] where each token's row belongs; -1 for tokens that
+                           were not granted and behind the last                   */
+    int32_t* positions; /* [t] its row in its sequence; -1 likewise               */
+} pariskv_page_step;
+
+/* Plans a step: pages given back go onto the stack, pages for the new rows are
+ * taken from it.  The pages given back are pushed so that taking as many again
+ * takes the same in the same order, sequence after sequence, row after row; the
+ * entries behind the free ones are left as they fell.  A sequence gets all of its
+ * rows or none: none when they exceed its table (batch tokens before it included:
+ * when its tokens do not fit into t), or when the pages wanted by it and by the
+ * sequences before it, those granted none for want of pages included, are more
+ * than there are.  The table's entries behind a sequence's rows are not read.
+ * A page may be in one table only; pages that tables share are the caller's.
+ * Errors: INVALID, UNSUPPORTED (batch, t), HIP. */
+int pariskv_plan_pages(const pariskv_page_step* step, void* stream);
+
+/* New tokens' rows on their way into the cache: queries and keys normalised for
+ * each head, y = x w / sqrt(mean(x^2) + eps), and rotated by their positions,
+ * keys and values written to their slots; one pass, float32 inside, rounded once.
+ *   q, k, v    device float16 [t][Hq | Hkv | Hkv][D], tokens q_stride, k_stride,
+ *              v_stride values apart (multiples of 8: the columns of one product)
+ *   positions  device int32 [t]
+ *   slots      device int32 [t]; for a token whose slot lies outside the pages
+ *              nothing is done (its row of q_out too is left as it was).  Slots
+ *              must differ: of equal ones any token's row may stay, or parts
+ *   freqs      device float [rot_dim / 2], radians a position: pair i turns by
+ *              positions * freqs[i], whole turns taken off in 64 bits (exact to
+ *              float32's rounding while that is below 2^31)
+ *   rot_dim    dims that are rotated, the first ones: a multiple of 16 up to D
+ *   pairs      0: dims i and i + rot_dim / 2 are pair i; 1: dims 2 i and 2 i + 1
+ *   q_weight, k_weight  device float [D], or NULL: no norm
+ *   q_out      device float16 [t][Hq][D]; may be q where its tokens are Hq D apart
+ * t = 0 does nothing.
+ * Errors: INVALID, UNSUPPORTED (t above 2^24), HIP. */
+int pariskv_rotate_rows(const pariskv_config* cfg, const pariskv_pages* pages, const void* q, int64_t q_stride,
+                        const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t t,
+                        const int32_t* positions, const int32_t* slots, const float* freqs, int32_t rot_dim,
+                        int32_t pairs, const float* q_weight, const float* k_weight, float eps, void* q_out,
+                        void* stream);
+
+/* Bytes of a workspace for pariskv_paged_attend with these sizes and every smaller
+ * batch, t and max_tokens (at least 256, below 140 MB; 0 on invalid input). */
+size_t pariskv_paged_workspace(const pariskv_config* cfg, int32_t batch, int64_t t, int64_t max_tokens);
+
+/* Attention of the new tokens of a batch -- one of each sequence, chunks of prompts
+ * and whole prompts, in any mixture -- over their sequences' pages:
+ *   o_i = sum_j softmax_j(f(scale <k_j, q_i>) - slope (p - j)) v_j,  j <= p
+ * for the token at position p, f the identity or, with softcap > 0,
+ * f(s) = softcap tanh(s / softcap); slope = slopes[query head], 0 without.
+ *   q        device float16 [t][Hq][D], tokens q_stride values apart; the tokens of
+ *            the sequences behind each other
+ *   table    device int32 [batch][table_width].  Rows of a page outside
+ *            [0, n_pages) are attended by nobody
+ *   lens     device int32 [batch]: rows of each sequence, its new tokens' included
+ *            (taken as 0..room of its table)
+ *   offsets  device int32 [batch + 1], rising, 0..t: sequence b has the tokens
+ *            offsets[b] up to offsets[b + 1], at positions up to lens[b] - 1
+ *   counts   device int32 [batch], or NULL: sequence b has the first counts[b] of
+ *            these only (of none for counts below 0)
+ *   max_tokens  the most tokens of a sequence, >= 1; those beyond are not computed
+ *   slopes   device float [Hq], or NULL
+ *   out      device float16 [t][Hq][D]; zero where a token attends nothing; rows of
+ *            tokens that no sequence has are left as they were
+ *   workspace  device, >= pariskv_paged_workspace(...) bytes, 256-byte aligned;
+ *            overwritten, so calls that overlap need one each
+ * Only sizes decide what is launched: a captured call holds for any lens, offsets,
+ * counts and table later written to the same memory.
+ * Scores and sums are float32 (finite scores, as for pariskv_tree_attend; one that
+ * is NaN makes its token's output NaN); calls with max_tokens * q_per_kv above 32
+ * round weights to float16 and sum them as rounded.  Before it is rounded itself an
+ * output is then within 2^-11 of the largest |v| that its token sees, otherwise
+ * within 2^-20; twice the scores' float32 rounding (2^-21 softcap with one) and
+ * 2^-33 a row come on top.  A row's values, whatever they are, reach only the tokens
+ * that attend it, whose dim is then infinite or NaN.
+ * t = 0 does nothing.
+ * Errors: INVALID, UNSUPPORTED (batch above 65535, t above 2^24, more than 2^24
+ * blocks), WORKSPACE, HIP. */
+int pariskv_paged_attend(const pariskv_config* cfg, const void* q, int64_t q_stride, const pariskv_pages* pages,
+                         const int32_t* table, int64_t table_width, const int32_t* lens, const int32_t* offsets,
+                         const int32_t* counts, int64_t t, int64_t max_tokens, int32_t batch, float scale,
+                         float softcap, const float* slopes, void* out, void* workspace, size_t ws_bytes,
+                         void* stream);
+
 /* ------------------------------------------------- without a caller workspace */
 
 /* Bytes of the static scratch array pariskv_retrieve_attend_noalloc keeps its

@@ -24,7 +24,8 @@ __all__ = [
     "window_regions", "window_attend", "retrieve_window_attend", "tiered_attend", "retrieve_tiered_attend",
     "offload_rows", "window_slot", "group_attend", "QuantCache", "quantize_rows", "dequantize_rows",
     "quant_attend", "quant_tiered_attend", "tree_attend", "quant_tree_attend", "tree_workspace_size",
-    "sink_window_attend", "sink_window_workspace_size", "MAX_TREE", "quantizer_table", "rotation_signs",
+    "sink_window_attend", "sink_window_workspace_size", "MAX_TREE",
+    "PagedCache", "PagePlan", "plan_pages", "rotate_rows", "paged_attend", "paged_workspace_size", "quantizer_table", "rotation_signs",
     "profile_enable", "profile_reset", "profile_read", "stream_copy", "stream_read",
 ]
 
@@ -75,6 +76,19 @@ class _Window(ctypes.Structure):
 class _QuantCache(ctypes.Structure):
     _fields_ = [("rec", ctypes.c_void_p), ("capacity", ctypes.c_int64), ("k_bits", ctypes.c_int32),
                 ("v_bits", ctypes.c_int32), ("host_mapped", ctypes.c_int32)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32)]
+
+
+class _PageStep(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_width", ctypes.c_int64), ("free_pages", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("n_free", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("batch", ctypes.c_int32), ("t", ctypes.c_int64),
+                ("new_lens", ctypes.c_void_p), ("new_free", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
+                ("granted", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
 
 
 class _Layout(ctypes.Structure):
@@ -152,6 +166,13 @@ def lib():
         L.pariskv_sink_window_workspace.restype = SZ
         L.pariskv_sink_window_attend.argtypes = [P(_Config), VP, VP, VP, I64, I64, VP, I64, VP, I64, I64, I32, F, VP,
                                                  VP, SZ, VP]
+        L.pariskv_plan_pages.argtypes = [P(_PageStep), VP]
+        L.pariskv_rotate_rows.argtypes = [P(_Config), P(_Pages), VP, I64, VP, I64, VP, I64, I64, VP, VP, VP, I32, I32, VP,
+                                          VP, F, VP, VP]
+        L.pariskv_paged_workspace.argtypes = [P(_Config), I32, I64, I64]
+        L.pariskv_paged_workspace.restype = SZ
+        L.pariskv_paged_attend.argtypes = [P(_Config), VP, I64, P(_Pages), VP, I64, VP, VP, VP, I64, I64, I32, F, F, VP,
+                                           VP, VP, SZ, VP]
         L.pariskv_stream_copy.argtypes = [VP, VP, SZ, VP]
         L.pariskv_stream_read.argtypes = [VP, SZ, ctypes.c_uint32, VP, VP]
         L.pariskv_quantizer_table.argtypes = [I32, P(ctypes.c_double), P(ctypes.c_double)]
@@ -858,6 +879,177 @@ def sink_window_attend(cfg, q, K, V, pos, sink, window, scale, starts=None, coun
     _require_here(stream, q, K, V, starts, counts, out, workspace)
     _check(lib().pariskv_sink_window_attend(cfg.c(), qp, kp, vp, cap, int(pos), sp, t, np_, int(sink), int(window), batch,
                                             float(scale), op, wp, workspace.numel(), _stream(stream)))
+    return out
+
+
+# ---- paged K/V cache
+
+
+class PagedCache:
+    """A pool of pages (see ``pariskv_pages``): K, V [n_pages][Hkv][page_size][D] float16 on the GPU."""
+
+    def __init__(self, K, V):
+        self.K, self.V = K, V
+
+    @classmethod
+    def empty(cls, cfg, n_pages, page_size, device="cuda"):
+        torch = _torch()
+        shape = (n_pages, cfg.n_kv_heads, page_size, HEAD_DIM)
+        return cls(*(torch.empty(shape, dtype=torch.float16, device=device) for _ in range(2)))
+
+    @property
+    def n_pages(self):
+        return int(self.K.shape[0])
+
+    @property
+    def page_size(self):
+        return int(self.K.shape[2])
+
+    def c(self, cfg, dev):
+        half = _torch().float16
+        shape = (self.K.shape[0] if isinstance(self.K, _torch().Tensor) and self.K.dim() == 4 else None, cfg.n_kv_heads,
+                 _rows(self.K), HEAD_DIM)
+        kp = _arg(self.K, "cache.K", half, shape, dev)
+        vp = _arg(self.V, "cache.V", half, tuple(self.K.shape), dev)
+        self._c = _Pages(kp, vp, self.K.shape[0], self.K.shape[2])
+        return ctypes.byref(self._c)
+
+
+class PagePlan:
+    """What plan_pages writes, int32 on the GPU (see ``pariskv_page_step``): lens [batch] and n_free [1] after the step,
+    offsets [batch + 1] of the sequences' tokens, counts [batch] granted, slots and positions [t] of the tokens."""
+
+    def __init__(self, lens, n_free, offsets, counts, slots, positions):
+        self.lens, self.n_free, self.offsets, self.counts = lens, n_free, offsets, counts
+        self.slots, self.positions = slots, positions
+
+    @classmethod
+    def empty(cls, batch, t, device="cuda", stream=None):
+        return cls(*(_new((n,), _torch().int32, device, stream) for n in (batch, 1, batch + 1, batch, t, t)))
+
+
+def plan_pages(table, free, n_free, lens, counts, page_size, t=None, plan=None, stream=None):
+    """Pages, slots and positions of a step's new tokens: counts[b] rows more for sequence b (below 0: rows given back)
+    of lens[b].  table [batch][width] and the stack free [n_pages], of which n_free [1] are free, are written in place; all
+    int32 on the GPU.  t: entries of slots and positions (without a plan).  A plan's lens and n_free may be lens and n_free
+    themselves, its counts counts.  Returns the plan."""
+    torch = _torch()
+    dev, i32 = [], _torch().int32
+    for x, nm, dims in ((table, "table", 2), (free, "free", 1)):
+        if not isinstance(x, torch.Tensor) or x.dim() != dims:
+            raise ValueError(f"{nm} must be a{' [batch][width]' if dims == 2 else ' [n_pages]'} int32 tensor")
+    batch = int(table.shape[0])
+    tp, fp = _arg(table, "table", i32, tuple(table.shape), dev), _arg(free, "free", i32, tuple(free.shape), dev)
+    np_, lp = _arg(n_free, "n_free", i32, (1,), dev), _arg(lens, "lens", i32, (batch,), dev)
+    cp = _arg(counts, "counts", i32, (batch,), dev)
+    if plan is None:
+        if t is None:
+            raise ValueError("t is required without a plan")
+        plan = PagePlan.empty(batch, int(t), table.device, stream)
+    elif not isinstance(plan, PagePlan):
+        raise TypeError("plan must be a PagePlan")
+    if not isinstance(plan.slots, torch.Tensor) or plan.slots.dim() != 1:
+        raise ValueError("plan.slots must be a [t] int32 tensor")
+    n = int(plan.slots.shape[0])
+    if t is not None and int(t) != n:
+        raise ValueError(f"t is {t}, but the plan has {n} slots")
+    outs = [_arg(getattr(plan, k), f"plan.{k}", i32, (m,), dev) for k, m in
+            (("lens", batch), ("n_free", 1), ("offsets", batch + 1), ("counts", batch), ("slots", n), ("positions", n))]
+    _require_device(dev)
+    _require_here(stream, table, free, n_free, lens, counts, plan.lens, plan.n_free, plan.offsets, plan.counts, plan.slots,
+                  plan.positions)
+    step = _PageStep(tp, table.shape[1], fp, free.shape[0], int(page_size), np_, lp, cp, batch, n, *outs)
+    _check(lib().pariskv_plan_pages(ctypes.byref(step), _stream(stream)))
+    return plan
+
+
+def _token_rows(x, name, heads, dev, t=None):
+    """(pointer, tokens, values from one token to the next) of [t][heads][D] float16, a token's heads next to each other:
+    a contiguous tensor or columns of a wider one."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        raise ValueError(f"{name} must be a [t][heads][D] float16 tensor")
+    if x.dtype != torch.float16:
+        raise TypeError(f"{name} must be {torch.float16}, got {x.dtype}")
+    n = int(x.shape[0])
+    if x.shape[1] != heads or x.shape[2] != HEAD_DIM or (t is not None and n != t):
+        raise ValueError(f"{name} must have shape [{'*' if t is None else t}, {heads}, {HEAD_DIM}], got {list(x.shape)}")
+    s = x.stride()
+    if n > 0 and (s[2] != 1 or (heads > 1 and s[1] != HEAD_DIM)):
+        raise ValueError(f"{name} must have its heads next to each other")
+    if not x.is_cuda:
+        dev.append((x, name))
+    step = s[0] if n > 1 else heads * HEAD_DIM
+    if step < heads * HEAD_DIM or step % 8 or x.data_ptr() % 16:
+        raise ValueError(f"{name} must have its tokens a multiple of 8 values apart, at 16-byte addresses")
+    return x.data_ptr(), n, step
+
+
+def rotate_rows(cfg, cache, q, k, v, positions, slots, freqs=None, q_weight=None, k_weight=None, eps=1e-6, pairs=False,
+                q_out=None, stream=None):
+    """Queries q [t][Hq][D] and keys k [t][Hkv][D] normalised (with a weight [D] float32) and rotated by positions times
+    freqs (float32 [rot_dim / 2] radians; halves of the first rot_dim dims against each other, with pairs neighbours), keys
+    and values v [t][Hkv][D] written to the slots of a PagedCache.  positions, slots int32 [t]; tokens whose slot lies outside
+    the pages are left alone.  q, k and v may be columns of one tensor.  Returns q_out [t][Hq][D] float16."""
+    torch = _torch()
+    dev, i32, f32 = [], _torch().int32, _torch().float32
+    if not isinstance(cache, PagedCache):
+        raise TypeError("cache must be a PagedCache")
+    qp, t, qs = _token_rows(q, "q", cfg.n_q_heads, dev)
+    kp, _, ks = _token_rows(k, "k", cfg.n_kv_heads, dev, t)
+    vp, _, vs = _token_rows(v, "v", cfg.n_kv_heads, dev, t)
+    cp = cache.c(cfg, dev)
+    pp, sp = _arg(positions, "positions", i32, (t,), dev), _arg(slots, "slots", i32, (t,), dev)
+    if freqs is not None and (not isinstance(freqs, torch.Tensor) or freqs.dim() != 1):
+        raise ValueError("freqs must be a [rot_dim / 2] float32 tensor")
+    rot = 0 if freqs is None else 2 * int(freqs.shape[0])
+    fp = _arg(freqs, "freqs", f32, (rot // 2,), dev, optional=True)
+    qw = _arg(q_weight, "q_weight", f32, (HEAD_DIM,), dev, optional=True)
+    kw = _arg(k_weight, "k_weight", f32, (HEAD_DIM,), dev, optional=True)
+    if q_out is None:
+        q_out = _new((t, cfg.n_q_heads, HEAD_DIM), torch.float16, q.device, stream)
+    op = _arg(q_out, "q_out", torch.float16, (t, cfg.n_q_heads, HEAD_DIM), dev)
+    _require_device(dev)
+    _require_here(stream, q, k, v, cache.K, cache.V, positions, slots, freqs, q_weight, k_weight, q_out)
+    _check(lib().pariskv_rotate_rows(cfg.c(), cp, qp, qs, kp, ks, vp, vs, t, pp, sp, fp, rot, int(bool(pairs)), qw, kw,
+                                     float(eps), op, _stream(stream)))
+    return q_out
+
+
+def paged_workspace_size(cfg, batch, t, max_tokens=None):
+    """Bytes of a workspace for paged_attend with these sizes and all smaller ones (0 on invalid sizes)."""
+    return int(lib().pariskv_paged_workspace(cfg.c(), int(batch), int(t), max(1, int(t if max_tokens is None else max_tokens))))
+
+
+def paged_attend(cfg, q, cache, table, lens, offsets, scale, counts=None, max_tokens=None, softcap=0.0, slopes=None,
+                 out=None, workspace=None, stream=None):
+    """Attention of the new tokens of a batch, q [t][Hq][D] with sequence b's at offsets[b] .. offsets[b + 1] (or the first
+    counts[b] of them), over the pages that table [batch][width] names: the token at position p sees the rows up to p, the
+    last one stands at lens[b] - 1; table, lens, offsets, counts int32.  max_tokens: the most tokens of a sequence (t without;
+    1 for a decode step).  softcap c > 0 makes a score s c tanh(s / c), slopes (float32 [Hq]) take slope times the distance
+    off it.  Returns out [t][Hq][D] float16; rows of tokens that no sequence has are left as they were."""
+    torch = _torch()
+    dev, i32 = [], _torch().int32
+    if not isinstance(cache, PagedCache):
+        raise TypeError("cache must be a PagedCache")
+    qp, t, qs = _token_rows(q, "q", cfg.n_q_heads, dev)
+    cp = cache.c(cfg, dev)
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be a [batch][width] int32 tensor")
+    batch, width = (int(x) for x in table.shape)
+    tp, lp = _arg(table, "table", i32, (batch, width), dev), _arg(lens, "lens", i32, (batch,), dev)
+    op, np_ = _arg(offsets, "offsets", i32, (batch + 1,), dev), _arg(counts, "counts", i32, (batch,), dev, optional=True)
+    sp = _arg(slopes, "slopes", torch.float32, (cfg.n_q_heads,), dev, optional=True)
+    most = max(1, t) if max_tokens is None else int(max_tokens)
+    if out is None:
+        out = _new((t, cfg.n_q_heads, HEAD_DIM), torch.float16, q.device, stream)
+    outp = _arg(out, "out", torch.float16, (t, cfg.n_q_heads, HEAD_DIM), dev)
+    workspace, wp = _workspace_arg(workspace, 0 if workspace is not None else paged_workspace_size(cfg, batch, t, most), q,
+                                   dev, stream)
+    _require_device(dev)
+    _require_here(stream, q, cache.K, cache.V, table, lens, offsets, counts, slopes, out, workspace)
+    _check(lib().pariskv_paged_attend(cfg.c(), qp, qs, cp, tp, width, lp, op, np_, t, most, batch, float(scale),
+                                      float(softcap), sp, outp, wp, workspace.numel(), _stream(stream)))
     return out
 
 

@@ -36,7 +36,7 @@ HIP_FLAGS = [
 EXACT_FP = {"encode.hip", "stage1.hip"}
 HIP_SOURCES = ["api.hip", "encode.hip", "stage1.hip", "stage2.hip", "attend.hip", "group_attend.hip",
                "calib.hip", "quant.hip", "quant_attend.hip", "chunk_attend.hip", "tile_attend.hip",
-               "prompt_attend.hip"]
+               "prompt_attend.hip", "plan_pages.hip", "rotate_rows.hip", "paged_attend.hip", "paged_prompt.hip"]
 CXX_SOURCES = ["quantizer.cpp"]
 
 

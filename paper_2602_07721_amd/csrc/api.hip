@@ -16,6 +16,7 @@
 #include "../../include/pariskv.h"
 #include "chunk_attend.hpp"
 #include "internal.hpp"
+#include "pages.hpp"
 #include "quant.hpp"
 
 namespace pariskv {
@@ -1147,6 +1148,214 @@ int pariskv_sink_window_attend(const pariskv_config* cfg, const void* q, const v
     const hipError_t e = few ? launch_chunk_attend(a, static_cast<hipStream_t>(stream))
                              : launch_prompt_attend(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? PARISKV_OK : hip_fail(e, "sink_window_attend launch");
+}
+
+// ---- paged K/V cache
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// A launch has at most 2^32 - 1 threads.
+static constexpr int64_t kMaxBlocks256 = UINT32_MAX / 256;
+// Tokens of a call, sequences of a paged one.
+static constexpr int64_t kMaxTokens = 1 << 24;
+static constexpr int32_t kMaxPagedBatch = 65535;
+
+static int check_page_size(int64_t n_pages, int32_t page_size) {
+    if (page_size < 1 || n_pages < 1 || n_pages > kMaxKvRows / page_size)
+        return fail(PARISKV_ERR_INVALID, "%lld pages of %d rows: both at least 1, together at most 2^30-1 rows",
+                    (long long)n_pages, page_size);
+    return PARISKV_OK;
+}
+
+static int check_pages(const pariskv_config* cfg, const pariskv_pages* p) {
+    if (!p) return fail(PARISKV_ERR_INVALID, "pages is NULL");
+    const int rc = check_page_size(p->n_pages, p->page_size);
+    if (rc) return rc;
+    if (!p->K || !p->V || !aligned16(p->K) || !aligned16(p->V))
+        return fail(PARISKV_ERR_INVALID, "the pages' K and V must be non-NULL and 16-byte aligned");
+    if (p->n_pages * p->page_size > INT32_MAX / cfg->n_kv_heads)
+        return fail(PARISKV_ERR_UNSUPPORTED, "%lld pages x %d rows x %d KV heads above 2^31-1", (long long)p->n_pages,
+                    p->page_size, cfg->n_kv_heads);
+    return PARISKV_OK;
+}
+
+static int check_tokens(int64_t t) {
+    if (t < 0) return fail(PARISKV_ERR_INVALID, "t %lld < 0", (long long)t);
+    if (t > kMaxTokens) return fail(PARISKV_ERR_UNSUPPORTED, "%lld tokens, above 2^24", (long long)t);
+    return PARISKV_OK;
+}
+
+static int check_paged_batch(int32_t batch) {
+    if (batch < 1) return fail(PARISKV_ERR_INVALID, "batch %d < 1", batch);
+    if (batch > kMaxPagedBatch) return fail(PARISKV_ERR_UNSUPPORTED, "batch %d above %d", batch, kMaxPagedBatch);
+    return PARISKV_OK;
+}
+
+int pariskv_plan_pages(const pariskv_page_step* step, void* stream) {
+    prof_chain_start();
+    if (!step) return fail(PARISKV_ERR_INVALID, "step is NULL");
+    const pariskv_page_step& s = *step;
+    int rc = check_paged_batch(s.batch);
+    if (rc) return rc;
+    if ((rc = check_page_size(s.n_pages, s.page_size)) != PARISKV_OK) return rc;
+    if ((rc = check_tokens(s.t)) != PARISKV_OK) return rc;
+    if (s.table_width < 1 || s.table_width > kMaxKvRows)
+        return fail(PARISKV_ERR_INVALID, "table_width %lld outside 1..2^30-1", (long long)s.table_width);
+    const void* all[] = {s.table, s.free_pages, s.n_free, s.lens, s.counts, s.new_lens, s.new_free, s.offsets, s.granted};
+    for (const void* p : all)
+        if (!p || !aligned4(p))
+            return fail(PARISKV_ERR_INVALID, "every array of the step must be non-NULL and 4-byte aligned");
+    if (s.t > 0 && (!s.slots || !s.positions || !aligned4(s.slots) || !aligned4(s.positions)))
+        return fail(PARISKV_ERR_INVALID, "slots and positions must be non-NULL and 4-byte aligned");
+    PlanArgs a{};
+    a.table = s.table;
+    a.width = s.table_width;
+    a.page = divide_by(s.page_size);
+    a.free = s.free_pages;
+    a.n_pages = s.n_pages;
+    a.n_free = s.n_free;
+    a.lens = s.lens;
+    a.counts = s.counts;
+    a.batch = s.batch;
+    a.t = (int32_t)s.t;
+    a.new_lens = s.new_lens;
+    a.new_free = s.new_free;
+    a.offsets = s.offsets;
+    a.granted = s.granted;
+    a.slots = s.slots;
+    a.positions = s.positions;
+    const hipError_t e = launch_plan_pages(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "plan_pages launch");
+}
+
+// Tokens stride values apart, each rows of D of them.
+static bool stride_ok(int64_t stride, int64_t heads) {
+    return stride >= heads * kD && stride % 8 == 0 && stride <= UINT32_MAX;
+}
+
+int pariskv_rotate_rows(const pariskv_config* cfg, const pariskv_pages* pages, const void* q, int64_t q_stride,
+                        const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t t,
+                        const int32_t* positions, const int32_t* slots, const float* freqs, int32_t rot_dim,
+                        int32_t pairs, const float* q_weight, const float* k_weight, float eps, void* q_out,
+                        void* stream) {
+    prof_chain_start();
+    int rc = check_config(cfg, 1);
+    if (rc) return rc;
+    if ((rc = check_pages(cfg, pages)) != PARISKV_OK) return rc;
+    if ((rc = check_tokens(t)) != PARISKV_OK) return rc;
+    if (rot_dim < 0 || rot_dim > kD || rot_dim % 16 != 0)
+        return fail(PARISKV_ERR_INVALID, "rot_dim %d is not a multiple of 16 in 0..%d", rot_dim, kD);
+    if (pairs != 0 && pairs != 1) return fail(PARISKV_ERR_INVALID, "pairs %d is not 0 or 1", pairs);
+    if (!std::isfinite(eps) || eps < 0.f) return fail(PARISKV_ERR_INVALID, "eps is not finite and >= 0");
+    if (!stride_ok(q_stride, (int64_t)cfg->n_kv_heads * cfg->q_per_kv) || !stride_ok(k_stride, cfg->n_kv_heads) ||
+        !stride_ok(v_stride, cfg->n_kv_heads))
+        return fail(PARISKV_ERR_INVALID, "token strides %lld, %lld, %lld: multiples of 8 values that hold the heads",
+                    (long long)q_stride, (long long)k_stride, (long long)v_stride);
+    if (t == 0) return PARISKV_OK;
+    if (!q || !k || !v || !q_out || !positions || !slots || (rot_dim > 0 && !freqs))
+        return fail(PARISKV_ERR_INVALID, "q, k, v, q_out, positions, slots and freqs (with rot_dim) must be non-NULL");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned4(positions) || !aligned4(slots) ||
+        !aligned4(freqs) || !aligned4(q_weight) || !aligned4(k_weight))
+        return fail(PARISKV_ERR_INVALID, "q, k, v and q_out must be 16-byte aligned, the other arrays 4-byte");
+    RotateArgs a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.positions = positions;
+    a.slots = slots;
+    a.freqs = freqs;
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.eps = eps;
+    a.rot = rot_dim;
+    a.pairs = pairs != 0;
+    a.q_out = q_out;
+    a.K = pages->K;
+    a.V = pages->V;
+    a.n_slots = pages->n_pages * pages->page_size;
+    a.page = divide_by(pages->page_size);
+    a.t = (int32_t)t;
+    a.hkv = cfg->n_kv_heads;
+    a.g = cfg->q_per_kv;
+    const hipError_t e = launch_rotate_rows(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "rotate_rows launch");
+}
+
+static int paged_shape(const pariskv_config* cfg, int32_t batch, int64_t t, int64_t max_tokens, PagedArgs* a) {
+    int rc = check_config(cfg, 1);
+    if (rc) return rc;
+    if ((rc = check_paged_batch(batch)) != PARISKV_OK) return rc;
+    if ((rc = check_tokens(t)) != PARISKV_OK) return rc;
+    if (max_tokens < 1) return fail(PARISKV_ERR_INVALID, "max_tokens %lld < 1", (long long)max_tokens);
+    a->batch = batch;
+    a->t = (int32_t)t;
+    a->most = (int32_t)(max_tokens < t ? max_tokens : t);
+    a->hkv = cfg->n_kv_heads;
+    a->g = cfg->q_per_kv;
+    a->width = 1;
+    a->page = divide_by(1);
+    const int64_t heads = (int64_t)cfg->n_kv_heads * batch;
+    // A block for every row of a few tokens' join; for every 128 rows of more, and the shares beyond.
+    const int64_t rows = (int64_t)a->most * a->g;
+    const int64_t blocks = rows <= 32 ? rows * heads : ((int64_t)t * a->g / 128 + batch) * cfg->n_kv_heads + 16384;
+    if (blocks > kMaxBlocks256)
+        return fail(PARISKV_ERR_UNSUPPORTED, "%d sequences x %d KV heads, %lld tokens: above 2^24 blocks", batch,
+                    cfg->n_kv_heads, (long long)t);
+    return PARISKV_OK;
+}
+
+size_t pariskv_paged_workspace(const pariskv_config* cfg, int32_t batch, int64_t t, int64_t max_tokens) {
+    PagedArgs a{};
+    if (paged_shape(cfg, batch, t, max_tokens, &a) != PARISKV_OK) return 0;
+    return t == 0 ? 256 : workspace_bytes(paged_plan(a));
+}
+
+int pariskv_paged_attend(const pariskv_config* cfg, const void* q, int64_t q_stride, const pariskv_pages* pages,
+                         const int32_t* table, int64_t table_width, const int32_t* lens, const int32_t* offsets,
+                         const int32_t* counts, int64_t t, int64_t max_tokens, int32_t batch, float scale,
+                         float softcap, const float* slopes, void* out, void* workspace, size_t ws_bytes,
+                         void* stream) {
+    prof_chain_start();
+    PagedArgs a{};
+    int rc = paged_shape(cfg, batch, t, max_tokens, &a);
+    if (rc) return rc;
+    if ((rc = check_pages(cfg, pages)) != PARISKV_OK) return rc;
+    if (table_width < 1 || table_width > kMaxKvRows)
+        return fail(PARISKV_ERR_INVALID, "table_width %lld outside 1..2^30-1", (long long)table_width);
+    if (!stride_ok(q_stride, (int64_t)cfg->n_kv_heads * cfg->q_per_kv))
+        return fail(PARISKV_ERR_INVALID, "token stride %lld: a multiple of 8 values that holds the heads",
+                    (long long)q_stride);
+    if (!std::isfinite(scale)) return fail(PARISKV_ERR_INVALID, "scale is not finite");
+    if (!std::isfinite(softcap) || softcap < 0.f) return fail(PARISKV_ERR_INVALID, "softcap is not finite and >= 0");
+    if (t == 0) return PARISKV_OK;
+    if (!q || !table || !lens || !offsets || !out)
+        return fail(PARISKV_ERR_INVALID, "q, table, lens, offsets and out must be non-NULL");
+    if (!aligned16(q) || !aligned16(out) || !aligned4(table) || !aligned4(lens) || !aligned4(offsets) ||
+        !aligned4(counts) || !aligned4(slopes))
+        return fail(PARISKV_ERR_INVALID, "q and out must be 16-byte aligned, the other arrays 4-byte");
+    a.q = q;
+    a.q_stride = q_stride;
+    a.K = pages->K;
+    a.V = pages->V;
+    a.n_pages = (int32_t)pages->n_pages;
+    a.page = divide_by(pages->page_size);
+    a.table = table;
+    a.width = table_width;
+    a.lens = lens;
+    a.offsets = offsets;
+    a.counts = counts;
+    a.scale = scale;
+    a.cap = softcap;
+    a.slopes = slopes;
+    a.out = out;
+    a.workspace = workspace;
+    const size_t need = workspace_bytes(paged_plan(a));
+    if ((rc = check_workspace(workspace, ws_bytes, need)) != PARISKV_OK) return rc;
+    const hipError_t e = launch_paged_attend(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PARISKV_OK : hip_fail(e, "paged_attend launch");
 }
 
 int pariskv_stream_copy(void* dst, const void* src, size_t bytes, void* stream) {
