@@ -1,6 +1,8 @@
 // Device code that both forms of the attention over pages share.
 #pragma once
 
+#include <type_traits>
+
 #include "chunk_attend_device.hpp"
 #include "pages.hpp"
 
@@ -20,6 +22,13 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int b) {
     const int64_t room = min(a.width * (int64_t)a.page.d, kMaxKvRows);
     s.len = (int)min((int64_t)max(a.lens[b], 0), room);
     return s;
+}
+
+// The same of one that the whole wave asks about, in scalar registers.
+__device__ __forceinline__ PagedSeq scalar_seq(const PagedArgs& a, int b) {
+    const PagedSeq s = paged_seq(a, b);
+    return PagedSeq{__builtin_amdgcn_readfirstlane(s.begin), __builtin_amdgcn_readfirstlane(s.count),
+                    __builtin_amdgcn_readfirstlane(s.len)};
 }
 
 // Where a key's row lies in K and V: its page's entry, and whether there is such a page.
@@ -76,17 +85,371 @@ __device__ __forceinline__ f4v paged_odd_part(const PagedArgs& a, int b, int hea
     return sum;
 }
 
-// Sum over the lanes before this one, 64 bits.
+// Sum over the lanes before this one and over all, of values of 0 to 2^57: their bits in three parts
+// whose sums fit 32, which are moved between lanes in registers.
 __device__ __forceinline__ int64_t wave_sum_before(int64_t v, int64_t* all) {
-    const int lane = threadIdx.x & 63;
-    int64_t in = v;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t x = __shfl_up((long long)in, d, 64);
-        if (lane >= d) in += x;
+    const uint32_t low = wave_incl_sum((uint32_t)v & 0xffffu);
+    const uint32_t mid = wave_incl_sum((uint32_t)(v >> 16) & 0xffffu);
+    const uint32_t high = wave_incl_sum((uint32_t)(v >> 32));
+    const int64_t sum = ((int64_t)high << 32) + ((int64_t)mid << 16) + low;
+    *all = ((int64_t)__builtin_amdgcn_readlane((int)high, 63) << 32) +
+           ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)mid, 63) << 16) +
+           (uint32_t)__builtin_amdgcn_readlane((int)low, 63);
+    return sum - v;
+}
+
+constexpr int kPgThreads = 256, kPgWaves = kPgThreads / 64;
+constexpr int kPgBlocks = 512;  // that the chip holds, 2 a CU
+
+__device__ __forceinline__ int64_t read_lane(int64_t x, int lane) {
+    return ((int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) |
+           (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+__device__ __forceinline__ PagedSeq read_lane(const PagedSeq& s, int lane) {
+    return PagedSeq{__builtin_amdgcn_readlane(s.begin, lane), __builtin_amdgcn_readlane(s.count, lane),
+                    __builtin_amdgcn_readlane(s.len, lane)};
+}
+
+// Work is planned by every wave for itself, without barriers: a lane has some neighbouring sequences.
+struct LaneSeqs {
+    int each, b0, b1;
+    __device__ __forceinline__ explicit LaneSeqs(const PagedArgs& a) {
+        each = (a.batch + 63) / 64;
+        b0 = min((int)(threadIdx.x & 63) * each, a.batch);
+        b1 = min(b0 + each, a.batch);
     }
-    *all = __shfl((long long)in, 63, 64);
-    return in - v;
+};
+
+// Which stretch of a line a block takes: consecutive blocks go to the 8 XCDs in turn, and each XCD
+// takes one length of the line, whose neighbours read the same keys.
+__device__ __forceinline__ int line_block(uint32_t block) { return (int)(block % 8 * (kPgBlocks / 8) + block / 8); }
+
+// The quotient of numbers that mostly fit 32 bits.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {
+    return ((x | d) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
+}
+
+// ---- at most 16 or 32 rows: a block's waves take 32 keys each in turn
+
+constexpr int kPfKeys = kPgWaves * kCaKeys;  // keys of a part, one step of every wave
+
+// Parts of a sequence's keys for one KV head; one also where there are tokens but no keys.
+__device__ __forceinline__ int few_parts(const PagedSeq& s) {
+    return s.count > 0 ? max(1, (s.len + kPfKeys - 1) / kPfKeys) : 0;
+}
+
+// The line of all parts, sequence by sequence and head by head, cut into stretches, one a block: the
+// first `more` have one part more than the others.  No block of the first `blocks` is without work.
+struct FewLine {
+    int64_t all, blocks, each, more;
+    __device__ __forceinline__ FewLine(const PagedArgs& a, int64_t parts) {
+        all = parts * a.hkv;
+        blocks = min(all, (int64_t)kPgBlocks);
+        each = blocks > 0 ? quotient(all, blocks) : 0;
+        more = all - each * blocks;
+    }
+    __device__ __forceinline__ int64_t begin(int64_t block) const { return block * each + min(block, more); }
+    __device__ __forceinline__ int64_t block_of(int64_t x) const {
+        const int64_t y = x - more * (each + 1);
+        return y < 0 ? quotient(x, each + 1) : more + quotient(y, each);
+    }
+};
+
+// Parts (64 KB of K and V) from which on all that is read cannot stay in the caches until it is read
+// again: it is then read past them.  A step of 4.3 GB takes 637 us so and 715 through the caches, one of
+// 95 MB, read before, 34 and 30.5.
+constexpr int64_t kStreamParts = (192 << 20) / (kPfKeys * 4 * kD);
+
+// What a block leaves for the joining kernel: the head that its stretch began and did not end (b < 0:
+// none), and the block that ends it.
+struct FewRecord {
+    int b, head, last;
+};
+// The workspace of sequences walked so: records; then outputs and states of the heads that blocks
+// share, two slots of `rows` rows a block: a head begun in another block in slot 2 i, one that is not
+// ended in slot 2 i + 1.
+constexpr size_t kFewRecordBytes = (kPgBlocks * sizeof(FewRecord) + 255) / 256 * 256;
+struct FewSpace {
+    FewRecord* record;  // [kPgBlocks]
+    float* part;        // [2 kPgBlocks][rows][D]
+    float2* state;      // [2 kPgBlocks][rows]
+    char* end;
+    __device__ __forceinline__ FewSpace(const PagedArgs& a, int rows) {
+        char* p = static_cast<char*>(a.workspace);
+        record = reinterpret_cast<FewRecord*>(p);
+        part = reinterpret_cast<float*>(p + kFewRecordBytes);
+        state = reinterpret_cast<float2*>(part + (int64_t)2 * kPgBlocks * rows * kD);
+        end = reinterpret_cast<char*>(state + (int64_t)2 * kPgBlocks * rows);
+    }
+    static size_t bytes(int rows) { return kFewRecordBytes + (size_t)2 * kPgBlocks * rows * (kD + 2) * 4; }
+};
+
+constexpr int few_wave_lds(int rows) {
+    return kCaKeys * kD * 2 > ca_state_bytes(rows) ? kCaKeys * kD * 2 : ca_state_bytes(rows);
+}
+
+// The M = count g rows of one KV head over parts [part0, part1) of its keys.  lds(w): few_wave_lds(R)
+// bytes of wave w, 16-byte aligned.  Outputs where these are all parts, else states: row r's
+// outputs at part[r D], its reference and sum, negative where paged_odd_part has something to add,
+// at state[r].
+template <int R, int SHAPE, bool STREAM, class Lds>
+__device__ __forceinline__ void few_rows_attend(const PagedArgs& a, int b, const PagedSeq& seq, int head, int part0,
+                                                int part1, int parts, Lds&& lds, float* part,
+                                                float2* state) {
+    using Rows = ChunkRows<R>;
+    constexpr int kHalves = Rows::kHalves, kSteps = Rows::kSteps;
+    int tid = threadIdx.x;
+    asm("" : "+v"(tid));  // what follows from it is made here, not kept in registers for the next call
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    unsigned char* vt = lds(wave);
+    const int vrow = lane >> 4, vchunk = lane & 15;  // of a load or a store of 4 rows of V
+    const int M = seq.count * a.g, len = seq.len;
+    const int first = part0 * kPgWaves, last = min(part1 * kPgWaves, (len + kCaKeys - 1) / kCaKeys);
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    const int row = min(Rows::row(lane), M - 1), tok = row / a.g, qhead = head * a.g + row % a.g;
+    const int p = len - seq.count + tok;
+
+    // A step's pages, one key a lane (and lane + 32): entries of the table, then rows of K and V and
+    // which of them there are.  Keys behind the last repeat it, those without a page the first that
+    // has one (there or not, row 0 of the pages is memory).
+    auto key_row = [&](int st) { return min(st * kCaKeys + (lane & 31), len - 1); };
+    auto entry_of = [&](int st) { return page_entry(a, b, key_row(st)); };
+    struct Step {
+        u4v k[8], v[8];
+        uint32_t there;  // its keys that have pages
+    };
+    auto read = [](const u4v* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; };
+    int entry = 0;  // of this lane's key of the next step that is fetched
+    auto fetch = [&](int st, Step& s) __attribute__((always_inline)) {
+        const bool good = (uint32_t)entry < (uint32_t)a.n_pages;
+        s.there = (uint32_t)__ballot(good);
+        int at = good ? page_row(a, entry, head, key_row(st)) : 0;
+        if (__builtin_expect(s.there != ~0u, 0)) {
+            const int other = s.there ? __builtin_amdgcn_readlane(at, __builtin_ctz(s.there)) : 0;
+            at = good ? at : other;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = __builtin_amdgcn_ds_bpermute((4 * i + vrow) << 2, at);
+            s.v[i] = read(reinterpret_cast<const u4v*>(static_cast<const _Float16*>(a.V) + (int64_t)r * kD) + vchunk);
+        }
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+            const int r = __builtin_amdgcn_ds_bpermute(Rows::key(h, lane) << 2, at);
+            const _Float16* k = static_cast<const _Float16*>(a.K) + (int64_t)r * kD;
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c)
+                s.k[h * kSteps + c] = read(reinterpret_cast<const u4v*>(k + Rows::template dim<false>(c, lane)));
+        }
+        if (st + kPgWaves < last) entry = entry_of(st + kPgWaves);
+    };
+    int st = first + wave;
+    Step s;
+    if (st < last) {
+        entry = entry_of(st);
+        fetch(st, s);
+    }
+    const _Float16* qr = static_cast<const _Float16*>(a.q) + (int64_t)(seq.begin + tok) * a.q_stride + qhead * kD;
+    h8v qf[kSteps];
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c)
+        qf[c] = query_part(*reinterpret_cast<const u4v*>(qr + Rows::template dim<false>(c, lane)), flip);
+    const ScoreShape<SHAPE> shape(a, qhead);
+    Rows rows(SHAPE ? 1.f : score_factor(a.scale), lane);
+    bool odd = false;  // whether some V there had values that are not finite
+    for (; st < last; st += kPgWaves) {
+        const uint32_t w = bits_to(min(p, len - 1) - st * kCaKeys) & s.there;
+        wave_lds_order();  // the step before has read its V
+#pragma unroll
+        for (int i = 0; i < 8; ++i) put_v(vt, 4 * i + vrow, vchunk, as_h8(s.v[i]));
+        if (__builtin_expect(!__all(w == ~0u), 0)) {
+            uint32_t m = 0u;
+            wave_lds_order();
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) note_odd(reinterpret_cast<const u4v*>(vt)[64 * i + lane], m);
+            if (__any(m & kOddBits)) {
+                odd = true;
+                clean_v(vt, lane);
+            }
+        }
+        wave_lds_order();
+        rows.scores(qf, [&](int h, int c) { return as_h8(s.k[h * kSteps + c]); });
+        if (st + kPgWaves < last) fetch(st + kPgWaves, s);
+        if constexpr (SHAPE != kPlainScores) {
+            const float from = (float)(st * kCaKeys - p);
+            if constexpr (R == 16) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        rows.s[h][i] = shape(rows.s[h][i], from + (float)(16 * h + 4 * rows.lg + i));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    rows.s[i] = shape(rows.s[i], from + (float)(8 * (i / 4) + 4 * rows.half + i % 4));
+            }
+        }
+        rows.accumulate(w, vt, lane);
+    }
+
+    wave_lds_order();
+    rows.leave(vt, lane, odd);
+    __syncthreads();
+    // Joins the waves' states, 32 lanes a row, 4 dims a lane.
+    const float c2 = rows.c2;
+    const int d4 = tid & 31;
+    for (int r = tid >> 5; r < M; r += kPgThreads / 32) {
+        float top = -__builtin_huge_valf(), l = 0.f;
+        bool some = false;
+        f4v acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kPgWaves; ++w) {
+            const float* of = reinterpret_cast<const float*>(lds(w));
+            top = fmaxf(top, of[R * kCaRow + r]);
+            some |= __builtin_signbit(of[R * (kCaRow + 1) + r]);
+        }
+        if (top > -__builtin_huge_valf())
+#pragma unroll
+            for (int w = 0; w < kPgWaves; ++w) {
+                const float* of = reinterpret_cast<const float*>(lds(w));
+                const float c = rescale(of[R * kCaRow + r], top, c2);
+                l += c * __builtin_fabsf(of[R * (kCaRow + 1) + r]);
+                acc += c * *reinterpret_cast<const f4v*>(of + r * kCaRow + 4 * d4);
+            }
+        if (part0 == 0 && part1 == parts) {
+            acc *= l > 0.f ? 1.f / l : l;
+            if (some) acc += paged_odd_part(a, b, head, len - seq.count + r / a.g, len, d4);
+            static_cast<h4v*>(a.out)[((int64_t)(seq.begin + r / a.g) * a.hkv * a.g + head * a.g + r % a.g) * (kD / 4) + d4] =
+                h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
+        } else {
+            reinterpret_cast<f4v*>(part)[r * (kD / 4) + d4] = acc;
+            if (d4 == 0) state[r] = float2{top, some ? -l : l};
+        }
+    }
+}
+
+// The stretch of block id over the sequences that `pick` takes.
+template <int R, int SHAPE, class Pick, class Lds>
+__device__ __forceinline__ void few_stretch(const PagedArgs& a, int id, Pick&& pick, Lds&& lds) {
+    const FewSpace ws(a, R);
+    auto parts_of = [&](const PagedSeq& s) { return pick(s) ? few_parts(s) : 0; };
+    const LaneSeqs mine(a);
+    PagedSeq seq{};
+    int64_t sum = 0, all;
+    for (int b = mine.b0; b < mine.b1; ++b) {
+        seq = paged_seq(a, b);
+        sum += parts_of(seq);
+    }
+    const int64_t before = wave_sum_before(sum, &all);
+    FewRecord record{-1, 0, 0};
+    const FewLine line(a, all);
+    auto leave = [&]() {
+        if (threadIdx.x == 0) ws.record[id] = record;
+    };
+    if (id >= line.blocks) return leave();
+    int64_t x = line.begin(id);
+    const int64_t end = line.begin(id + 1);
+    const uint64_t who = __ballot(before * a.hkv <= x && x < (before + sum) * a.hkv);
+    if (who == 0) return leave();  // not with lengths that stay as they are
+    const int owner = (int)__builtin_ctzll(who);
+    int64_t at = before;
+    int b = mine.b0;
+    if (mine.each > 1 && (int)(threadIdx.x & 63) == owner)
+        for (; b < mine.b1 - 1; ++b) {
+            seq = paged_seq(a, b);
+            const int n = parts_of(seq);
+            if (x < (at + n) * a.hkv) break;
+            at += n;
+            seq = paged_seq(a, b + 1);
+        }
+    seq = read_lane(seq, owner);
+    b = __builtin_amdgcn_readlane(b, owner);
+    int parts = parts_of(seq);
+    if (parts == 0) return leave();  // as above
+    const int64_t skip = x - read_lane(at, owner) * a.hkv;
+    int head = __builtin_amdgcn_readfirstlane((int)quotient(skip, parts));
+    int part0 = __builtin_amdgcn_readfirstlane((int)(skip - (int64_t)head * parts));
+    int64_t slot = 2 * id;
+    for (;;) {
+        const int part1 = (int)min((int64_t)parts, part0 + (end - x));
+        if (part0 == 0) slot = 2 * id + 1;
+        if (part0 == 0 && part1 < parts) record = FewRecord{b, head, (int)line.block_of(x + parts - 1)};
+        auto attend = [&](auto stream) __attribute__((always_inline)) {
+            few_rows_attend<R, SHAPE, decltype(stream)::value>(a, b, seq, head, part0, part1, parts, lds,
+                                                               ws.part + slot * R * kD, ws.state + slot * R);
+        };
+        line.all > kStreamParts ? attend(std::true_type()) : attend(std::false_type());
+        x += part1 - part0;
+        part0 = 0;
+        if (x >= end) return leave();
+        __syncthreads();  // the states are read
+        if (++head == a.hkv) {
+            head = 0;
+            do {
+                if (++b >= a.batch) return leave();  // as above
+                seq = scalar_seq(a, b);
+                parts = parts_of(seq);
+            } while (parts == 0);
+        }
+    }
+}
+
+// Joins the states of row r of the head that block id began and did not end: 8 groups of 32 lanes take
+// every eighth block, 4 dims a lane.
+constexpr int kPjGroups = 8;
+__device__ __forceinline__ void few_join(const PagedArgs& a, int rows, float c2, int id, int r) {
+    __shared__ f4v so[kPjGroups][32];
+    __shared__ float sr[kPjGroups], sl[kPjGroups];
+    const FewSpace ws(a, rows);
+    const FewRecord rec = ws.record[id];
+    if (rec.b < 0) return;
+    const int b = rec.b, head = rec.head;
+    const PagedSeq seq = paged_seq(a, b);
+    if (r >= seq.count * a.g) return;
+    const int d4 = threadIdx.x & 31, sub = threadIdx.x >> 5;
+    bool odd = false;
+    float top = -__builtin_huge_valf(), l = 0.f;
+    f4v acc{0.f, 0.f, 0.f, 0.f};
+    for (int i = id + sub; i <= rec.last; i += kPjGroups) {
+        const int64_t at = (int64_t)(2 * i + (i == id ? 1 : 0)) * rows + r;
+        const float2 st = ws.state[at];
+        const f4v v = reinterpret_cast<const f4v*>(ws.part)[at * (kD / 4) + d4];
+        if (st.x == -__builtin_huge_valf()) continue;  // saw no key
+        odd |= __builtin_signbit(st.y);
+        const float to = fmaxf(top, st.x);
+        const float c0 = rescale(top, to, c2), c1 = rescale(st.x, to, c2);
+        l = l * c0 + __builtin_fabsf(st.y) * c1;
+        acc = acc * c0 + v * c1;
+        top = to;
+    }
+    so[sub][d4] = acc;
+    if (d4 == 0) {
+        sr[sub] = top;
+        sl[sub] = odd ? -l : l;
+    }
+    __syncthreads();
+    if (sub != 0) return;
+    top = -__builtin_huge_valf();
+    l = 0.f;
+    acc = f4v{0.f, 0.f, 0.f, 0.f};
+    odd = false;
+#pragma unroll
+    for (int i = 0; i < kPjGroups; ++i) {
+        top = fmaxf(top, sr[i]);
+        odd |= __builtin_signbit(sl[i]);
+    }
+    if (top > -__builtin_huge_valf())
+#pragma unroll
+        for (int i = 0; i < kPjGroups; ++i) {
+            const float c = rescale(sr[i], top, c2);
+            l += c * __builtin_fabsf(sl[i]);
+            acc += c * so[i][d4];
+        }
+    acc *= l > 0.f ? 1.f / l : l;
+    const int tok = r / a.g;
+    if (odd) acc += paged_odd_part(a, b, head, seq.len - seq.count + tok, seq.len, d4);
+    static_cast<h4v*>(a.out)[((int64_t)(seq.begin + tok) * a.hkv * a.g + head * a.g + r % a.g) * (kD / 4) + d4] =
+        h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
 }
 
 hipError_t launch_paged_prompt(const PagedArgs& a, hipStream_t s);

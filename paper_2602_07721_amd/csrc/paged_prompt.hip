@@ -15,10 +15,17 @@
 // computed on; a lane has looked up one of its keys' pages while the tile before was computed on, and
 // gets those of the rows that it loads by permutes.
 //
-// Where the rows are few or lengths differ, one block a tile of rows would leave the chip to the
-// longest sequence: keys are cut into shares of about a kPmShares-th of all the call's work each,
-// and a second kernel joins the shares' softmax states.  Each block finds its place from sums over
-// the lengths, so a captured call stays right when lengths change.
+// Sequences of at most 16 rows, single tokens mostly, are walked as paged_attend.hip does it instead, by
+// blocks of their own, the first: bound by HBM, they all run at once, and the tiles' blocks follow in the
+// place of those that are done.  Side by side with them from the start, tiles wait for their keys behind
+// the others' many loads: 5 us for 64 keys that take 1.3 otherwise.
+//
+// How the work is shared out, which every wave finds for itself from sums over the lengths, so a
+// captured call stays right when lengths change: where there is twice as much of it for each of the
+// blocks that the chip holds as the longest tile of rows has, a block takes a tile, the longest of a
+// sequence first.  Else the tiles, one behind the other, are cut into as many stretches of equal work
+// as the chip holds blocks, wherever the cuts fall, and a second kernel joins the softmax states of
+// the tiles that were cut (at most three halves of a tile a block more through memory). 
 
 #include <hip/hip_fp16.h>
 
@@ -29,181 +36,224 @@ namespace pariskv {
 namespace {
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
-typedef const __attribute__((address_space(1))) void* global_ptr;
 
-constexpr int kPmThreads = 256;
-constexpr int kPmRows = 128;  // rows of a block
-constexpr int kPmKeys = 64;   // keys of a tile
-constexpr int kPmShares = 1024;  // shares of about equal work that a call is cut into at least
-constexpr int kPmJoinRows = 8;   // rows of a joining block
+// 16 bytes a lane from memory straight into LDS, lane i's behind lane i - 1's.  The builtin for 64-bit
+// addresses makes the compiler wait for every LDS read at once as long as one is under way, where here
+// reads are waited for one by one (562 us for 605: 8192 tokens, 32 heads).  What it writes is seen after
+// loads_done() and a barrier; the compiler's own waits count it in as they are in order.
+__device__ __forceinline__ void load_lds(const void* from, void* to) {
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)to);
+    uint32_t m0;  // which the compiler takes for its own
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0)
+                 : "v"(from), "s"(lds)
+                 : "memory");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
-// How one sequence is cut: tiles of rows of a KV head, tiles of keys that the last of them sees, and
-// shares of the keys.
+constexpr int kPmRows = 128;    // rows of a tile
+constexpr int kPmKeys = 64;     // keys of a tile
+constexpr int kPmAhead = 4;     // operands read ahead
+constexpr int kPmFewRows = 16;  // rows of a sequence that is walked as few
+constexpr int kPmJoinRows = 8;  // rows of a joining block at a time
+
+struct FewRows {
+    int g;
+    __device__ __forceinline__ bool operator()(const PagedSeq& s) const { return s.count * g <= kPmFewRows; }
+};
+
+// How one sequence of more rows is cut: into tiles of rows of a KV head, which cost base + kPmRows (i +
+// 1), in units of a key times a query head, with what its first loads and its outputs take, as long as
+// 4 tiles of keys.
 struct PromptCut {
-    int tiles, keys, shares;
+    int tiles;
+    int64_t base;
+    __device__ __forceinline__ PromptCut(const PagedArgs& a, const PagedSeq& s) {
+        const int M = s.count * a.g;
+        tiles = M <= kPmFewRows ? 0 : (M + kPmRows - 1) / kPmRows;
+        base = (int64_t)max(s.len - s.count, 0) * a.g + 4 * kPmKeys * a.g;
+    }
+    // Cost of the tiles before tile i, of one KV head.
+    __device__ __forceinline__ int64_t cost(int64_t i) const { return i * base + kPmRows / 2 * i * (i + 1); }
 };
-__device__ __forceinline__ PromptCut prompt_cut(const PagedArgs& a, const PagedSeq& s) {
-    PromptCut c;
-    c.tiles = (s.count * a.g + kPmRows - 1) / kPmRows;
-    c.keys = s.count > 0 ? max(1, (s.len + kPmKeys - 1) / kPmKeys) : 0;
-    c.shares = 1;
-    return c;
+// Tiles of keys that the last row of a tile sees.
+__device__ __forceinline__ int tile_keys(const PagedArgs& a, const PagedSeq& s, int tile) {
+    const int last = s.len - s.count + (min((tile + 1) * kPmRows, s.count * a.g) - 1) / a.g;
+    return (max(last + 1, 0) + kPmKeys - 1) / kPmKeys;
 }
 
-// The workspace, for the joining kernel: for each sequence its shares, where the tiles of rows that
-// are cut begin (its and all before), and where their states do; then states and outputs.
-struct CutLine {
-    int64_t row;    // of its first state
-    int32_t tile;   // of its first cut tile of rows
-    int32_t shares;
-};
-struct PromptSpace {
-    CutLine* cuts;  // [batch + 1]
-    float2* state;  // [rows]
-    float* part;    // [rows][D]
-};
-// Rows of states: a sequence's M rows of hkv heads in S <= keys / cap + 1 shares, S > 1 only where
-// keys > cap, are at most 2 M hkv keys / cap, all together 2 * kPmRows * kPmShares; and a row of a KV
-// head has at most kPmShares + 1 shares.
-__host__ __device__ inline int64_t prompt_state_rows(const PagedArgs& a) {
-    const int64_t most = (int64_t)2 * kPmRows * kPmShares, few = (int64_t)a.t * a.g * a.hkv * (kPmShares / a.hkv + 2);
-    return few < most ? few : most;
-}
-__host__ __device__ inline size_t prompt_line_bytes(const PagedArgs& a) {
-    return (((size_t)a.batch + 1) * sizeof(CutLine) + 255) / 256 * 256;
-}
-__device__ __forceinline__ PromptSpace prompt_space(const PagedArgs& a) {
-    PromptSpace w;
-    char* p = static_cast<char*>(a.workspace);
-    w.cuts = reinterpret_cast<CutLine*>(p);
-    w.part = reinterpret_cast<float*>(p + prompt_line_bytes(a));
-    w.state = reinterpret_cast<float2*>(w.part + prompt_state_rows(a) * kD);
-    return w;
-}
-
-// What a block works on.
+// A place in the line of all tiles: before tile `key` of a tile's keys; b = batch: its end.
 struct PromptPlace {
-    int b, head, tile, share, shares;
-    int64_t row;  // of the sequence's first state
+    int b, head, tile, key;
 };
-
-// Sums of x over the threads before this one, and over all.
-__device__ __forceinline__ int64_t block_sum_before(int64_t x, int64_t* totals, int64_t* all) {
-    const int wave = threadIdx.x >> 6;
-    int64_t sum;
-    int64_t before = wave_sum_before(x, &sum);
-    if ((threadIdx.x & 63) == 0) totals[wave] = sum;
-    __syncthreads();
-    sum = 0;
-#pragma unroll
-    for (int w = 0; w < kPmThreads / 64; ++w) {
-        before += w < wave ? totals[w] : 0;
-        sum += totals[w];
-    }
-    *all = sum;
-    return before;
+__device__ __forceinline__ PromptPlace read_lane(const PromptPlace& p, int lane) {
+    return PromptPlace{__builtin_amdgcn_readlane(p.b, lane), __builtin_amdgcn_readlane(p.head, lane),
+                       __builtin_amdgcn_readlane(p.tile, lane), __builtin_amdgcn_readlane(p.key, lane)};
+}
+__device__ __forceinline__ bool operator<(const PromptPlace& x, const PromptPlace& y) {
+    if (x.b != y.b) return x.b < y.b;
+    if (x.head != y.head) return x.head < y.head;
+    if (x.tile != y.tile) return x.tile < y.tile;
+    return x.key < y.key;
+}
+// The place `cost` behind the beginning of sequence b.
+__device__ __forceinline__ PromptPlace prompt_place(const PagedArgs& a, int b, const PagedSeq& s, const PromptCut& c,
+                                                    int64_t cost) {
+    PromptPlace p;
+    p.b = b;
+    const int64_t per = c.cost(c.tiles);
+    p.head = (int)quotient(cost, per);
+    cost -= p.head * per;
+    // The last tile i whose tiles before cost no more: 64 i^2 + (base + 64) i = cost solved, then put right.
+    const double h = (double)(c.base + kPmRows / 2) / kPmRows;
+    int64_t i = (int64_t)(sqrt(h * h + (double)cost / (kPmRows / 2)) - h);
+    i = min(max(i, (int64_t)0), (int64_t)c.tiles - 1);
+    while (i > 0 && c.cost(i) > cost) --i;
+    while (i + 1 < c.tiles && c.cost(i + 1) <= cost) ++i;
+    p.tile = (int)i;
+    p.key = (int)quotient((cost - c.cost(i)) * tile_keys(a, s, p.tile), c.base + kPmRows * (i + 1));
+    return p;
 }
 
-// The block's place; false where there is none.
-__device__ __forceinline__ bool prompt_place(const PagedArgs& a, PromptPlace& pl) {
-    __shared__ int64_t totals[4][kPmThreads / 64];
-    __shared__ PromptPlace found;
-    const int tid = threadIdx.x;
-    const int each = (a.batch + kPmThreads - 1) / kPmThreads;
-    const int b0 = min(tid * each, a.batch), b1 = min(b0 + each, a.batch);
-    int64_t work = 0, all;
-    for (int b = b0; b < b1; ++b) {
-        const PromptCut c = prompt_cut(a, paged_seq(a, b));
-        work += (int64_t)c.tiles * c.keys;
+// What a block leaves for the joining kernel: the tile that its stretch began and did not end (b < 0:
+// none), and whether it begins in the middle of a tile, and ends that.
+enum { kMiddle = 1, kEnds = 2 };
+struct PromptRecord {
+    int b, head, tile;
+    int first;
+};
+// The workspace, behind that of the few rows: records, then outputs and states, two slots of kPmRows
+// rows a block: a tile begun in another block in slot 2 i, one that is not ended in slot 2 i + 1.
+constexpr size_t kPmRecordBytes = (kPgBlocks * sizeof(PromptRecord) + 255) / 256 * 256;
+struct PromptSpace {
+    PromptRecord* record;  // [kPgBlocks]
+    float* part;           // [2 kPgBlocks][kPmRows][D]
+    float2* state;         // [2 kPgBlocks][kPmRows]
+    __device__ __forceinline__ explicit PromptSpace(const PagedArgs& a) {
+        char* p = FewSpace(a, kPmFewRows).end;
+        record = reinterpret_cast<PromptRecord*>(p);
+        part = reinterpret_cast<float*>(p + kPmRecordBytes);
+        state = reinterpret_cast<float2*>(part + (int64_t)2 * kPgBlocks * kPmRows * kD);
     }
-    block_sum_before(work, totals[0], &all);
-    const int64_t cap = max((all * a.hkv + kPmShares - 1) / kPmShares, (int64_t)4);
-    auto cut = [&](int b, PagedSeq& s) {
+};
+
+// The stretch of a block, from one place up to another, and the sequence that it begins in.
+struct PromptStretch {
+    PromptPlace begin, end;
+    PagedSeq seq;
+};
+__device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint32_t block) {
+    const LaneSeqs mine(a);
+    const PromptPlace none{a.batch, 0, 0, 0};
+    PromptStretch out{none, none, PagedSeq{}};
+    int64_t work = 0, tokens = 0, items = 0, most = 0, all, all_tokens, all_items;
+    PagedSeq s{};
+    for (int b = mine.b0; b < mine.b1; ++b) {
         s = paged_seq(a, b);
-        PromptCut c = prompt_cut(a, s);
-        c.shares = c.keys > 0 ? (int)((c.keys + cap - 1) / cap) : 0;
-        return c;
-    };
-    int64_t items = 0, rows = 0, tiles = 0, all_items, all_rows, all_tiles;
-    PagedSeq s;
-    for (int b = b0; b < b1; ++b) {
-        const PromptCut c = cut(b, s);
-        items += (int64_t)c.tiles * c.shares * a.hkv;
-        if (c.shares > 1) {
-            rows += (int64_t)s.count * a.g * c.shares * a.hkv;
-            tiles += (int64_t)c.tiles * a.hkv;
-        }
+        const PromptCut c(a, s);
+        tokens += s.count;
+        if (c.tiles == 0) continue;
+        work += c.cost(c.tiles) * a.hkv;
+        items += (int64_t)c.tiles * a.hkv;
+        most = max(most, c.base + (int64_t)kPmRows * c.tiles);
     }
-    const int64_t first = block_sum_before(items, totals[1], &all_items);
-    int64_t at = first, row = block_sum_before(rows, totals[2], &all_rows);
-    int64_t tile = block_sum_before(tiles, totals[3], &all_tiles);
-    if (blockIdx.x == 0) {
-        const PromptSpace ws = prompt_space(a);
-        int64_t r = row, t = tile;
-        for (int b = b0; b < b1; ++b) {
-            const PromptCut c = cut(b, s);
-            ws.cuts[b] = CutLine{r, (int32_t)t, c.shares};
-            if (c.shares > 1) {
-                r += (int64_t)s.count * a.g * c.shares * a.hkv;
-                t += (int64_t)c.tiles * a.hkv;
-            }
-        }
-        if (tid == 0) ws.cuts[a.batch] = CutLine{all_rows, (int32_t)all_tiles, 0};
-    }
-    const int64_t id = blockIdx.x;
-    if (id >= all_items) return false;
-    if (first <= id && id < first + items) {
-        for (int b = b0;; ++b) {
-            const PromptCut c = cut(b, s);
-            const int64_t n = (int64_t)c.tiles * c.shares * a.hkv;
-            if (id < at + n) {
-                // Consecutive blocks go to the 8 XCDs in turn, and so do the KV heads: those that
-                // read the same keys share an L2.  The last tiles, which see the most keys, first.
-                const int in = (int)(id - at);
-                found.b = b;
-                found.head = in % a.hkv;
-                found.tile = c.tiles - 1 - in / a.hkv / c.shares;
-                found.share = in / a.hkv % c.shares;
-                found.shares = c.shares;
-                found.row = row;
-                break;
+    const int64_t before = wave_sum_before(work, &all);
+    const int64_t first_item = wave_sum_before(items, &all_items);
+    wave_sum_before(tokens, &all_tokens);
+    if (all == 0 || all_tokens > a.t) return out;  // offsets that do not rise
+    // A sequence of this lane's, found by what is before it.
+    PromptPlace place = none;
+    auto find = [&](int64_t x, int64_t at, auto&& size, auto&& there) {
+        for (int b = mine.b0; b < mine.b1; ++b) {
+            if (mine.each > 1) s = paged_seq(a, b);
+            const PromptCut c(a, s);
+            const int64_t n = size(c) * a.hkv;
+            if (x < at + n) {
+                place = there(b, c, x - at);
+                return;
             }
             at += n;
-            if (c.shares > 1) row += (int64_t)s.count * a.g * c.shares * a.hkv;
         }
+    };
+    const int64_t step = quotient(all, kPgBlocks), rest = all - step * kPgBlocks;
+    if (!__any(most > step / 2)) {
+        const int64_t id = block;
+        const uint64_t who = __ballot(first_item <= id && id < first_item + items);
+        if (who == 0) return out;
+        if (first_item <= id && id < first_item + items)
+            find(id, first_item, [&](const PromptCut& c) { return (int64_t)c.tiles; },
+                 [&](int b, const PromptCut& c, int64_t in) {
+                     // Consecutive blocks go to the 8 XCDs in turn, and so do the KV heads: those that
+                     // read the same keys share an L2.
+                     return PromptPlace{b, (int)in % a.hkv, c.tiles - 1 - (int)in / a.hkv, 0};
+                 });
+        const int owner = (int)__builtin_ctzll(who);
+        out.begin = out.end = read_lane(place, owner);
+        ++out.end.tile;
+        out.seq = read_lane(s, owner);
+        return out;
     }
-    __syncthreads();
-    pl = found;
-    return true;
+    if (block >= kPgBlocks) return out;
+#pragma unroll 1
+    for (int e = 1; e >= 0; --e) {
+        const int64_t id = line_block(block) + e, x = id * step + min(id, rest);
+        const uint64_t who = __ballot(before <= x && x < before + work);
+        if (who == 0) continue;  // the end of the line
+        if (before <= x && x < before + work)
+            find(x, before, [&](const PromptCut& c) { return c.cost(c.tiles); },
+                 [&](int b, const PromptCut& c, int64_t in) { return prompt_place(a, b, s, c, in); });
+        const int owner = (int)__builtin_ctzll(who);
+        (e ? out.end : out.begin) = read_lane(place, owner);
+        out.seq = read_lane(s, owner);
+    }
+    return out;
 }
 
 template <int SHAPE>
-__global__ __launch_bounds__(kPmThreads, 2) void paged_prompt_kernel(PagedArgs a) {
+__global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a) {
     // Arrays of their own, chosen at compile time: in one array the compiler cannot tell a read of
     // this tile from the loads under way to the next, and waits for them first.
     __shared__ u4v sk0[kPmKeys * 16], sk1[kPmKeys * 16], sv0[kPmKeys * 16], sv1[kPmKeys * 16];
+    static_assert(few_wave_lds(kPmFewRows) <= (int)sizeof sk0, "a wave's share of few rows takes one of them");
     __shared__ int again;  // whether a wave has outputs that are not finite
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (blockIdx.x < kPgBlocks) {
+        few_stretch<kPmFewRows, SHAPE>(a, line_block(blockIdx.x), FewRows{a.g}, [&](int w) {
+            return reinterpret_cast<unsigned char*>(w == 0 ? sk0 : w == 1 ? sk1 : w == 2 ? sv0 : sv1);
+        });
+        return;
+    }
+    const uint32_t block = blockIdx.x - kPgBlocks;
+    PromptStretch stretch = prompt_stretch(a, block);
+    PromptPlace place_now = stretch.begin;
+    PagedSeq seq = stretch.seq;
+    const PromptPlace end = stretch.end;
+    PromptRecord record{-1, 0, 0, 0};
+    const PromptSpace ws(a);
+    while (place_now < end) {
+    const int b = place_now.b, head = place_now.head;
+    const int keys = tile_keys(a, seq, place_now.tile);
+    const bool last_one = b == end.b && head == end.head && place_now.tile == end.tile;
+    const int tile0 = place_now.key, tile1 = last_one ? end.key : keys;
+    const bool whole = tile0 == 0 && tile1 == keys;
+    const int64_t slot = 2 * line_block(block) + (tile0 > 0 ? 0 : 1);
+    if (!whole) {
+        if (tile0 > 0) record.first = kMiddle | (tile1 == keys ? kEnds : 0);
+        else record = PromptRecord{b, head, place_now.tile, record.first};
+    }
+    int tid = threadIdx.x;
+    asm("" : "+v"(tid));  // what follows from it is made here, not kept in registers for the next tile
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
-
-    PromptPlace pl;
-    if (!prompt_place(a, pl)) return;  // the whole block
-    const int b = __builtin_amdgcn_readfirstlane(pl.b), head = __builtin_amdgcn_readfirstlane(pl.head);
-    const PagedSeq seq = paged_seq(a, b);
     const int M = seq.count * a.g, len = seq.len, start = len - seq.count;
-    const int row0 = pl.tile * kPmRows, row1 = min(row0 + kPmRows, M);
-    // Positions of the block's and of this wave's first and last rows.
-    const int first_p = start + row0 / a.g, last_p = start + (row1 - 1) / a.g;
+    const int row0 = place_now.tile * kPmRows, row1 = min(row0 + kPmRows, M);
+    // Positions of the tile's first row, and of this wave's last.
+    const int first_p = start + row0 / a.g;
     const int wave_row = row0 + 32 * wave;
     const bool idle = wave_row >= row1;  // a wave without rows
     const int wave_last = start + min(wave_row + 31, row1 - 1) / a.g;
     const int row = min(wave_row + col, row1 - 1), tok = row / a.g, qhead = head * a.g + row % a.g;
     const int p = start + tok;
-    // The tiles of keys that some row sees; this share's.
-    const int all_tiles = (max(last_p + 1, 0) + kPmKeys - 1) / kPmKeys;
-    const int tile0 = (int)((int64_t)all_tiles * pl.share / pl.shares);
-    const int tile1 = (int)((int64_t)all_tiles * (pl.share + 1) / pl.shares);
-    const int full = max(first_p + 1, 0) / kPmKeys;  // the tiles before it are whole for every row
+    const int full = max(first_p + 1, 0) / kPmKeys;  // the tiles of keys before it are whole for every row
 
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
     const ScoreShape<SHAPE> shape(a, qhead);
@@ -235,10 +285,8 @@ __global__ __launch_bounds__(kPmThreads, 2) void paged_prompt_kernel(PagedArgs a
         for (int i = 0; i < 4; ++i) {
             const int first = 16 * i + 4 * wave, key = first + (lane >> 4), c = lane & 15;
             const int64_t from = (int64_t)__builtin_amdgcn_ds_bpermute(key << 2, at) * 256;
-            __builtin_amdgcn_global_load_lds((global_ptr)(Kg + from + ((c ^ (key & 15)) << 4)),
-                                             (lds_ptr)(nk + first * 16), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((global_ptr)(Vg + from + ((c ^ (4 * (key & 3))) << 4)),
-                                             (lds_ptr)(nv + first * 16), 16, 0, 0);
+            load_lds(Kg + from + ((c ^ (key & 15)) << 4), nk + first * 16);
+            load_lds(Vg + from + ((c ^ (4 * (key & 3))) << 4), nv + first * 16);
         }
     };
     // Values of V that are not finite (see finite_part) matter where not every row sees every key.
@@ -282,17 +330,26 @@ __global__ __launch_bounds__(kPmThreads, 2) void paged_prompt_kernel(PagedArgs a
         }
         const int base_row = tile * kPmKeys;
         if (!idle && base_row <= wave_last) {
+            // Operands are read from LDS four instructions ahead of their use; left alone, the compiler
+            // reads each when it is needed.
             f16v s[2];
+            auto key_part = [&](int i) {  // of instruction i: dims 16 (i / 2) on, keys 32 (i % 2) on
+                return as_h8(ck[(32 * (i & 1) + col) * 16 + ((2 * (i >> 1) + half) ^ (col & 15))]);
+            };
+            h8v kf[kPmAhead];
+#pragma unroll
+            for (int i = 0; i < kPmAhead; ++i) kf[i] = key_part(i);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        as_h8(ck[(32 * h + col) * 16 + ((2 * c + half) ^ (col & 15))]), qf[c], s[h], 0, 0, 0);
+            for (int i = 0; i < 16; ++i) {
+                const h8v k = kf[i % kPmAhead];
+                __builtin_amdgcn_sched_barrier(0);
+                s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[i >> 1], s[i & 1], 0, 0, 0);
+                if (i + kPmAhead < 16) kf[i % kPmAhead] = key_part(i + kPmAhead);
+            }
             if constexpr (SHAPE != kPlainScores) {
                 const float from = (float)(base_row + 4 * half - p);
 #pragma unroll
@@ -338,6 +395,19 @@ __global__ __launch_bounds__(kPmThreads, 2) void paged_prompt_kernel(PagedArgs a
                 }
             }
             __builtin_amdgcn_s_setprio(1);  // ahead of another wave's S^T
+            // Values of instruction i: keys 16 (i / 4) on, dims 32 (i % 4) on.
+            auto value_part = [&](int i) {
+                // One offset from the array: longer chains lose which array it is.
+                const int at = tkey * 256 + (((4 * (i & 3) + tchunk) ^ (4 * (tkey & 3))) << 4) + (lane & 1) * 8 +
+                               16 * (i >> 2) * 256;
+                const char* vp = reinterpret_cast<const char*>(cv);
+                const s4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(vp + at));
+                const s4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(vp + (at + 8 * 256)));
+                return join_h4(a0, a1);
+            };
+            h8v vf[kPmAhead];
+#pragma unroll
+            for (int i = 0; i < kPmAhead; ++i) vf[i] = value_part(i);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 h8v pf[2];
@@ -352,21 +422,17 @@ __global__ __launch_bounds__(kPmThreads, 2) void paged_prompt_kernel(PagedArgs a
                     pf[i / 8][i % 8 + 1] = e[1];
                 }
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        // One offset from the array: longer chains lose which array it is.
-                        const int at = tkey * 256 + (((4 * d + tchunk) ^ (4 * (tkey & 3))) << 4) + (lane & 1) * 8 +
-                                       16 * (2 * h + k) * 256;
-                        const char* vp = reinterpret_cast<const char*>(cv);
-                        const s4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(vp + at));
-                        const s4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v)(vp + (at + 8 * 256)));
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(join_h4(a0, a1), pf[k], o[d], 0, 0, 0);
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const int i = 8 * h + j, d = j & 3;
+                    const h8v v = vf[i % kPmAhead];
+                    __builtin_amdgcn_sched_barrier(1);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[j >> 2], o[d], 0, 0, 0);
+                    if (i + kPmAhead < 16) vf[i % kPmAhead] = value_part(i + kPmAhead);
                 }
             }
         }
         __builtin_amdgcn_s_setprio(0);
+        loads_done();
         if (careful && tile + 1 < tile1) clean(tile + 1, next, nv);
         __syncthreads();  // and the next tile is there
         there = next;
@@ -382,6 +448,7 @@ __global__ __launch_bounds__(kPmThreads, 2) void paged_prompt_kernel(PagedArgs a
         if (tile0 < tile1) {
             load(place(tile0, entry_of(tile0), there), sk0, sv0);
             if (tile0 + 1 < tile1) entry = entry_of(tile0 + 1);
+            loads_done();
             clean(tile0, there, sv0);
         }
         __syncthreads();
@@ -423,88 +490,121 @@ __global__ __launch_bounds__(kPmThreads, 2) void paged_prompt_kernel(PagedArgs a
 
     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     const float l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-    if (wave_row + col >= row1) return;
-    if (pl.shares == 1) {
-        const float inv = l > 0.f ? 1.f / l : l;
-        h4v* out = static_cast<h4v*>(a.out) + ((int64_t)(seq.begin + tok) * a.hkv * a.g + qhead) * (kD / 4);
+    if (wave_row + col < row1) {
+        if (whole) {
+            const float inv = l > 0.f ? 1.f / l : l;
+            h4v* out = static_cast<h4v*>(a.out) + ((int64_t)(seq.begin + tok) * a.hkv * a.g + qhead) * (kD / 4);
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                out[8 * d + 2 * (i / 4) + half] =
-                    h4v{(_Float16)(o[d][i] * inv), (_Float16)(o[d][i + 1] * inv), (_Float16)(o[d][i + 2] * inv),
-                        (_Float16)(o[d][i + 3] * inv)};
-    } else {
-        const PromptSpace ws = prompt_space(a);
-        const int64_t at = pl.row + ((int64_t)head * pl.shares + pl.share) * M + row;
-        if (at >= prompt_state_rows(a)) return;  // offsets that do not rise
-        const float fix = at_r(r, nm, c2);
-        f4v* out = reinterpret_cast<f4v*>(ws.part) + at * (kD / 4);
+                for (int i = 0; i < 16; i += 4)
+                    out[8 * d + 2 * (i / 4) + half] =
+                        h4v{(_Float16)(o[d][i] * inv), (_Float16)(o[d][i + 1] * inv), (_Float16)(o[d][i + 2] * inv),
+                            (_Float16)(o[d][i + 3] * inv)};
+        } else {
+            const float fix = at_r(r, nm, c2);
+            f4v* out = reinterpret_cast<f4v*>(ws.part) + (slot * kPmRows + row - row0) * (kD / 4);
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                out[8 * d + 2 * (i / 4) + half] = f4v{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * fix;
-        if (half == 0) ws.state[at] = float2{left_r(r, l), l * fix};
+                for (int i = 0; i < 16; i += 4)
+                    out[8 * d + 2 * (i / 4) + half] = f4v{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * fix;
+            if (half == 0) ws.state[slot * kPmRows + row - row0] = float2{left_r(r, l), l * fix};
+        }
+    }
+    if (last_one) break;
+    place_now.key = 0;
+    const PromptCut cut(a, seq);
+    if (++place_now.tile == cut.tiles) {
+        place_now.tile = 0;
+        if (++place_now.head == a.hkv) {
+            place_now.head = 0;
+            do {
+                if (++place_now.b >= a.batch) break;
+                seq = scalar_seq(a, place_now.b);
+            } while (PromptCut(a, seq).tiles == 0);
+        }
+    }
+    __syncthreads();  // LDS is read
+    }
+    if (block < kPgBlocks && threadIdx.x == 0) ws.record[line_block(block)] = record;
+}
+
+// Joins the states of the tile that block id of the line began and did not end: 32 lanes a row, 4 dims
+// a lane, a quarter of the tile a block.
+constexpr int kPmJoinBlocks = 4;
+__device__ __forceinline__ void tile_join(const PagedArgs& a, int shaped, int id, int quarter) {
+    const PromptSpace ws(a);
+    const int lane = threadIdx.x & 63;
+    const PromptRecord rec = ws.record[id];
+    if (rec.b < 0) return;
+    // The block that ends the tile: the first behind with that mark.
+    int last = id;
+    for (int i = id + 1; i < kPgBlocks; i += 64) {
+        const uint64_t ends = __ballot(i + lane < kPgBlocks && (ws.record[min(i + lane, kPgBlocks - 1)].first & kEnds));
+        if (ends) {
+            last = i + (int)__builtin_ctzll(ends);
+            break;
+        }
+    }
+    const PagedSeq seq = paged_seq(a, rec.b);
+    const int d4 = threadIdx.x & 31;
+    const float c2 = shaped ? 1.f : score_factor(a.scale);
+    auto slot_of = [&](int i) -> int64_t {
+        return i == id ? 2 * i + 1 : (ws.record[i].first & kMiddle) ? 2 * i : -1;
+    };
+    for (int j = 0; j < kPmRows / kPmJoinBlocks / kPmJoinRows; ++j) {
+        const int row = (quarter * (kPmRows / kPmJoinBlocks / kPmJoinRows) + j) * kPmJoinRows +
+                        (int)(threadIdx.x >> 5);
+        const int at = rec.tile * kPmRows + row;
+        if (at >= seq.count * a.g) return;
+        float top = -__builtin_huge_valf(), l = 0.f;
+        for (int i = id; i <= last; ++i) {
+            const int64_t slot = slot_of(i);
+            if (slot >= 0) top = fmaxf(top, ws.state[slot * kPmRows + row].x);
+        }
+        f4v acc{0.f, 0.f, 0.f, 0.f};
+        for (int i = id; i <= last; ++i) {
+            const int64_t slot = slot_of(i);
+            if (slot < 0) continue;
+            const float2 st = ws.state[slot * kPmRows + row];
+            // A share that saw no key that counts left zeros, or values that are not finite.
+            const float c = st.x == -__builtin_huge_valf() ? 1.f : rescale(st.x, top, c2);
+            l += c * st.y;
+            acc += c * reinterpret_cast<const f4v*>(ws.part)[(slot * kPmRows + row) * (kD / 4) + d4];
+        }
+        acc *= l > 0.f ? 1.f / l : l;
+        static_cast<h4v*>(a.out)[((int64_t)(seq.begin + at / a.g) * a.hkv * a.g + rec.head * a.g + at % a.g) * (kD / 4) + d4] =
+            h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
     }
 }
 
-// Joins the shares' states, 32 lanes a row, 4 dims a lane: a block takes 8 rows of a cut tile.
-__global__ __launch_bounds__(32 * kPmJoinRows) void paged_prompt_join_kernel(PagedArgs a, int shaped) {
-    constexpr int kBlocks = kPmRows / kPmJoinRows;
-    const PromptSpace ws = prompt_space(a);
-    const int id = (int)(blockIdx.x / kBlocks);
-    if (id >= ws.cuts[a.batch].tile) return;
-    int lo = 0, hi = a.batch;  // the last sequence whose first cut tile is not behind it
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (ws.cuts[mid].tile <= id) lo = mid;
-        else hi = mid;
-    }
-    const CutLine cut = ws.cuts[lo];
-    const PagedSeq seq = paged_seq(a, lo);
-    const int M = seq.count * a.g, in = id - cut.tile, head = in % a.hkv;
-    if (in < 0) return;
-    const int row = in / a.hkv * kPmRows + (int)(blockIdx.x % kBlocks) * kPmJoinRows + (int)(threadIdx.x >> 5);
-    if (row >= M) return;
-    const int d4 = threadIdx.x & 31;
-    const float c2 = shaped ? 1.f : score_factor(a.scale);
-    const int64_t at = cut.row + (int64_t)head * cut.shares * M + row;
-    if (at + (int64_t)(cut.shares - 1) * M >= prompt_state_rows(a)) return;  // as above
-    float top = -__builtin_huge_valf(), l = 0.f;
-    f4v acc{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < cut.shares; ++s) {
-        const float2 st = ws.state[at + (int64_t)s * M];
-        const f4v v = reinterpret_cast<const f4v*>(ws.part)[(at + (int64_t)s * M) * (kD / 4) + d4];
-        if (st.x == -__builtin_huge_valf()) {  // saw no key that counts: zeros, or values that are not finite
-            acc += v;
-            continue;
-        }
-        const float to = fmaxf(top, st.x);
-        const float c0 = rescale(top, to, c2), c1 = rescale(st.x, to, c2);
-        l = l * c0 + st.y * c1;
-        acc = acc * c0 + v * c1;
-        top = to;
-    }
-    acc *= l > 0.f ? 1.f / l : l;
-    static_cast<h4v*>(a.out)[((int64_t)(seq.begin + row / a.g) * a.hkv * a.g + head * a.g + row % a.g) * (kD / 4) + d4] =
-        h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
+// Both joins in one launch: a block for every quarter of a tile that may be cut, then one for every row
+// of the sequences of few.
+__global__ __launch_bounds__(32 * kPjGroups) void paged_prompt_join_kernel(PagedArgs a, int shaped) {
+    static_assert(kPjGroups == kPmJoinRows, "blocks of both take as many threads");
+    const int id = (int)blockIdx.x - kPgBlocks * kPmJoinBlocks;
+    if (id < 0)
+        tile_join(a, shaped, (int)blockIdx.x / kPmJoinBlocks, (int)blockIdx.x % kPmJoinBlocks);
+    else
+        few_join(a, kPmFewRows, shaped ? 1.f : score_factor(a.scale), id / kPmFewRows, id % kPmFewRows);
 }
 
 }  // namespace
 
 size_t paged_prompt_bytes(const PagedArgs& a) {
-    return prompt_line_bytes(a) + (size_t)prompt_state_rows(a) * (kD + 2) * 4;
+    return FewSpace::bytes(kPmFewRows) + kPmRecordBytes + (size_t)2 * kPgBlocks * kPmRows * (kD + 2) * 4;
 }
 
 hipError_t launch_paged_prompt(const PagedArgs& a, hipStream_t s) {
     const int shape = (a.cap > 0.f ? kCappedScores : 0) | (a.slopes ? kBiasedScores : 0);
-    // At most so many tiles of rows, and shares beyond one a tile.
+    // At most so many tiles of rows.
     const int64_t some = a.batch < a.t ? a.batch : a.t;
     const int64_t tiles = ((int64_t)a.t * a.g / kPmRows + some) * a.hkv;
     ProfEvents pe = prof_begin("paged_attend");
     auto go = [&](auto kernel) {
-        hipExtLaunchKernelGGL(kernel, dim3((unsigned)(tiles + kPmShares)), dim3(kPmThreads), 0, s, pe.start, pe.stop, 0, a);
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)(kPgBlocks + (tiles > kPgBlocks ? tiles : kPgBlocks))), dim3(kPgThreads), 0, s,
+                              pe.start, pe.stop, 0, a);
     };
     if (shape == kPlainScores) go(paged_prompt_kernel<0>);
     else if (shape == kCappedScores) go(paged_prompt_kernel<1>);
@@ -512,10 +612,9 @@ hipError_t launch_paged_prompt(const PagedArgs& a, hipStream_t s) {
     else go(paged_prompt_kernel<3>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t cut = tiles < kPmShares ? tiles : kPmShares;
     pe = prof_begin("paged_join");
-    hipExtLaunchKernelGGL(paged_prompt_join_kernel, dim3((unsigned)(cut * (kPmRows / kPmJoinRows))),
-                          dim3(32 * kPmJoinRows), 0, s, pe.start, pe.stop, 0, a, shape);
+    hipExtLaunchKernelGGL(paged_prompt_join_kernel, dim3(kPgBlocks * (kPmJoinBlocks + kPmFewRows)), dim3(32 * kPjGroups), 0,
+                          s, pe.start, pe.stop, 0, a, shape);
     return hipGetLastError();
 }
 
