@@ -531,51 +531,68 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
 }
 
 // Joins the states of the tile that block id of the line began and did not end: 32 lanes a row, 4 dims
-// a lane, a quarter of the tile a block.
-constexpr int kPmJoinBlocks = 4;
+// a lane, 4 rows at a time, a quarter of the tile a block.
+constexpr int kPmJoinBlocks = 4, kPmJoinTurns = kPmRows / kPmJoinBlocks / kPmJoinRows;
 __device__ __forceinline__ void tile_join(const PagedArgs& a, int shaped, int id, int quarter) {
+    __shared__ int slots[kPgBlocks];
     const PromptSpace ws(a);
-    const int lane = threadIdx.x & 63;
+    const int tid = threadIdx.x;
     const PromptRecord rec = ws.record[id];
     if (rec.b < 0) return;
-    // The block that ends the tile: the first behind with that mark.
-    int last = id;
-    for (int i = id + 1; i < kPgBlocks; i += 64) {
-        const uint64_t ends = __ballot(i + lane < kPgBlocks && (ws.record[min(i + lane, kPgBlocks - 1)].first & kEnds));
-        if (ends) {
-            last = i + (int)__builtin_ctzll(ends);
-            break;
+    // The block that ends the tile is the first behind with that mark; each between, and it, may have a state.
+    int states = 1;
+    if (tid == 0) slots[0] = 2 * id + 1;
+    for (int i = id + 1; i < kPgBlocks; i += 64) {  // every wave alike
+        const int at = i + (tid & 63), first = at < kPgBlocks ? ws.record[at].first : 0;
+        const uint64_t ends = __ballot(first & kEnds);
+        const uint64_t mine = __ballot(first & kMiddle) & (ends ? (2ull << __builtin_ctzll(ends)) - 1 : ~0ull);
+        if (mine >> (tid & 63) & 1) slots[states + __builtin_popcountll(mine & ((1ull << (tid & 63)) - 1))] = 2 * at;
+        states += __builtin_popcountll(mine);
+        if (ends) break;
+    }
+    __syncthreads();
+    const PagedSeq seq = paged_seq(a, rec.b);
+    const int d4 = tid & 31, M = seq.count * a.g;
+    const int row0 = quarter * kPmJoinTurns * kPmJoinRows + (tid >> 5);  // then every kPmJoinRows-th
+    const float c2 = shaped ? 1.f : score_factor(a.scale);
+    float top[kPmJoinTurns], l[kPmJoinTurns];
+    f4v acc[kPmJoinTurns];
+#pragma unroll
+    for (int j = 0; j < kPmJoinTurns; ++j) {
+        top[j] = -__builtin_huge_valf();
+        l[j] = 0.f;
+        acc[j] = f4v{0.f, 0.f, 0.f, 0.f};
+    }
+    // Rows behind the last hold what was there; they are not written.
+    for (int i = 0; i < states; ++i) {
+        float2 st[kPmJoinTurns];
+        f4v v[kPmJoinTurns];
+#pragma unroll
+        for (int j = 0; j < kPmJoinTurns; ++j) {
+            const int64_t at = (int64_t)slots[i] * kPmRows + row0 + j * kPmJoinRows;
+            st[j] = ws.state[at];
+            v[j] = reinterpret_cast<const f4v*>(ws.part)[at * (kD / 4) + d4];
+        }
+#pragma unroll
+        for (int j = 0; j < kPmJoinTurns; ++j) {
+            if (st[j].x == -__builtin_huge_valf()) {  // saw no key that counts: zeros, or values that are not finite
+                acc[j] += v[j];
+                continue;
+            }
+            const float to = fmaxf(top[j], st[j].x);
+            const float c0 = rescale(top[j], to, c2), c1 = rescale(st[j].x, to, c2);
+            l[j] = l[j] * c0 + st[j].y * c1;
+            acc[j] = acc[j] * c0 + v[j] * c1;
+            top[j] = to;
         }
     }
-    const PagedSeq seq = paged_seq(a, rec.b);
-    const int d4 = threadIdx.x & 31;
-    const float c2 = shaped ? 1.f : score_factor(a.scale);
-    auto slot_of = [&](int i) -> int64_t {
-        return i == id ? 2 * i + 1 : (ws.record[i].first & kMiddle) ? 2 * i : -1;
-    };
-    for (int j = 0; j < kPmRows / kPmJoinBlocks / kPmJoinRows; ++j) {
-        const int row = (quarter * (kPmRows / kPmJoinBlocks / kPmJoinRows) + j) * kPmJoinRows +
-                        (int)(threadIdx.x >> 5);
-        const int at = rec.tile * kPmRows + row;
-        if (at >= seq.count * a.g) return;
-        float top = -__builtin_huge_valf(), l = 0.f;
-        for (int i = id; i <= last; ++i) {
-            const int64_t slot = slot_of(i);
-            if (slot >= 0) top = fmaxf(top, ws.state[slot * kPmRows + row].x);
-        }
-        f4v acc{0.f, 0.f, 0.f, 0.f};
-        for (int i = id; i <= last; ++i) {
-            const int64_t slot = slot_of(i);
-            if (slot < 0) continue;
-            const float2 st = ws.state[slot * kPmRows + row];
-            // A share that saw no key that counts left zeros, or values that are not finite.
-            const float c = st.x == -__builtin_huge_valf() ? 1.f : rescale(st.x, top, c2);
-            l += c * st.y;
-            acc += c * reinterpret_cast<const f4v*>(ws.part)[(slot * kPmRows + row) * (kD / 4) + d4];
-        }
-        acc *= l > 0.f ? 1.f / l : l;
+#pragma unroll
+    for (int j = 0; j < kPmJoinTurns; ++j) {
+        const int at = rec.tile * kPmRows + row0 + j * kPmJoinRows;
+        if (at >= M) break;
+        const f4v o = acc[j] * (l[j] > 0.f ? 1.f / l[j] : l[j]);
         static_cast<h4v*>(a.out)[((int64_t)(seq.begin + at / a.g) * a.hkv * a.g + rec.head * a.g + at % a.g) * (kD / 4) + d4] =
-            h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
+            h4v{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
     }
 }
 
