@@ -885,6 +885,30 @@ def sink_window_attend(cfg, q, K, V, pos, sink, window, scale, starts=None, coun
 # ---- paged K/V cache
 
 
+def _tensors(specs):
+    """Pointers of tensor arguments (tensor, name, dtype, shape, whether it may be None), checked as _arg does, with the
+    tensors' devices: for calls that a decode step makes, where a microsecond shows."""
+    Tensor = _torch().Tensor
+    ptrs, devices = [], set()
+    for t, name, dtype, shape, optional in specs:
+        if not (isinstance(t, Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous()):
+            _arg(t, name, dtype, shape, optional=optional)  # raises, or there is none
+            ptrs.append(None)
+            continue
+        devices.add(t.get_device())
+        ptrs.append(t.data_ptr())
+    return ptrs, devices
+
+
+def _require_on(devices, specs, stream):
+    """What _require_device and _require_here say of tensors on these devices."""
+    if -1 in devices:
+        _require_device([(t, name) for t, name, *_ in specs if t is not None and not t.is_cuda])
+    here = _torch().cuda.current_device()
+    if devices != {here} or stream is not None:
+        _require_here(stream, *(t for t, *_ in specs))
+
+
 class PagedCache:
     """A pool of pages (see ``pariskv_pages``): K, V [n_pages][Hkv][page_size][D] float16 on the GPU."""
 
@@ -905,14 +929,17 @@ class PagedCache:
     def page_size(self):
         return int(self.K.shape[2])
 
-    def c(self, cfg, dev):
-        half = _torch().float16
-        shape = (self.K.shape[0] if isinstance(self.K, _torch().Tensor) and self.K.dim() == 4 else None, cfg.n_kv_heads,
-                 _rows(self.K), HEAD_DIM)
-        kp = _arg(self.K, "cache.K", half, shape, dev)
-        vp = _arg(self.V, "cache.V", half, tuple(self.K.shape), dev)
-        self._c = _Pages(kp, vp, self.K.shape[0], self.K.shape[2])
-        return ctypes.byref(self._c)
+
+def _pages_specs(cfg, cache):
+    """The specs of a cache's tensors, its pages and their size."""
+    if not isinstance(cache, PagedCache):
+        raise TypeError("cache must be a PagedCache")
+    half, K = _torch().float16, cache.K
+    if not isinstance(K, _torch().Tensor) or K.dim() != 4:
+        raise ValueError("cache.K must be a [n_pages][Hkv][page_size][D] float16 tensor")
+    pages, _, size, _ = K.shape
+    shape = (pages, cfg.n_kv_heads, size, HEAD_DIM)
+    return (K, "cache.K", half, shape, False), (cache.V, "cache.V", half, shape, False), pages, size
 
 
 class PagePlan:
@@ -934,14 +961,11 @@ def plan_pages(table, free, n_free, lens, counts, page_size, t=None, plan=None, 
     int32 on the GPU.  t: entries of slots and positions (without a plan).  A plan's lens and n_free may be lens and n_free
     themselves, its counts counts.  Returns the plan."""
     torch = _torch()
-    dev, i32 = [], _torch().int32
-    for x, nm, dims in ((table, "table", 2), (free, "free", 1)):
+    i32 = torch.int32
+    for x, nm, dims in ((table, "table [batch][width]", 2), (free, "free [n_pages]", 1)):
         if not isinstance(x, torch.Tensor) or x.dim() != dims:
-            raise ValueError(f"{nm} must be a{' [batch][width]' if dims == 2 else ' [n_pages]'} int32 tensor")
-    batch = int(table.shape[0])
-    tp, fp = _arg(table, "table", i32, tuple(table.shape), dev), _arg(free, "free", i32, tuple(free.shape), dev)
-    np_, lp = _arg(n_free, "n_free", i32, (1,), dev), _arg(lens, "lens", i32, (batch,), dev)
-    cp = _arg(counts, "counts", i32, (batch,), dev)
+            raise ValueError(f"{nm} must be an int32 tensor")
+    batch, width = table.shape
     if plan is None:
         if t is None:
             raise ValueError("t is required without a plan")
@@ -950,39 +974,43 @@ def plan_pages(table, free, n_free, lens, counts, page_size, t=None, plan=None, 
         raise TypeError("plan must be a PagePlan")
     if not isinstance(plan.slots, torch.Tensor) or plan.slots.dim() != 1:
         raise ValueError("plan.slots must be a [t] int32 tensor")
-    n = int(plan.slots.shape[0])
+    n = plan.slots.shape[0]
     if t is not None and int(t) != n:
         raise ValueError(f"t is {t}, but the plan has {n} slots")
-    outs = [_arg(getattr(plan, k), f"plan.{k}", i32, (m,), dev) for k, m in
-            (("lens", batch), ("n_free", 1), ("offsets", batch + 1), ("counts", batch), ("slots", n), ("positions", n))]
-    _require_device(dev)
-    _require_here(stream, table, free, n_free, lens, counts, plan.lens, plan.n_free, plan.offsets, plan.counts, plan.slots,
-                  plan.positions)
-    step = _PageStep(tp, table.shape[1], fp, free.shape[0], int(page_size), np_, lp, cp, batch, n, *outs)
+    one, each = (1,), (batch,)
+    specs = ((table, "table", i32, (batch, width), False), (free, "free", i32, free.shape, False),
+             (n_free, "n_free", i32, one, False), (lens, "lens", i32, each, False), (counts, "counts", i32, each, False),
+             (plan.lens, "plan.lens", i32, each, False), (plan.n_free, "plan.n_free", i32, one, False),
+             (plan.offsets, "plan.offsets", i32, (batch + 1,), False), (plan.counts, "plan.counts", i32, each, False),
+             (plan.slots, "plan.slots", i32, (n,), False), (plan.positions, "plan.positions", i32, (n,), False))
+    (tp, fp, np_, lp, cp, *outs), devices = _tensors(specs)
+    _require_on(devices, specs, stream)
+    step = _PageStep(tp, width, fp, free.shape[0], int(page_size), np_, lp, cp, batch, n, *outs)
     _check(lib().pariskv_plan_pages(ctypes.byref(step), _stream(stream)))
     return plan
 
 
-def _token_rows(x, name, heads, dev, t=None):
-    """(pointer, tokens, values from one token to the next) of [t][heads][D] float16, a token's heads next to each other:
-    a contiguous tensor or columns of a wider one."""
+def _token_rows(x, name, heads, t=None):
+    """(pointer, values from one token to the next) of [t][heads][D] float16, a token's heads next to each other: a
+    contiguous tensor or columns of a wider one."""
     torch = _torch()
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
         raise ValueError(f"{name} must be a [t][heads][D] float16 tensor")
-    if x.dtype != torch.float16:
+    if x.dtype is not torch.float16:
         raise TypeError(f"{name} must be {torch.float16}, got {x.dtype}")
-    n = int(x.shape[0])
-    if x.shape[1] != heads or x.shape[2] != HEAD_DIM or (t is not None and n != t):
-        raise ValueError(f"{name} must have shape [{'*' if t is None else t}, {heads}, {HEAD_DIM}], got {list(x.shape)}")
-    s = x.stride()
-    if n > 0 and (s[2] != 1 or (heads > 1 and s[1] != HEAD_DIM)):
+    if t is None:
+        t = x.shape[0]
+    if x.shape != (t, heads, HEAD_DIM):
+        raise ValueError(f"{name} must have shape [{t}, {heads}, {HEAD_DIM}], got {list(x.shape)}")
+    step, head, dim = x.stride()
+    if t > 0 and (dim != 1 or (heads > 1 and head != HEAD_DIM)):
         raise ValueError(f"{name} must have its heads next to each other")
-    if not x.is_cuda:
-        dev.append((x, name))
-    step = s[0] if n > 1 else heads * HEAD_DIM
-    if step < heads * HEAD_DIM or step % 8 or x.data_ptr() % 16:
+    if t < 2:
+        step = heads * HEAD_DIM
+    ptr = x.data_ptr()
+    if step < heads * HEAD_DIM or step % 8 or ptr % 16:
         raise ValueError(f"{name} must have its tokens a multiple of 8 values apart, at 16-byte addresses")
-    return x.data_ptr(), n, step
+    return ptr, step
 
 
 def rotate_rows(cfg, cache, q, k, v, positions, slots, freqs=None, q_weight=None, k_weight=None, eps=1e-6, pairs=False,
@@ -992,33 +1020,32 @@ def rotate_rows(cfg, cache, q, k, v, positions, slots, freqs=None, q_weight=None
     and values v [t][Hkv][D] written to the slots of a PagedCache.  positions, slots int32 [t]; tokens whose slot lies outside
     the pages are left alone.  q, k and v may be columns of one tensor.  Returns q_out [t][Hq][D] float16."""
     torch = _torch()
-    dev, i32, f32 = [], _torch().int32, _torch().float32
-    if not isinstance(cache, PagedCache):
-        raise TypeError("cache must be a PagedCache")
-    qp, t, qs = _token_rows(q, "q", cfg.n_q_heads, dev)
-    kp, _, ks = _token_rows(k, "k", cfg.n_kv_heads, dev, t)
-    vp, _, vs = _token_rows(v, "v", cfg.n_kv_heads, dev, t)
-    cp = cache.c(cfg, dev)
-    pp, sp = _arg(positions, "positions", i32, (t,), dev), _arg(slots, "slots", i32, (t,), dev)
+    i32, f32 = torch.int32, torch.float32
+    K, V, n_pages, size = _pages_specs(cfg, cache)
+    qp, qs = _token_rows(q, "q", cfg.n_q_heads)
+    t = q.shape[0]
+    kp, ks = _token_rows(k, "k", cfg.n_kv_heads, t)
+    vp, vs = _token_rows(v, "v", cfg.n_kv_heads, t)
     if freqs is not None and (not isinstance(freqs, torch.Tensor) or freqs.dim() != 1):
         raise ValueError("freqs must be a [rot_dim / 2] float32 tensor")
-    rot = 0 if freqs is None else 2 * int(freqs.shape[0])
-    fp = _arg(freqs, "freqs", f32, (rot // 2,), dev, optional=True)
-    qw = _arg(q_weight, "q_weight", f32, (HEAD_DIM,), dev, optional=True)
-    kw = _arg(k_weight, "k_weight", f32, (HEAD_DIM,), dev, optional=True)
+    half = 0 if freqs is None else freqs.shape[0]
     if q_out is None:
         q_out = _new((t, cfg.n_q_heads, HEAD_DIM), torch.float16, q.device, stream)
-    op = _arg(q_out, "q_out", torch.float16, (t, cfg.n_q_heads, HEAD_DIM), dev)
-    _require_device(dev)
-    _require_here(stream, q, k, v, cache.K, cache.V, positions, slots, freqs, q_weight, k_weight, q_out)
-    _check(lib().pariskv_rotate_rows(cfg.c(), cp, qp, qs, kp, ks, vp, vs, t, pp, sp, fp, rot, int(bool(pairs)), qw, kw,
-                                     float(eps), op, _stream(stream)))
+    specs = (K, V, (positions, "positions", i32, (t,), False), (slots, "slots", i32, (t,), False),
+             (freqs, "freqs", f32, (half,), True), (q_weight, "q_weight", f32, (HEAD_DIM,), True),
+             (k_weight, "k_weight", f32, (HEAD_DIM,), True),
+             (q_out, "q_out", torch.float16, (t, cfg.n_q_heads, HEAD_DIM), False))
+    (Kp, Vp, pp, sp, fp, qw, kw, op), devices = _tensors(specs)
+    devices.update((q.get_device(), k.get_device(), v.get_device()))
+    _require_on(devices, ((q, "q"), (k, "k"), (v, "v")) + specs, stream)
+    _check(lib().pariskv_rotate_rows(cfg.c(), ctypes.byref(_Pages(Kp, Vp, n_pages, size)), qp, qs, kp, ks, vp, vs, t, pp, sp,
+                                     fp, 2 * half, bool(pairs), qw, kw, eps, op, _stream(stream)))
     return q_out
 
 
 def paged_workspace_size(cfg, batch, t, max_tokens=None):
     """Bytes of a workspace for paged_attend with these sizes and all smaller ones (0 on invalid sizes)."""
-    return int(lib().pariskv_paged_workspace(cfg.c(), int(batch), int(t), max(1, int(t if max_tokens is None else max_tokens))))
+    return int(lib().pariskv_paged_workspace(cfg.c(), int(batch), int(t), max(1, int(t)) if max_tokens is None else int(max_tokens)))
 
 
 def paged_attend(cfg, q, cache, table, lens, offsets, scale, counts=None, max_tokens=None, softcap=0.0, slopes=None,
@@ -1029,27 +1056,28 @@ def paged_attend(cfg, q, cache, table, lens, offsets, scale, counts=None, max_to
     1 for a decode step).  softcap c > 0 makes a score s c tanh(s / c), slopes (float32 [Hq]) take slope times the distance
     off it.  Returns out [t][Hq][D] float16; rows of tokens that no sequence has are left as they were."""
     torch = _torch()
-    dev, i32 = [], _torch().int32
-    if not isinstance(cache, PagedCache):
-        raise TypeError("cache must be a PagedCache")
-    qp, t, qs = _token_rows(q, "q", cfg.n_q_heads, dev)
-    cp = cache.c(cfg, dev)
+    i32, half = torch.int32, torch.float16
+    K, V, n_pages, size = _pages_specs(cfg, cache)
+    qp, qs = _token_rows(q, "q", cfg.n_q_heads)
+    t = q.shape[0]
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise ValueError("table must be a [batch][width] int32 tensor")
-    batch, width = (int(x) for x in table.shape)
-    tp, lp = _arg(table, "table", i32, (batch, width), dev), _arg(lens, "lens", i32, (batch,), dev)
-    op, np_ = _arg(offsets, "offsets", i32, (batch + 1,), dev), _arg(counts, "counts", i32, (batch,), dev, optional=True)
-    sp = _arg(slopes, "slopes", torch.float32, (cfg.n_q_heads,), dev, optional=True)
+    batch, width = table.shape
     most = max(1, t) if max_tokens is None else int(max_tokens)
     if out is None:
-        out = _new((t, cfg.n_q_heads, HEAD_DIM), torch.float16, q.device, stream)
-    outp = _arg(out, "out", torch.float16, (t, cfg.n_q_heads, HEAD_DIM), dev)
-    workspace, wp = _workspace_arg(workspace, 0 if workspace is not None else paged_workspace_size(cfg, batch, t, most), q,
-                                   dev, stream)
-    _require_device(dev)
-    _require_here(stream, q, cache.K, cache.V, table, lens, offsets, counts, slopes, out, workspace)
-    _check(lib().pariskv_paged_attend(cfg.c(), qp, qs, cp, tp, width, lp, op, np_, t, most, batch, float(scale),
-                                      float(softcap), sp, outp, wp, workspace.numel(), _stream(stream)))
+        out = _new(q.shape, half, q.device, stream)
+    if workspace is None:
+        workspace = _new((max(256, paged_workspace_size(cfg, batch, t, most)),), torch.uint8, q.device, stream)
+    bytes_ = workspace.numel() if isinstance(workspace, torch.Tensor) and workspace.dim() == 1 else None
+    specs = (K, V, (table, "table", i32, (batch, width), False), (lens, "lens", i32, (batch,), False),
+             (offsets, "offsets", i32, (batch + 1,), False), (counts, "counts", i32, (batch,), True),
+             (slopes, "slopes", torch.float32, (cfg.n_q_heads,), True), (out, "out", half, q.shape, False),
+             (workspace, "workspace", torch.uint8, (bytes_,), False))
+    (Kp, Vp, tp, lp, op, np_, sp, outp, wp), devices = _tensors(specs)
+    devices.add(q.get_device())
+    _require_on(devices, ((q, "q"),) + specs, stream)
+    _check(lib().pariskv_paged_attend(cfg.c(), qp, qs, ctypes.byref(_Pages(Kp, Vp, n_pages, size)), tp, width, lp, op, np_, t,
+                                      most, batch, scale, softcap, sp, outp, wp, bytes_, _stream(stream)))
     return out
 
 

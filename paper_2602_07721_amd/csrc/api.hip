@@ -1251,6 +1251,10 @@ int pariskv_rotate_rows(const pariskv_config* cfg, const pariskv_pages* pages, c
         !stride_ok(v_stride, cfg->n_kv_heads))
         return fail(PARISKV_ERR_INVALID, "token strides %lld, %lld, %lld: multiples of 8 values that hold the heads",
                     (long long)q_stride, (long long)k_stride, (long long)v_stride);
+    // Groups of 16 lanes take up to 8 heads of a token (more groups only in small calls).
+    const int64_t hkv = cfg->n_kv_heads, groups = (hkv * cfg->q_per_kv + 7) / 8 + 2 * ((hkv + 7) / 8);
+    if (groups * t / 16 >= kMaxBlocks256)
+        return fail(PARISKV_ERR_UNSUPPORTED, "%lld tokens of %lld KV heads: above 2^24 blocks", (long long)t, (long long)hkv);
     if (t == 0) return PARISKV_OK;
     if (!q || !k || !v || !q_out || !positions || !slots || (rot_dim > 0 && !freqs))
         return fail(PARISKV_ERR_INVALID, "q, k, v, q_out, positions, slots and freqs (with rot_dim) must be non-NULL");

@@ -6,10 +6,14 @@
 //
 // Everything in float32, rounded once.  An angle is position * frequency in 64 bits, less its whole
 // turns, before it is rounded to float32: 4 million positions on, float32 would be off by a quarter
-// radian.  Its sine and cosine are made once a token, in LDS, for all of its heads.
+// radian.
 //
-// Bound by HBM: 512 bytes a row of q, k and v.  16 lanes a row, 16 bytes a lane, so the norm's sum
-// is four lane moves; a pair's other half comes from the lane that holds it.
+// Bound by HBM: 512 bytes a row of q, k and v.  16 lanes take some heads of one kind of a token, 16 bytes
+// a lane, 4 rows at a time and the next 4 on their way: the norm's sum is four lane moves, a pair's other
+// half comes from the lane that holds it.  The lanes' sines, cosines and weights, made while the first rows
+// are on their way and folded into two factors a dim, serve all of them: 16384 tokens of 32 + 16 heads 84
+// us, 4.8 TB/s (a copy: 5.2); 107 us with sines in LDS behind a barrier for a block of 4 tokens, and 94
+// with cosines, sines and weights in registers of their own, which leave fewer waves.
 
 #include <hip/hip_fp16.h>
 
@@ -23,114 +27,124 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef int int4v __attribute__((ext_vector_type(4)));
 
 constexpr int kRrThreads = 256, kRrGroups = kRrThreads / 16;
-constexpr int kRrManyTokens = 4;  // tokens of a block in large calls
 constexpr int kRrAhead = 4;       // rows whose loads a group has in flight
+constexpr int kRrMostHeads = 8;  // heads of a group
 
 enum { kNoPairs = 0, kHalves = 1, kNeighbours = 2 };
 
-template <int PAIRS, int TOKENS>
-__global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a) {
-    __shared__ float2 turn[TOKENS][kD / 2];  // cosine, sine
-    __shared__ int at[TOKENS];               // row of the slot's first head in the cache, -1: no slot
-    const int tid = threadIdx.x, c = tid & 15, group = tid >> 4;
-    const int t0 = blockIdx.x * TOKENS;
-    const int hq = a.hkv * a.g, heads = hq + 2 * a.hkv;
+// Groups of a token of up to n heads each: of q, of k, of v.  Those of a kind take heads in turn, so
+// that a wave's read next to each other.
+struct RowGroups {
+    int q, kv;
+    __host__ __device__ RowGroups(const RotateArgs& a, int n)
+        : q((a.hkv * a.g + n - 1) / n), kv((a.hkv + n - 1) / n) {}
+    __host__ __device__ int64_t all(const RotateArgs& a) const { return (int64_t)a.t * (q + 2 * kv); }
+};
+
+template <int PAIRS>
+__global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, int heads, bool past) {
+    const RowGroups gr(a, heads);
+    const int c = threadIdx.x & 15;  // dims 8 c .. 8 c + 7 of a row
+    // All of q's groups, then k's, then v's: a wave's are of one kind mostly.
+    int64_t id = (int64_t)blockIdx.x * kRrGroups + (threadIdx.x >> 4);
+    const int64_t nq = (int64_t)a.t * gr.q, nk = (int64_t)a.t * gr.kv;
+    const int kind = id < nq ? 0 : id < nq + nk ? 1 : 2;
+    id -= kind == 0 ? 0 : kind == 1 ? nq : nq + nk;
+    const uint32_t per = (uint32_t)(kind == 0 ? gr.q : gr.kv);
+    const int tok = (int)((uint32_t)id / per), first = (int)((uint32_t)id % per);
+    if (tok >= a.t) return;
+    const int slot = a.slots[tok];
+    if (slot < 0 || slot >= a.n_slots) return;
+    const int all = kind == 0 ? a.hkv * a.g : a.hkv;
+    const __half* from = kind == 0 ? static_cast<const __half*>(a.q) + tok * a.q_stride
+                       : kind == 1 ? static_cast<const __half*>(a.k) + tok * a.k_stride
+                                   : static_cast<const __half*>(a.v) + tok * a.v_stride;
+    int4v x[kRrAhead];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int u = 0; u < kRrAhead; ++u)
+            x[u] = reinterpret_cast<const int4v*>(from + min(h0 + u * (int)per, all - 1) * kD)[c];
+    };
+    load(first);
+
+    const int page = (int)a.page((uint32_t)slot), size = (int)a.page.d;
+    // Row 0 of the kind, and how far apart its heads' rows are.
+    const int64_t to_row = kind == 0 ? (int64_t)tok * all : (int64_t)page * a.hkv * size + (slot - page * size);
+    const int step = kind == 0 ? 1 : size;
+    int4v* to = static_cast<int4v*>(kind == 0 ? a.q_out : kind == 1 ? a.K : a.V) + to_row * (kD / 8) + c;
+
+    // The pairs' other halves, and which halves this lane's are.
     const int half = a.rot / 2;
-
-    if (tid < TOKENS) {
-        const int slot = t0 + tid < a.t ? a.slots[t0 + tid] : -1;
-        int row = -1;
-        if (slot >= 0 && slot < a.n_slots) {
-            const int page = (int)a.page((uint32_t)slot), size = (int)a.page.d;
-            row = page * a.hkv * size + (slot - page * size);
-        }
-        at[tid] = row;
-    }
-    if constexpr (PAIRS != kNoPairs) {
-        for (int i = tid; i < TOKENS * half; i += kRrThreads) {
-            const int tok = i / half, f = i % half;
-            const double turns = (double)a.positions[min(t0 + tok, a.t - 1)] * (double)a.freqs[f] * 0.15915494309189535;
-            float s, co;
-            sincospif(2.f * (float)(turns - rint(turns)), &s, &co);
-            turn[tok][f] = float2{co, s};
-        }
-    }
-    __syncthreads();
-
-    // Dims 8 c .. 8 c + 7 of a row, those of the pairs' other halves, and which halves these are.
-    const bool turns = 8 * c < a.rot, first = PAIRS != kHalves || 8 * c < half;
-    const int other = PAIRS == kHalves && turns ? (first ? c + half / 8 : c - half / 8) : c;
-    const int other_lane = (((tid & 48) | other) & 63) << 2;
-    const int f0 = PAIRS == kHalves ? (turns ? 8 * min(c, other) : 0) : 4 * c;
-    float w[2][8], wo[2][8];
+    const bool turns = PAIRS != kNoPairs && kind < 2 && 8 * c < a.rot;
+    const bool is_first = PAIRS != kHalves || 8 * c < half;
+    const int other = PAIRS == kHalves && turns ? (is_first ? c + half / 8 : c - half / 8) : c;
+    const int other_lane = (int)((threadIdx.x & 48) | other) << 2;
+    // y = inv (x A + x' B), x' the pair's other half: weights, cosines and sines in two factors a dim.
+    const float* weight = kind == 0 ? a.q_weight : a.k_weight;
+    const bool norm = kind < 2 && weight;
+    float fa[8], fb[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        w[0][i] = a.q_weight ? a.q_weight[8 * c + i] : 1.f;
-        w[1][i] = a.k_weight ? a.k_weight[8 * c + i] : 1.f;
-        wo[0][i] = PAIRS == kHalves && a.q_weight ? a.q_weight[8 * other + i] : 1.f;
-        wo[1][i] = PAIRS == kHalves && a.k_weight ? a.k_weight[8 * other + i] : 1.f;
+        fa[i] = norm ? weight[8 * c + i] : 1.f;
+        fb[i] = !norm ? 1.f : PAIRS == kHalves ? weight[8 * other + i] : weight[8 * c + (i ^ 1)];
     }
-
-    const int rows = min(TOKENS, a.t - t0) * heads;
-    auto source = [&](int r) {
-        const int tok = r / heads, h = r % heads;
-        const int64_t token = t0 + tok;
-        const __half* p = h < hq            ? static_cast<const __half*>(a.q) + token * a.q_stride + h * kD
-                          : h < hq + a.hkv ? static_cast<const __half*>(a.k) + token * a.k_stride + (h - hq) * kD
-                                           : static_cast<const __half*>(a.v) + token * a.v_stride + (h - hq - a.hkv) * kD;
-        return reinterpret_cast<const int4v*>(p) + c;
-    };
-    for (int r0 = group; r0 < rows; r0 += kRrGroups * kRrAhead) {
-        int4v x[kRrAhead];
+    if (PAIRS != kNoPairs && turns) {
+        const double p = a.positions[tok];
+        const int f0 = PAIRS == kHalves ? 8 * min(c, other) : 4 * c;
+        float si = 0.f, co = 0.f;
 #pragma unroll
-        for (int u = 0; u < kRrAhead; ++u) x[u] = *source(min(r0 + u * kRrGroups, rows - 1));
+        for (int i = 0; i < 8; ++i) {
+            if (PAIRS == kHalves || i % 2 == 0) {
+                const double turn = p * (double)a.freqs[f0 + (PAIRS == kHalves ? i : i / 2)] * 0.15915494309189535;
+                // In turns; within 2^-22.9 of sine and cosine over 2^24 values of half a turn either way.
+                const float x = (float)(turn - rint(turn));
+                si = __builtin_amdgcn_sinf(x);
+                co = __builtin_amdgcn_cosf(x);
+            }
+            fa[i] *= co;
+            fb[i] *= (PAIRS == kHalves ? is_first : i % 2 == 0) ? -si : si;
+        }
+    }
+    for (int h0 = first; h0 < all; h0 += kRrAhead * (int)per) {
+        int4v y[kRrAhead];
+#pragma unroll
+        for (int u = 0; u < kRrAhead; ++u) y[u] = x[u];
+        if (h0 + kRrAhead * (int)per < all) load(h0 + kRrAhead * (int)per);
 #pragma unroll
         for (int u = 0; u < kRrAhead; ++u) {
-            const int r = min(r0 + u * kRrGroups, rows - 1);
-            const int tok = r / heads, h = r % heads;
-            const int kind = h < hq ? 0 : h < hq + a.hkv ? 1 : 2;
-            int4v y = x[u];
-            const half8 in = __builtin_bit_cast(half8, y);
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)in[i], (float)in[i], s);
-            s = row_sum_f32(s);
-            const bool norm = kind == 0 ? a.q_weight != nullptr : a.k_weight != nullptr;
-            const float inv = norm ? rsqrtf(s * (1.f / kD) + a.eps) : 1.f;
-            half8 pair = in;
-            if constexpr (PAIRS == kHalves) {
-                int4v z;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) z[i] = __builtin_amdgcn_ds_bpermute(other_lane, y[i]);
-                pair = __builtin_bit_cast(half8, z);
-            }
             if (kind < 2) {
+                const half8 in = __builtin_bit_cast(half8, y[u]);
+                float inv = 1.f;
+                if (norm) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)in[i], (float)in[i], s);
+                    inv = rsqrtf(row_sum_f32(s) * (1.f / kD) + a.eps);
+                }
+                half8 pair = in;
+                if constexpr (PAIRS == kHalves) {
+                    int4v z;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = __builtin_amdgcn_ds_bpermute(other_lane, y[u][i]);
+                    pair = __builtin_bit_cast(half8, z);
+                }
                 half8 out;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float own = (float)in[i] * inv * (kind == 0 ? w[0][i] : w[1][i]);
-                    float res = own;
-                    if constexpr (PAIRS == kHalves) {
-                        const float2 cs = turn[tok][f0 + i];
-                        const float oth = (float)pair[i] * inv * (kind == 0 ? wo[0][i] : wo[1][i]);
-                        if (turns) res = first ? own * cs.x - oth * cs.y : own * cs.x + oth * cs.y;
-                    } else if constexpr (PAIRS == kNeighbours) {
-                        const float2 cs = turn[tok][f0 + i / 2];
-                        const float oth = (float)in[i ^ 1] * inv * (kind == 0 ? w[0][i ^ 1] : w[1][i ^ 1]);
-                        if (turns) res = i % 2 == 0 ? own * cs.x - oth * cs.y : own * cs.x + oth * cs.y;
+                    float res = (float)in[i] * fa[i];
+                    if constexpr (PAIRS != kNoPairs) {
+                        const float both = __builtin_fmaf((float)(PAIRS == kHalves ? pair[i] : in[i ^ 1]), fb[i], res);
+                        res = turns ? both : res;
                     }
-                    out[i] = (_Float16)res;
+                    out[i] = (_Float16)(res * inv);
                 }
-                y = __builtin_bit_cast(int4v, out);
+                y[u] = __builtin_bit_cast(int4v, out);
             }
-            if (r0 + u * kRrGroups >= rows || at[tok] < 0) continue;
-            char* to;
-            if (kind == 0)
-                to = static_cast<char*>(a.q_out) + ((int64_t)(t0 + tok) * hq + h) * (2 * kD);
-            else
-                to = static_cast<char*>(kind == 1 ? a.K : a.V) +
-                     ((int64_t)at[tok] + (int64_t)(h - hq - (kind - 1) * a.hkv) * a.page.d) * (2 * kD);
-            reinterpret_cast<int4v*>(to)[c] = y;
+            const int h = h0 + u * (int)per;
+            if (h >= all) continue;
+            int4v* at = to + (int64_t)h * step * (kD / 8);
+            if (past) __builtin_nontemporal_store(y[u], at);
+            else *at = y[u];
         }
     }
 }
@@ -138,20 +152,20 @@ __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a) {
 }  // namespace
 
 hipError_t launch_rotate_rows(const RotateArgs& a, hipStream_t s) {
-    // One token a block leaves no CU idle in small calls; several share the weights' loads.
-    const bool many = a.t >= 2048;
-    const int per = many ? kRrManyTokens : 1;
+    // As many heads a group as make its sines worth it, but no fewer groups than fill the chip.
+    int heads = kRrMostHeads;
+    while (heads > kRrAhead && RowGroups(a, heads).all(a) < 256 * 8 * kRrGroups) heads /= 2;
+    const int64_t blocks = (RowGroups(a, heads).all(a) + kRrGroups - 1) / kRrGroups;
+    // Outputs that no cache holds until they are read go past them: 16384 tokens of 48 heads 98.5 -> 92.6 us.
+    const bool past = (int64_t)a.t * (a.hkv * a.g + 2 * a.hkv) * kD * 2 > (64 << 20);
     const ProfEvents pe = prof_begin("rotate_rows");
     auto go = [&](auto kernel) {
-        hipExtLaunchKernelGGL(kernel, dim3((unsigned)((a.t + per - 1) / per)), dim3(kRrThreads), 0, s, pe.start, pe.stop,
-                              0, a);
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRrThreads), 0, s, pe.start, pe.stop, 0, a, heads,
+                              past);
     };
-    if (a.rot == 0)
-        many ? go(rotate_rows_kernel<kNoPairs, kRrManyTokens>) : go(rotate_rows_kernel<kNoPairs, 1>);
-    else if (!a.pairs)
-        many ? go(rotate_rows_kernel<kHalves, kRrManyTokens>) : go(rotate_rows_kernel<kHalves, 1>);
-    else
-        many ? go(rotate_rows_kernel<kNeighbours, kRrManyTokens>) : go(rotate_rows_kernel<kNeighbours, 1>);
+    if (a.rot == 0) go(rotate_rows_kernel<kNoPairs>);
+    else if (!a.pairs) go(rotate_rows_kernel<kHalves>);
+    else go(rotate_rows_kernel<kNeighbours>);
     return hipGetLastError();
 }
 
