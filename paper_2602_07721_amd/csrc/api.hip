@@ -1301,11 +1301,9 @@ static int paged_shape(const pariskv_config* cfg, int32_t batch, int64_t t, int6
     a->g = cfg->q_per_kv;
     a->width = 1;
     a->page = divide_by(1);
-    const int64_t heads = (int64_t)cfg->n_kv_heads * batch;
-    // A block for every row of a few tokens' join; for every 128 rows of more, and the shares beyond.
-    const int64_t rows = (int64_t)a->most * a->g;
-    const int64_t blocks = rows <= 32 ? rows * heads : ((int64_t)t * a->g / 128 + batch) * cfg->n_kv_heads + 16384;
-    if (blocks > kMaxBlocks256)
+    // A block for every tile of 128 rows, and a fixed number more.
+    const int64_t blocks = (t * cfg->q_per_kv / 128 + batch) * cfg->n_kv_heads + 16384;
+    if ((int64_t)a->most * a->g > 32 && blocks > kMaxBlocks256)
         return fail(PARISKV_ERR_UNSUPPORTED, "%d sequences x %d KV heads, %lld tokens: above 2^24 blocks", batch,
                     cfg->n_kv_heads, (long long)t);
     return PARISKV_OK;
