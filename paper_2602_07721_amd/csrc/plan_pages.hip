@@ -8,9 +8,10 @@
 // sequences at a time: a scan in each wave's registers and one over the waves' totals in LDS.
 // Sums saturate at 2^32 - 1, which is past every limit that they are compared with.
 //
-// Bound by latency: lengths in, two scans, the popped pages, the slots, each waiting for the one
-// before.  Up to kPlanOwn token slots are filled by the same block, more by a second kernel of
-// many blocks (a block writes 1024 slots in about 1 us, a launch costs 3).
+// Bound by latency: lengths in, three scans, the popped pages, the slots, each waiting for the one
+// before.  A decode step's tokens are placed by their sequences' threads; up to kPlanOwn of prompts by
+// the same block, more by a second kernel of many blocks (a block writes 1024 slots in about 1 us, a
+// launch costs 3).
 
 #include "pages.hpp"
 
@@ -105,7 +106,7 @@ __device__ __forceinline__ void fill_token(const PlanArgs& a, int i, Offset&& of
 }
 
 __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
-    __shared__ uint32_t t0[kPlanWaves], t1[kPlanWaves];
+    __shared__ uint32_t t0[kPlanWaves], t1[kPlanWaves], taken;
     const int tid = threadIdx.x, lane = tid & 63;
     const uint32_t pages = (uint32_t)a.n_pages;
     const uint32_t free0 = (uint32_t)min((int64_t)max(a.n_free[0], 0), a.n_pages);
@@ -148,7 +149,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
     }
     const uint32_t top = min(add_sat(free0, back), pages);
 
-    uint32_t taken = 0, tokens = 0, wanted = 0;  // of the sequences before
+    // The pages that are taken are the first of those that are wanted: once a sequence finds too few,
+    // so does every one behind it that wants any.
+    if (tid == 0) taken = 0u;  // seen at the next barrier
+    uint32_t tokens = 0, wanted = 0;  // of the sequences before
+    bool far = false;  // whether some sequence has more tokens than its thread places
+    const bool place = a.t <= kPlanOwn;
     for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
         const int b = b0 + tid;
         const Ask k = ask_of(a, b);
@@ -161,10 +167,20 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
         const uint32_t first = upto - needs;  // where it is ok, nothing saturated
         const uint32_t takes = ok ? needs : 0u;
         if (b < a.batch) {
-            if (takes == 1) a.table[(int64_t)b * a.width + k.held] = a.free[top - 1 - first];
+            int32_t* row = a.table + (int64_t)b * a.width;
+            int page = 0;
+            if (takes == 1) row[k.held] = page = a.free[top - 1 - first];
             a.new_lens[b] = (int32_t)(ok || k.shrinks ? k.after : k.len);
             a.granted[b] = ok ? (int32_t)k.fresh : 0;
             a.offsets[b + 1] = (int32_t)min(end, (uint32_t)a.t);
+            // A decode step's token: its page is at hand, or the last one held.
+            if (place && k.fresh == 1 && end <= (uint32_t)a.t) {
+                if (ok && takes == 0) page = row[k.held - 1];
+                a.slots[end - 1] = ok ? page * (int)a.page.d + (int)(k.len - a.page(k.len) * a.page.d) : -1;
+                a.positions[end - 1] = ok ? (int)k.len : -1;
+            }
+            far |= k.fresh > 1;
+            if (takes > 0) atomicMax(&taken, upto);
         }
         uint64_t who = __ballot(takes > 1);
         while (who) {
@@ -176,23 +192,25 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
             int32_t* to = a.table + (int64_t)(b0 + (tid - lane) + l) * a.width + held;
             for (uint32_t j = lane; j < n; j += 64) to[j] = a.free[top - 1 - f - j];
         }
-        // The pages that are taken are the first of those that are wanted: once a sequence finds too
-        // few, so does every one behind it that wants any.
-        uint32_t all_taken;
-        __syncthreads();
-        block_incl_sat(takes, t0, &all_taken);
-        taken = add_sat(taken, all_taken);
         tokens = add_sat(tokens, all_tokens);
         wanted = add_sat(wanted, all_pages);
-        __syncthreads();
+        if (b0 + kPlanThreads < a.batch) __syncthreads();  // the totals are read
     }
+    const bool rest = __syncthreads_or(far);  // and all of the plan is there
     if (tid == 0) {
         a.offsets[0] = 0;
         a.new_free[0] = (int32_t)(top - taken);
     }
-    if (a.t > kPlanOwn) return;
-    __syncthreads();
-    for (int i = tid; i < a.t; i += kPlanThreads) fill_token(a, i, [&](int b) { return a.offsets[b]; });
+    if (!place) return;
+    const int real = (int)min(tokens, (uint32_t)a.t);
+    for (int i = (rest ? 0 : real) + tid; i < a.t; i += kPlanThreads) {
+        if (i < real) {
+            fill_token(a, i, [&](int b) { return b == 0 ? 0 : a.offsets[b]; });
+        } else {
+            a.slots[i] = -1;
+            a.positions[i] = -1;
+        }
+    }
 }
 
 __global__ __launch_bounds__(kFillThreads) void fill_slots_kernel(PlanArgs a) {
