@@ -44,9 +44,7 @@ __device__ __forceinline__ int page_row(const PagedArgs& a, int entry, int head,
 enum { kPlainScores = 0, kCappedScores = 1, kBiasedScores = 2 };
 
 // With a shape, scores are in powers of two: s' = cap log2(e) tanh(scale s / cap), or the plain
-// product, plus slope log2(e) times the distance.  tanh(u) = 1 - 2 / (2^(2 log2(e) u) + 1) is off by
-// 2^-23 at most; where u is small, a series in u keeps that relative to u (the next term is 2^-24 of
-// it at 0.2).
+// product, plus slope log2(e) times the distance.
 template <int SHAPE>
 struct ScoreShape {
     float unit, cap, slope;  // s times unit is u (capped) or the score in powers of two
@@ -57,20 +55,44 @@ struct ScoreShape {
         cap = SHAPE & kCappedScores ? a.cap * kLog2e : 0.f;
         slope = SHAPE & kBiasedScores ? a.slopes[head] * kLog2e : 0.f;
     }
-    // Of the key `distance` behind the token (negative: how far behind).
-    __device__ __forceinline__ float operator()(float s, float distance) const {
-        float x = s * unit;
+    // Of a lane's N scores, which the functions give for their numbers: the score, and how far its key is
+    // behind the token (negative).
+    //
+    // Where all of a wave's |u| are below 0.2, a series, within 2^-24 of tanh(u), in five instructions of
+    // the vector unit; else tanh(u) = 1 - 2 / (2^(2 log2(e) u) + 1), within 2^-23 of 1, with two that take
+    // four times as long.  8192 tokens, 32 heads, cap 30: 867 us with both for every score.
+    template <int N, class Score, class Distance>
+    __device__ __forceinline__ void operator()(Score&& score, Distance&& distance) const {
         if constexpr ((SHAPE & kCappedScores) != 0) {
-            const float u = x, u2 = u * u;
-            const float e = __builtin_amdgcn_exp2f(u * 2.8853900817779268f);
-            const float far = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
-            float near = __builtin_fmaf(u2, -0.053968254f, 0.13333334f);
-            near = __builtin_fmaf(u2, near, -0.33333334f);
-            near = __builtin_fmaf(u2 * u, near, u);
-            x = cap * (u2 < 0.04f ? near : far);
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                score(i) *= unit;
+                top = fmaxf(top, __builtin_fabsf(score(i)));
+            }
+            if (__all(top < 0.2f)) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float u = score(i), u2 = u * u;
+                    float x = __builtin_fmaf(u2, cap * -0.053968254f, cap * 0.13333334f);
+                    x = __builtin_fmaf(u2, x, cap * -0.33333334f);
+                    score(i) = u * __builtin_fmaf(u2, x, cap);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(score(i) * 2.8853900817779268f);
+                    score(i) = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(e + 1.f), cap);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) score(i) *= unit;
         }
-        if constexpr ((SHAPE & kBiasedScores) != 0) x = __builtin_fmaf(slope, distance, x);
-        return x;
+        if constexpr ((SHAPE & kBiasedScores) != 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) score(i) = __builtin_fmaf(slope, distance(i), score(i));
+        }
     }
 };
 
@@ -277,17 +299,12 @@ __device__ __forceinline__ void few_rows_attend(const PagedArgs& a, int b, const
         if (st + kPgWaves < last) fetch(st + kPgWaves, s);
         if constexpr (SHAPE != kPlainScores) {
             const float from = (float)(st * kCaKeys - p);
-            if constexpr (R == 16) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        rows.s[h][i] = shape(rows.s[h][i], from + (float)(16 * h + 4 * rows.lg + i));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    rows.s[i] = shape(rows.s[i], from + (float)(8 * (i / 4) + 4 * rows.half + i % 4));
-            }
+            if constexpr (R == 16)
+                shape.template operator()<8>([&](int i) -> float& { return reinterpret_cast<float*>(rows.s)[i]; },
+                                             [&](int i) { return from + (float)(16 * (i / 4) + 4 * rows.lg + i % 4); });
+            else
+                shape.template operator()<16>([&](int i) -> float& { return reinterpret_cast<float*>(&rows.s)[i]; },
+                                              [&](int i) { return from + (float)(8 * (i / 4) + 4 * rows.half + i % 4); });
         }
         rows.accumulate(w, vt, lane);
     }

@@ -352,10 +352,8 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
             }
             if constexpr (SHAPE != kPlainScores) {
                 const float from = (float)(base_row + 4 * half - p);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[h][i] = shape(s[h][i], from + (float)(32 * h + 8 * (i / 4) + i % 4));
+                shape.template operator()<32>([&](int i) -> float& { return reinterpret_cast<float*>(s)[i]; },
+                                              [&](int i) { return from + (float)(8 * (i / 4) + i % 4); });
             }
             if (partly(tile, there)) {
                 uint32_t w[2];

@@ -4,8 +4,8 @@
 // All of it is sums over the sequences before: sequence b's tokens begin at the sum of the counts
 // before it, the i-th page that the step needs is the i-th from the top of the stack of free ones,
 // and the pages that sequences give back go onto the stack first, the last one lowest, so that
-// taking as many again takes the same ones in the same order.  A block of 1024 threads takes 1024
-// sequences at a time: a scan in each wave's registers and one over the waves' totals in LDS.
+// taking as many again takes the same ones in the same order.  A block takes as many
+// sequences at a time as it has threads: a scan in each wave's registers and one over the waves' totals in LDS.
 // Sums saturate at 2^32 - 1, which is past every limit that they are compared with.
 //
 // Bound by latency: lengths in, three scans, the popped pages, the slots, each waiting for the one
@@ -19,7 +19,8 @@ namespace pariskv {
 
 namespace {
 
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+constexpr int kPlanMost = 1024;  // threads of the planning block, fewer for fewer sequences
+constexpr int kPlanFew = 256;
 constexpr int kPlanOwn = 4096;  // token slots that the planning block fills itself
 constexpr int kFillThreads = 256;
 
@@ -38,6 +39,7 @@ __device__ __forceinline__ uint32_t wave_incl_sat(uint32_t v) {
 
 // Sum of v over the threads up to this one, and over all.  Ends with a barrier behind it that the
 // next call's writes to `totals` have to wait for: calls in turn take two arrays in turn.
+template <int THREADS>
 __device__ __forceinline__ uint32_t block_incl_sat(uint32_t v, uint32_t* totals, uint32_t* all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t in = wave_incl_sat(v);
@@ -45,7 +47,7 @@ __device__ __forceinline__ uint32_t block_incl_sat(uint32_t v, uint32_t* totals,
     __syncthreads();
     uint32_t before = 0, sum = 0;
 #pragma unroll
-    for (int w = 0; w < kPlanWaves; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         const uint32_t x = totals[w];
         before = add_sat(before, w < wave ? x : 0u);
         sum = add_sat(sum, x);
@@ -105,8 +107,9 @@ __device__ __forceinline__ void fill_token(const PlanArgs& a, int i, Offset&& of
     a.positions[i] = pos;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
-    __shared__ uint32_t t0[kPlanWaves], t1[kPlanWaves], taken;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void plan_pages_kernel(PlanArgs a) {
+    __shared__ uint32_t t0[THREADS / 64], t1[THREADS / 64], taken;
     const int tid = threadIdx.x, lane = tid & 63;
     const uint32_t pages = (uint32_t)a.n_pages;
     const uint32_t free0 = (uint32_t)min((int64_t)max(a.n_free[0], 0), a.n_pages);
@@ -114,22 +117,22 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
     // Given back: the i-th page, in the order of the sequences and of their rows, goes to place
     // free0 + all - 1 - i.
     uint32_t back = 0;
-    if (a.batch > kPlanThreads) {
+    if (a.batch > THREADS) {
         uint32_t mine = 0;
-        for (int b = tid; b < a.batch; b += kPlanThreads) {
+        for (int b = tid; b < a.batch; b += THREADS) {
             const Ask k = ask_of(a, b);
             mine = add_sat(mine, k.shrinks ? k.held - k.wants : 0u);
         }
-        block_incl_sat(mine, t0, &back);
+        block_incl_sat<THREADS>(mine, t0, &back);
         __syncthreads();
     }
     uint32_t before = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
+    for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
         const Ask k = ask_of(a, b0 + tid);
         const uint32_t gives = k.shrinks ? k.held - k.wants : 0u;
         uint32_t all;
-        const uint32_t first = add_sat(before, block_incl_sat(gives, t0, &all) - gives);
-        if (a.batch <= kPlanThreads) back = all;
+        const uint32_t first = add_sat(before, block_incl_sat<THREADS>(gives, t0, &all) - gives);
+        if (a.batch <= THREADS) back = all;
         const int64_t end = (int64_t)free0 + back - 1;
         uint64_t who = __ballot(gives > 0);
         while (who) {  // a wave's lanes take the pages of one sequence after the other
@@ -155,14 +158,14 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
     uint32_t tokens = 0, wanted = 0;  // of the sequences before
     bool far = false;  // whether some sequence has more tokens than its thread places
     const bool place = a.t <= kPlanOwn;
-    for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
+    for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
         const int b = b0 + tid;
         const Ask k = ask_of(a, b);
         uint32_t all_tokens, all_pages;
-        const uint32_t end = add_sat(tokens, block_incl_sat(k.fresh, t0, &all_tokens));
+        const uint32_t end = add_sat(tokens, block_incl_sat<THREADS>(k.fresh, t0, &all_tokens));
         const bool fits = k.room && end <= (uint32_t)a.t;
         const uint32_t needs = fits && k.fresh > 0 ? k.wants - k.held : 0u;
-        const uint32_t upto = add_sat(wanted, block_incl_sat(needs, t1, &all_pages));
+        const uint32_t upto = add_sat(wanted, block_incl_sat<THREADS>(needs, t1, &all_pages));
         const bool ok = fits && k.fresh > 0 && (needs == 0 || upto <= top);
         const uint32_t first = upto - needs;  // where it is ok, nothing saturated
         const uint32_t takes = ok ? needs : 0u;
@@ -194,7 +197,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
         }
         tokens = add_sat(tokens, all_tokens);
         wanted = add_sat(wanted, all_pages);
-        if (b0 + kPlanThreads < a.batch) __syncthreads();  // the totals are read
+        if (b0 + THREADS < a.batch) __syncthreads();  // the totals are read
     }
     const bool rest = __syncthreads_or(far);  // and all of the plan is there
     if (tid == 0) {
@@ -203,7 +206,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(PlanArgs a) {
     }
     if (!place) return;
     const int real = (int)min(tokens, (uint32_t)a.t);
-    for (int i = (rest ? 0 : real) + tid; i < a.t; i += kPlanThreads) {
+    for (int i = (rest ? 0 : real) + tid; i < a.t; i += THREADS) {
         if (i < real) {
             fill_token(a, i, [&](int b) { return b == 0 ? 0 : a.offsets[b]; });
         } else {
@@ -222,7 +225,12 @@ __global__ __launch_bounds__(kFillThreads) void fill_slots_kernel(PlanArgs a) {
 
 hipError_t launch_plan_pages(const PlanArgs& a, hipStream_t s) {
     ProfEvents pe = prof_begin("plan_pages");
-    hipExtLaunchKernelGGL(plan_pages_kernel, dim3(1), dim3(kPlanThreads), 0, s, pe.start, pe.stop, 0, a);
+    auto go = [&](auto kernel, int threads) {
+        hipExtLaunchKernelGGL(kernel, dim3(1), dim3(threads), 0, s, pe.start, pe.stop, 0, a);
+    };
+    // Fewer waves meet at a barrier sooner.
+    a.batch <= kPlanFew && a.t <= 4 * kPlanFew ? go(plan_pages_kernel<kPlanFew>, kPlanFew)
+                                               : go(plan_pages_kernel<kPlanMost>, kPlanMost);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.t <= kPlanOwn) return e;
     pe = prof_begin("fill_slots");
