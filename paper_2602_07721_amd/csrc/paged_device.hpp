@@ -140,6 +140,22 @@ struct LaneSeqs {
         b0 = min((int)(threadIdx.x & 63) * each, a.batch);
         b1 = min(b0 + each, a.batch);
     }
+    // f(b, sequence b) for each of them; the loads of 8 are on their way at a time.
+    template <class F>
+    __device__ __forceinline__ void each_of(const PagedArgs& a, F&& f) const {
+        if (each == 1) {
+            if (b0 < b1) f(b0, paged_seq(a, b0));
+            return;
+        }
+        for (int b = b0; b < b1; b += 8) {
+            PagedSeq s[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s[u] = paged_seq(a, min(b + u, b1 - 1));
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (b + u < b1) f(b + u, s[u]);
+        }
+    }
 };
 
 // Which stretch of a line a block takes: consecutive blocks go to the 8 XCDs in turn, and each XCD
@@ -210,50 +226,51 @@ constexpr int few_wave_lds(int rows) {
     return kCaKeys * kD * 2 > ca_state_bytes(rows) ? kCaKeys * kD * 2 : ca_state_bytes(rows);
 }
 
-// The M = count g rows of one KV head over parts [part0, part1) of its keys.  lds(w): few_wave_lds(R)
-// bytes of wave w, 16-byte aligned.  Outputs where these are all parts, else states: row r's
-// outputs at part[r D], its reference and sum, negative where paged_odd_part has something to add,
-// at state[r].
-template <int R, int SHAPE, bool STREAM, class Lds>
-__device__ __forceinline__ void few_rows_attend(const PagedArgs& a, int b, const PagedSeq& seq, int head, int part0,
-                                                int part1, int parts, Lds&& lds, float* part,
-                                                float2* state) {
+// What a block takes of a head at a time: parts [part0, part1) of the keys of its M = count g rows.
+struct FewSegment {
+    int b, head, part0, part1, parts;
+    PagedSeq seq;
+    __device__ __forceinline__ int first() const { return part0 * kPgWaves; }  // steps of 32 keys
+    __device__ __forceinline__ int last() const {
+        return min(part1 * kPgWaves, (seq.len + kCaKeys - 1) / kCaKeys);
+    }
+};
+
+// Walks segments from g, at place x of the line, up to `end`.  lds(w): few_wave_lds(R) bytes of wave w,
+// 16-byte aligned.  A head's outputs where its parts are all here, else states: row r's outputs, its
+// reference and sum, negative where paged_odd_part has something to add.  A wave's next step, of this
+// segment or of the next, is on its way while one is computed on and while segments end.
+template <int R, int SHAPE, bool STREAM, class Parts, class Lds>
+__device__ __forceinline__ FewRecord few_walk(const PagedArgs& a, const FewSpace& ws, const FewLine& line, int id,
+                                              FewSegment g, int64_t x, int64_t end, Parts&& parts_of, Lds&& lds) {
     using Rows = ChunkRows<R>;
     constexpr int kHalves = Rows::kHalves, kSteps = Rows::kSteps;
-    int tid = threadIdx.x;
-    asm("" : "+v"(tid));  // what follows from it is made here, not kept in registers for the next call
-    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned char* vt = lds(wave);
     const int vrow = lane >> 4, vchunk = lane & 15;  // of a load or a store of 4 rows of V
-    const int M = seq.count * a.g, len = seq.len;
-    const int first = part0 * kPgWaves, last = min(part1 * kPgWaves, (len + kCaKeys - 1) / kCaKeys);
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-    const int row = min(Rows::row(lane), M - 1), tok = row / a.g, qhead = head * a.g + row % a.g;
-    const int p = len - seq.count + tok;
 
     // A step's pages, one key a lane (and lane + 32): entries of the table, then rows of K and V and
     // which of them there are.  Keys behind the last repeat it, those without a page the first that
     // has one (there or not, row 0 of the pages is memory).
-    auto key_row = [&](int st) { return min(st * kCaKeys + (lane & 31), len - 1); };
-    auto entry_of = [&](int st) { return page_entry(a, b, key_row(st)); };
-    struct Step {
-        u4v k[8], v[8];
-        uint32_t there;  // its keys that have pages
-    };
+    auto key_row = [&](int st, int len) { return min(st * kCaKeys + (lane & 31), len - 1); };
+    auto entry_of = [&](int b, int st, int len) { return page_entry(a, b, key_row(st, len)); };
     auto read = [](const u4v* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; };
-    int entry = 0;  // of this lane's key of the next step that is fetched
-    auto fetch = [&](int st, Step& s) __attribute__((always_inline)) {
-        const bool good = (uint32_t)entry < (uint32_t)a.n_pages;
-        s.there = (uint32_t)__ballot(good);
-        int at = good ? page_row(a, entry, head, key_row(st)) : 0;
-        if (__builtin_expect(s.there != ~0u, 0)) {
-            const int other = s.there ? __builtin_amdgcn_readlane(at, __builtin_ctz(s.there)) : 0;
+    u4v kreg[8], vreg[8];
+    uint32_t there = 0;  // the step's keys that have pages
+    int entry = 0;       // of this lane's key of the step behind
+    auto fetch = [&](int b, int head, int len, int st, int last, int e) __attribute__((always_inline)) {
+        const bool good = (uint32_t)e < (uint32_t)a.n_pages;
+        there = (uint32_t)__ballot(good);
+        int at = good ? page_row(a, e, head, key_row(st, len)) : 0;
+        if (__builtin_expect(there != ~0u, 0)) {
+            const int other = there ? __builtin_amdgcn_readlane(at, __builtin_ctz(there)) : 0;
             at = good ? at : other;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = __builtin_amdgcn_ds_bpermute((4 * i + vrow) << 2, at);
-            s.v[i] = read(reinterpret_cast<const u4v*>(static_cast<const _Float16*>(a.V) + (int64_t)r * kD) + vchunk);
+            vreg[i] = read(reinterpret_cast<const u4v*>(static_cast<const _Float16*>(a.V) + (int64_t)r * kD) + vchunk);
         }
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
@@ -261,87 +278,133 @@ __device__ __forceinline__ void few_rows_attend(const PagedArgs& a, int b, const
             const _Float16* k = static_cast<const _Float16*>(a.K) + (int64_t)r * kD;
 #pragma unroll
             for (int c = 0; c < kSteps; ++c)
-                s.k[h * kSteps + c] = read(reinterpret_cast<const u4v*>(k + Rows::template dim<false>(c, lane)));
+                kreg[h * kSteps + c] = read(reinterpret_cast<const u4v*>(k + Rows::template dim<false>(c, lane)));
         }
-        if (st + kPgWaves < last) entry = entry_of(st + kPgWaves);
+        if (st + kPgWaves < last) entry = entry_of(b, st + kPgWaves, len);
     };
-    int st = first + wave;
-    Step s;
-    if (st < last) {
-        entry = entry_of(st);
-        fetch(st, s);
-    }
-    const _Float16* qr = static_cast<const _Float16*>(a.q) + (int64_t)(seq.begin + tok) * a.q_stride + qhead * kD;
     h8v qf[kSteps];
+    auto load_q = [&](const FewSegment& s) {
+        const int row = min(Rows::row(lane), s.seq.count * a.g - 1);
+        const _Float16* qr = static_cast<const _Float16*>(a.q) + (int64_t)(s.seq.begin + row / a.g) * a.q_stride +
+                             (s.head * a.g + row % a.g) * kD;
 #pragma unroll
-    for (int c = 0; c < kSteps; ++c)
-        qf[c] = query_part(*reinterpret_cast<const u4v*>(qr + Rows::template dim<false>(c, lane)), flip);
-    const ScoreShape<SHAPE> shape(a, qhead);
-    Rows rows(SHAPE ? 1.f : score_factor(a.scale), lane);
-    bool odd = false;  // whether some V there had values that are not finite
-    for (; st < last; st += kPgWaves) {
-        const uint32_t w = bits_to(min(p, len - 1) - st * kCaKeys) & s.there;
-        wave_lds_order();  // the step before has read its V
-#pragma unroll
-        for (int i = 0; i < 8; ++i) put_v(vt, 4 * i + vrow, vchunk, as_h8(s.v[i]));
-        if (__builtin_expect(!__all(w == ~0u), 0)) {
-            uint32_t m = 0u;
-            wave_lds_order();
-#pragma unroll 1
-            for (int i = 0; i < 8; ++i) note_odd(reinterpret_cast<const u4v*>(vt)[64 * i + lane], m);
-            if (__any(m & kOddBits)) {
-                odd = true;
-                clean_v(vt, lane);
-            }
-        }
-        wave_lds_order();
-        rows.scores(qf, [&](int h, int c) { return as_h8(s.k[h * kSteps + c]); });
-        if (st + kPgWaves < last) fetch(st + kPgWaves, s);
-        if constexpr (SHAPE != kPlainScores) {
-            const float from = (float)(st * kCaKeys - p);
-            if constexpr (R == 16)
-                shape.template operator()<8>([&](int i) -> float& { return reinterpret_cast<float*>(rows.s)[i]; },
-                                             [&](int i) { return from + (float)(16 * (i / 4) + 4 * rows.lg + i % 4); });
-            else
-                shape.template operator()<16>([&](int i) -> float& { return reinterpret_cast<float*>(&rows.s)[i]; },
-                                              [&](int i) { return from + (float)(8 * (i / 4) + 4 * rows.half + i % 4); });
-        }
-        rows.accumulate(w, vt, lane);
-    }
+        for (int c = 0; c < kSteps; ++c)
+            qf[c] = query_part(*reinterpret_cast<const u4v*>(qr + Rows::template dim<false>(c, lane)), flip);
+    };
 
-    wave_lds_order();
-    rows.leave(vt, lane, odd);
-    __syncthreads();
-    // Joins the waves' states, 32 lanes a row, 4 dims a lane.
-    const float c2 = rows.c2;
-    const int d4 = tid & 31;
-    for (int r = tid >> 5; r < M; r += kPgThreads / 32) {
-        float top = -__builtin_huge_valf(), l = 0.f;
-        bool some = false;
-        f4v acc{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < kPgWaves; ++w) {
-            const float* of = reinterpret_cast<const float*>(lds(w));
-            top = fmaxf(top, of[R * kCaRow + r]);
-            some |= __builtin_signbit(of[R * (kCaRow + 1) + r]);
+    FewRecord record{-1, 0, 0};
+    if (g.first() + wave < g.last())
+        fetch(g.b, g.head, g.seq.len, g.first() + wave, g.last(), entry_of(g.b, g.first() + wave, g.seq.len));
+    load_q(g);
+    for (;;) {
+        // The segment behind this one, and this wave's first step of it.
+        const int64_t next_x = x + g.part1 - g.part0;
+        bool more = next_x < end;
+        FewSegment n = g;
+        int next_st = 0, next_last = 0, next_entry = 0;
+        if (more) {
+            if (++n.head == a.hkv) {
+                n.head = 0;
+                do {
+                    if (++n.b >= a.batch) break;  // not with lengths that stay as they are
+                    n.seq = scalar_seq(a, n.b);
+                    n.parts = parts_of(n.seq);
+                } while (n.parts == 0);
+                more = n.b < a.batch;
+            }
+            n.part0 = 0;
+            n.part1 = (int)min((int64_t)n.parts, end - next_x);
         }
-        if (top > -__builtin_huge_valf())
+        if (more) {
+            next_st = wave;
+            next_last = n.last();
+            if (next_st < next_last) next_entry = entry_of(n.b, next_st, n.seq.len);
+        }
+
+        const int M = g.seq.count * a.g, len = g.seq.len, last = g.last();
+        const int row = min(Rows::row(lane), M - 1), p = len - g.seq.count + row / a.g;
+        const ScoreShape<SHAPE> shape(a, g.head * a.g + row % a.g);
+        Rows rows(SHAPE ? 1.f : score_factor(a.scale), lane);
+        bool odd = false;  // whether some V there had values that are not finite
+        int st = g.first() + wave;
+        const bool idle = st >= last;  // no step of this segment
+        for (; st < last; st += kPgWaves) {
+            const uint32_t w = bits_to(min(p, len - 1) - st * kCaKeys) & there;
+            wave_lds_order();  // the step before has read its V
+#pragma unroll
+            for (int i = 0; i < 8; ++i) put_v(vt, 4 * i + vrow, vchunk, as_h8(vreg[i]));
+            if (__builtin_expect(!__all(w == ~0u), 0)) {
+                uint32_t m = 0u;
+                wave_lds_order();
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) note_odd(reinterpret_cast<const u4v*>(vt)[64 * i + lane], m);
+                if (__any(m & kOddBits)) {
+                    odd = true;
+                    clean_v(vt, lane);
+                }
+            }
+            wave_lds_order();
+            rows.scores(qf, [&](int h, int c) { return as_h8(kreg[h * kSteps + c]); });
+            const bool here = st + kPgWaves < last;
+            if (here || next_st < next_last)
+                fetch(here ? g.b : n.b, here ? g.head : n.head, here ? len : n.seq.len, here ? st + kPgWaves : next_st,
+                      here ? last : next_last, here ? entry : next_entry);
+            if constexpr (SHAPE != kPlainScores) {
+                const float from = (float)(st * kCaKeys - p);
+                if constexpr (R == 16)
+                    shape.template operator()<8>([&](int i) -> float& { return reinterpret_cast<float*>(rows.s)[i]; },
+                                                 [&](int i) { return from + (float)(16 * (i / 4) + 4 * rows.lg + i % 4); });
+                else
+                    shape.template operator()<16>([&](int i) -> float& { return reinterpret_cast<float*>(&rows.s)[i]; },
+                                                  [&](int i) { return from + (float)(8 * (i / 4) + 4 * rows.half + i % 4); });
+            }
+            rows.accumulate(w, vt, lane);
+        }
+        if (idle && next_st < next_last) fetch(n.b, n.head, n.seq.len, next_st, next_last, next_entry);
+        if (more) load_q(n);
+
+        wave_lds_order();
+        rows.leave(vt, lane, odd);
+        __syncthreads();
+        // Joins the waves' states, 32 lanes a row, 4 dims a lane.
+        const bool whole = g.part0 == 0 && g.part1 == g.parts;
+        const int64_t slot = 2 * id + (g.part0 == 0 ? 1 : 0);
+        if (g.part0 == 0 && !whole) record = FewRecord{g.b, g.head, (int)line.block_of(x + g.parts - 1)};
+        const float c2 = rows.c2;
+        const int d4 = tid & 31;
+        for (int r = tid >> 5; r < M; r += kPgThreads / 32) {
+            float top = -__builtin_huge_valf(), l = 0.f;
+            bool some = false;
+            f4v acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < kPgWaves; ++w) {
                 const float* of = reinterpret_cast<const float*>(lds(w));
-                const float c = rescale(of[R * kCaRow + r], top, c2);
-                l += c * __builtin_fabsf(of[R * (kCaRow + 1) + r]);
-                acc += c * *reinterpret_cast<const f4v*>(of + r * kCaRow + 4 * d4);
+                top = fmaxf(top, of[R * kCaRow + r]);
+                some |= __builtin_signbit(of[R * (kCaRow + 1) + r]);
             }
-        if (part0 == 0 && part1 == parts) {
-            acc *= l > 0.f ? 1.f / l : l;
-            if (some) acc += paged_odd_part(a, b, head, len - seq.count + r / a.g, len, d4);
-            static_cast<h4v*>(a.out)[((int64_t)(seq.begin + r / a.g) * a.hkv * a.g + head * a.g + r % a.g) * (kD / 4) + d4] =
-                h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
-        } else {
-            reinterpret_cast<f4v*>(part)[r * (kD / 4) + d4] = acc;
-            if (d4 == 0) state[r] = float2{top, some ? -l : l};
+            if (top > -__builtin_huge_valf())
+#pragma unroll
+                for (int w = 0; w < kPgWaves; ++w) {
+                    const float* of = reinterpret_cast<const float*>(lds(w));
+                    const float c = rescale(of[R * kCaRow + r], top, c2);
+                    l += c * __builtin_fabsf(of[R * (kCaRow + 1) + r]);
+                    acc += c * *reinterpret_cast<const f4v*>(of + r * kCaRow + 4 * d4);
+                }
+            if (whole) {
+                const int tok = r / a.g;
+                acc *= l > 0.f ? 1.f / l : l;
+                if (some) acc += paged_odd_part(a, g.b, g.head, len - g.seq.count + tok, len, d4);
+                static_cast<h4v*>(a.out)[((int64_t)(g.seq.begin + tok) * a.hkv * a.g + g.head * a.g + r % a.g) * (kD / 4) + d4] =
+                    h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
+            } else {
+                reinterpret_cast<f4v*>(ws.part)[(slot * R + r) * (kD / 4) + d4] = acc;
+                if (d4 == 0) ws.state[slot * R + r] = float2{top, some ? -l : l};
+            }
         }
+        if (!more) return record;
+        __syncthreads();  // the states are read
+        g = n;
+        x = next_x;
     }
 }
 
@@ -353,62 +416,48 @@ __device__ __forceinline__ void few_stretch(const PagedArgs& a, int id, Pick&& p
     const LaneSeqs mine(a);
     PagedSeq seq{};
     int64_t sum = 0, all;
-    for (int b = mine.b0; b < mine.b1; ++b) {
-        seq = paged_seq(a, b);
-        sum += parts_of(seq);
-    }
+    mine.each_of(a, [&](int b, const PagedSeq& s) {
+        seq = s;
+        sum += parts_of(s);
+    });
     const int64_t before = wave_sum_before(sum, &all);
-    FewRecord record{-1, 0, 0};
     const FewLine line(a, all);
-    auto leave = [&]() {
-        if (threadIdx.x == 0) ws.record[id] = record;
-    };
-    if (id >= line.blocks) return leave();
-    int64_t x = line.begin(id);
-    const int64_t end = line.begin(id + 1);
-    const uint64_t who = __ballot(before * a.hkv <= x && x < (before + sum) * a.hkv);
-    if (who == 0) return leave();  // not with lengths that stay as they are
-    const int owner = (int)__builtin_ctzll(who);
-    int64_t at = before;
-    int b = mine.b0;
-    if (mine.each > 1 && (int)(threadIdx.x & 63) == owner)
-        for (; b < mine.b1 - 1; ++b) {
-            seq = paged_seq(a, b);
-            const int n = parts_of(seq);
-            if (x < (at + n) * a.hkv) break;
-            at += n;
-            seq = paged_seq(a, b + 1);
-        }
-    seq = read_lane(seq, owner);
-    b = __builtin_amdgcn_readlane(b, owner);
-    int parts = parts_of(seq);
-    if (parts == 0) return leave();  // as above
-    const int64_t skip = x - read_lane(at, owner) * a.hkv;
-    int head = __builtin_amdgcn_readfirstlane((int)quotient(skip, parts));
-    int part0 = __builtin_amdgcn_readfirstlane((int)(skip - (int64_t)head * parts));
-    int64_t slot = 2 * id;
-    for (;;) {
-        const int part1 = (int)min((int64_t)parts, part0 + (end - x));
-        if (part0 == 0) slot = 2 * id + 1;
-        if (part0 == 0 && part1 < parts) record = FewRecord{b, head, (int)line.block_of(x + parts - 1)};
-        auto attend = [&](auto stream) __attribute__((always_inline)) {
-            few_rows_attend<R, SHAPE, decltype(stream)::value>(a, b, seq, head, part0, part1, parts, lds,
-                                                               ws.part + slot * R * kD, ws.state + slot * R);
-        };
-        line.all > kStreamParts ? attend(std::true_type()) : attend(std::false_type());
-        x += part1 - part0;
-        part0 = 0;
-        if (x >= end) return leave();
-        __syncthreads();  // the states are read
-        if (++head == a.hkv) {
-            head = 0;
-            do {
-                if (++b >= a.batch) return leave();  // as above
-                seq = scalar_seq(a, b);
-                parts = parts_of(seq);
-            } while (parts == 0);
+    FewRecord record{-1, 0, 0};
+    if (id < line.blocks) {
+        const int64_t x = line.begin(id), end = line.begin(id + 1);
+        const bool own = before * a.hkv <= x && x < (before + sum) * a.hkv;
+        const uint64_t who = __ballot(own);
+        if (who != 0) {  // else lengths have changed
+            const int owner = (int)__builtin_ctzll(who);
+            int64_t at = before, found_at = before;
+            int found = mine.b0;
+            if (mine.each > 1 && own)
+                mine.each_of(a, [&](int b, const PagedSeq& s) {
+                    const int n = parts_of(s);
+                    if (at * a.hkv <= x && n > 0) {  // the last of these
+                        found = b;
+                        found_at = at;
+                        seq = s;
+                    }
+                    at += n;
+                });
+            FewSegment g;
+            g.seq = read_lane(seq, owner);
+            g.b = __builtin_amdgcn_readlane(found, owner);
+            g.parts = parts_of(g.seq);
+            if (g.parts > 0) {  // as above
+                const int64_t skip = x - read_lane(found_at, owner) * a.hkv;
+                g.head = min(__builtin_amdgcn_readfirstlane((int)quotient(skip, g.parts)), a.hkv - 1);
+                g.part0 = __builtin_amdgcn_readfirstlane((int)(skip - (int64_t)g.head * g.parts));
+                g.part1 = (int)min((int64_t)g.parts, g.part0 + (end - x));
+                auto walk = [&](auto stream) __attribute__((always_inline)) {
+                    return few_walk<R, SHAPE, decltype(stream)::value>(a, ws, line, id, g, x, end, parts_of, lds);
+                };
+                record = line.all > kStreamParts ? walk(std::true_type()) : walk(std::false_type());
+            }
         }
     }
+    if (threadIdx.x == 0) ws.record[id] = record;
 }
 
 // Joins the states of row r of the head that block id began and did not end: 8 groups of 32 lanes take

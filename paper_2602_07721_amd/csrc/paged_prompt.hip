@@ -148,45 +148,48 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
     PromptStretch out{none, none, PagedSeq{}};
     int64_t work = 0, tokens = 0, items = 0, most = 0, all, all_tokens, all_items;
     PagedSeq s{};
-    for (int b = mine.b0; b < mine.b1; ++b) {
-        s = paged_seq(a, b);
+    mine.each_of(a, [&](int b, const PagedSeq& q) {
+        s = q;
         const PromptCut c(a, s);
         tokens += s.count;
-        if (c.tiles == 0) continue;
+        if (c.tiles == 0) return;
         work += c.cost(c.tiles) * a.hkv;
         items += (int64_t)c.tiles * a.hkv;
         most = max(most, c.base + (int64_t)kPmRows * c.tiles);
-    }
+    });
     const int64_t before = wave_sum_before(work, &all);
     const int64_t first_item = wave_sum_before(items, &all_items);
     wave_sum_before(tokens, &all_tokens);
     if (all == 0 || all_tokens > a.t) return out;  // offsets that do not rise
-    // A sequence of this lane's, found by what is before it.
-    PromptPlace place = none;
-    auto find = [&](int64_t x, int64_t at, auto&& size, auto&& there) {
-        for (int b = mine.b0; b < mine.b1; ++b) {
-            if (mine.each > 1) s = paged_seq(a, b);
-            const PromptCut c(a, s);
-            const int64_t n = size(c) * a.hkv;
-            if (x < at + n) {
-                place = there(b, c, x - at);
-                return;
+    // The sequence of this lane's that has place x of a line: the last that begins there or before.
+    int found = mine.b0;
+    int64_t found_at = 0;
+    auto find = [&](int64_t x, int64_t at, auto&& size) {
+        found_at = at;
+        if (mine.each == 1) return;
+        mine.each_of(a, [&](int b, const PagedSeq& q) {
+            const int64_t n = size(PromptCut(a, q)) * a.hkv;
+            if (at <= x && n > 0) {
+                found = b;
+                found_at = at;
+                s = q;
             }
             at += n;
-        }
+        });
     };
+    PromptPlace place = none;
     const int64_t step = quotient(all, kPgBlocks), rest = all - step * kPgBlocks;
     if (!__any(most > step / 2)) {
         const int64_t id = block;
         const uint64_t who = __ballot(first_item <= id && id < first_item + items);
         if (who == 0) return out;
-        if (first_item <= id && id < first_item + items)
-            find(id, first_item, [&](const PromptCut& c) { return (int64_t)c.tiles; },
-                 [&](int b, const PromptCut& c, int64_t in) {
-                     // Consecutive blocks go to the 8 XCDs in turn, and so do the KV heads: those that
-                     // read the same keys share an L2.
-                     return PromptPlace{b, (int)in % a.hkv, c.tiles - 1 - (int)in / a.hkv, 0};
-                 });
+        if (first_item <= id && id < first_item + items) {
+            find(id, first_item, [](const PromptCut& c) { return (int64_t)c.tiles; });
+            // Consecutive blocks go to the 8 XCDs in turn, and so do the KV heads: those that read the
+            // same keys share an L2.
+            const int in = (int)(id - found_at);
+            place = PromptPlace{found, in % a.hkv, PromptCut(a, s).tiles - 1 - in / a.hkv, 0};
+        }
         const int owner = (int)__builtin_ctzll(who);
         out.begin = out.end = read_lane(place, owner);
         ++out.end.tile;
@@ -199,9 +202,10 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
         const int64_t id = line_block(block) + e, x = id * step + min(id, rest);
         const uint64_t who = __ballot(before <= x && x < before + work);
         if (who == 0) continue;  // the end of the line
-        if (before <= x && x < before + work)
-            find(x, before, [&](const PromptCut& c) { return c.cost(c.tiles); },
-                 [&](int b, const PromptCut& c, int64_t in) { return prompt_place(a, b, s, c, in); });
+        if (before <= x && x < before + work) {
+            find(x, before, [](const PromptCut& c) { return c.cost(c.tiles); });
+            place = prompt_place(a, found, s, PromptCut(a, s), x - found_at);
+        }
         const int owner = (int)__builtin_ctzll(who);
         (e ? out.end : out.begin) = read_lane(place, owner);
         out.seq = read_lane(s, owner);
