@@ -54,7 +54,6 @@ __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, i
     const int tok = (int)((uint32_t)id / per), first = (int)((uint32_t)id % per);
     if (tok >= a.t) return;
     const int slot = a.slots[tok];
-    if (slot < 0 || slot >= a.n_slots) return;
     const int all = kind == 0 ? a.hkv * a.g : a.hkv;
     const __half* from = kind == 0 ? static_cast<const __half*>(a.q) + tok * a.q_stride
                        : kind == 1 ? static_cast<const __half*>(a.k) + tok * a.k_stride
@@ -66,12 +65,6 @@ __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, i
             x[u] = reinterpret_cast<const int4v*>(from + min(h0 + u * (int)per, all - 1) * kD)[c];
     };
     load(first);
-
-    const int page = (int)a.page((uint32_t)slot), size = (int)a.page.d;
-    // Row 0 of the kind, and how far apart its heads' rows are.
-    const int64_t to_row = kind == 0 ? (int64_t)tok * all : (int64_t)page * a.hkv * size + (slot - page * size);
-    const int step = kind == 0 ? 1 : size;
-    int4v* to = static_cast<int4v*>(kind == 0 ? a.q_out : kind == 1 ? a.K : a.V) + to_row * (kD / 8) + c;
 
     // The pairs' other halves, and which halves this lane's are.
     const int half = a.rot / 2;
@@ -105,6 +98,12 @@ __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, i
             fb[i] *= (PAIRS == kHalves ? is_first : i % 2 == 0) ? -si : si;
         }
     }
+    if (slot < 0 || slot >= a.n_slots) return;
+    const int page = (int)a.page((uint32_t)slot), size = (int)a.page.d;
+    // Row 0 of the kind, and how far apart its heads' rows are.
+    const int64_t to_row = kind == 0 ? (int64_t)tok * all : (int64_t)page * a.hkv * size + (slot - page * size);
+    const int step = kind == 0 ? 1 : size;
+    int4v* to = static_cast<int4v*>(kind == 0 ? a.q_out : kind == 1 ? a.K : a.V) + to_row * (kD / 8) + c;
     for (int h0 = first; h0 < all; h0 += kRrAhead * (int)per) {
         int4v y[kRrAhead];
 #pragma unroll
