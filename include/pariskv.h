@@ -634,11 +634,11 @@ typedef struct pariskv_page_step {
  * taken from it.  The pages given back are pushed so that taking as many again
  * takes the same in the same order, sequence after sequence, row after row; the
  * entries behind the free ones are left as they fell.  A sequence gets all of its
- * rows or none: none when they exceed its table (batch tokens before it included:
- * when its tokens do not fit into t), or when the pages wanted by it and by the
- * sequences before it, those granted none for want of pages included, are more
- * than there are.  The table's entries behind a sequence's rows are not read.
- * A page may be in one table only; pages that tables share are the caller's.
+ * rows or none, and keeps what it has: none when its rows would exceed its table,
+ * when its tokens end behind t, or when the pages wanted by it and by the sequences
+ * before it, those that found too few included, are more than there are.  The
+ * table's entries behind a sequence's rows are not read.  A page given back must
+ * not be in another table: pages that tables share are the caller's to count.
  * Errors: INVALID, UNSUPPORTED (batch, t), HIP. */
 int pariskv_plan_pages(const pariskv_page_step* step, void* stream);
 
@@ -667,7 +667,7 @@ int pariskv_rotate_rows(const pariskv_config* cfg, const pariskv_pages* pages, c
                         void* stream);
 
 /* Bytes of a workspace for pariskv_paged_attend with these sizes and every smaller
- * batch, t and max_tokens (at least 256, below 140 MB; 0 on invalid input). */
+ * batch, t and max_tokens (at least 256, below 80 MB; 0 on invalid input). */
 size_t pariskv_paged_workspace(const pariskv_config* cfg, int32_t batch, int64_t t, int64_t max_tokens);
 
 /* Attention of the new tokens of a batch -- one of each sequence, chunks of prompts
@@ -685,7 +685,9 @@ size_t pariskv_paged_workspace(const pariskv_config* cfg, int32_t batch, int64_t
  *            offsets[b] up to offsets[b + 1], at positions up to lens[b] - 1
  *   counts   device int32 [batch], or NULL: sequence b has the first counts[b] of
  *            these only (of none for counts below 0)
- *   max_tokens  the most tokens of a sequence, >= 1; those beyond are not computed
+ *   max_tokens  the most tokens of a sequence, >= 1; one with more has the first
+ *            max_tokens of them only, as with counts
+ *   softcap  0, or 2^-20 to 2^100
  *   slopes   device float [Hq], or NULL
  *   out      device float16 [t][Hq][D]; zero where a token attends nothing; rows of
  *            tokens that no sequence has are left as they were
@@ -694,12 +696,13 @@ size_t pariskv_paged_workspace(const pariskv_config* cfg, int32_t batch, int64_t
  * Only sizes decide what is launched: a captured call holds for any lens, offsets,
  * counts and table later written to the same memory.
  * Scores and sums are float32 (finite scores, as for pariskv_tree_attend; one that
- * is NaN makes its token's output NaN); calls with max_tokens * q_per_kv above 32
- * round weights to float16 and sum them as rounded.  Before it is rounded itself an
- * output is then within 2^-11 of the largest |v| that its token sees, otherwise
- * within 2^-20; twice the scores' float32 rounding (2^-21 softcap with one) and
- * 2^-33 a row come on top.  A row's values, whatever they are, reach only the tokens
- * that attend it, whose dim is then infinite or NaN.
+ * is NaN makes its token's output NaN); in calls with max_tokens * q_per_kv above 32
+ * the weights of sequences with more than 16 rows (tokens times q_per_kv) are rounded
+ * to float16, and summed so.  Before it is rounded itself an output is then within
+ * 2^-11 of the largest |v| that its token sees, otherwise within 2^-20; twice the
+ * scores' float32 rounding (2^-21 softcap with one) and 2^-33 a row come on top.  A
+ * row's values, whatever they are, reach only the tokens that attend it, whose dim is
+ * then infinite or NaN.  The same call gives the same bits again.
  * t = 0 does nothing.
  * Errors: INVALID, UNSUPPORTED (batch above 65535, t above 2^24, more than 2^24
  * blocks), WORKSPACE, HIP. */

@@ -1331,7 +1331,8 @@ int pariskv_paged_attend(const pariskv_config* cfg, const void* q, int64_t q_str
         return fail(PARISKV_ERR_INVALID, "token stride %lld: a multiple of 8 values that holds the heads",
                     (long long)q_stride);
     if (!std::isfinite(scale)) return fail(PARISKV_ERR_INVALID, "scale is not finite");
-    if (!std::isfinite(softcap) || softcap < 0.f) return fail(PARISKV_ERR_INVALID, "softcap is not finite and >= 0");
+    if (softcap != 0.f && !(softcap >= 0x1p-20f && softcap <= 0x1p100f))
+        return fail(PARISKV_ERR_INVALID, "softcap %g is not 0 or 2^-20 to 2^100", softcap);
     if (t == 0) return PARISKV_OK;
     if (!q || !table || !lens || !offsets || !out)
         return fail(PARISKV_ERR_INVALID, "q, table, lens, offsets and out must be non-NULL");

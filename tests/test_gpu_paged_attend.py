@@ -410,3 +410,63 @@ def test_calls_on_two_streams():
         got = [pk.paged_attend(cfg, q, cache, table, lens, offsets, SCALE, max_tokens=m, stream=s) for q, s in zip(qs, streams)]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_pages_past_four_gigabytes():
+    # 9.2 GB of keys and as much of values; the sequences' pages lie in their last part.
+    r = np.random.default_rng(11)
+    hkv, g, page, pages = 8, 2, 64, 70000
+    cfg = config(hkv, g)
+    cache = pk.PagedCache.empty(cfg, pages, page)
+    lens, counts = [700, 100], [1, 40]
+    held = [11, 2]
+    mine = pages - 1 - r.permutation(3000)[:13]
+    table = np.full((2, 12), -1)
+    table[0, :11], table[1, :2] = mine[:11], mine[11:]
+    rows = []
+    for b, n in enumerate(lens):
+        x = r.standard_normal((n, hkv * g + 2 * hkv, D)).astype(np.float16)
+        j = np.arange(n)
+        gx = gpu(x)
+        pk.rotate_rows(cfg, cache, gx[:, :16], gx[:, 16:24], gx[:, 24:], ints(j), ints(table[b, j // page] * page + j % page))
+        rows.append((x[:, 16:24], x[:, 24:]))
+        at = gpu(table[b, j // page].astype(np.int64))
+        assert torch.equal(cache.K[at, :, gpu(j % page)], gx[:, 16:24]) and torch.equal(cache.V[at, :, gpu(j % page)], gx[:, 24:])
+    for most in (1, 40):
+        m = [min(c, most) for c in counts]
+        q = r.standard_normal((sum(m), hkv * g, D)).astype(np.float16)
+        got = pk.paged_attend(cfg, gpu(q), cache, ints(table), ints(lens), ints([0, m[0], sum(m)]), SCALE,
+                              max_tokens=most).cpu().numpy()
+        for b, n in enumerate(lens):
+            lo = 0 if b == 0 else m[0]
+            for h in range(hkv):
+                k, v = (x[:, h] for x in rows[b])
+                qh = q[lo:lo + m[b]].reshape(m[b], hkv, g, D)[:, h]
+                want = attend64(qh, k, v, np.arange(n - m[b], n), np.ones(n, bool), SCALE, 0.0, None)
+                check(got[lo:lo + m[b]].reshape(m[b], hkv, g, D)[:, h], want, tolerance(qh, k, v, SCALE), f"seq {b} head {h}")
+
+
+@pytest.mark.parametrize("most", [1, 40])
+def test_the_widest_batch(most):
+    # 65535 sequences of one row, whose output is its value, and some longer ones among them.
+    r = np.random.default_rng(12)
+    batch, long = 65535, {5: 300, 40000: 70, 65534: 129}
+    cache = pk.PagedCache(*(torch.randn(batch + 50, 1, 16, D, device="cuda").half() for _ in range(2)))
+    table, lens = np.zeros((batch, 19), np.int64), np.ones(batch, np.int64)
+    perm = r.permutation(batch + 50)
+    table[:, 0] = perm[:batch]
+    for b, n in long.items():
+        lens[b] = n
+        table[b, 1:] = r.integers(0, batch + 50, 18)
+    q = torch.randn(batch, 2, D, device="cuda").half()
+    got = pk.paged_attend(config(1, 2), q, cache, ints(table), ints(lens), ints(np.arange(batch + 1)), SCALE, max_tokens=most)
+    one = torch.from_numpy(lens == 1).cuda()
+    v = cache.V[torch.from_numpy(table[:, 0]).cuda(), 0, 0]
+    assert torch.equal(got[one], v[one][:, None].expand(-1, 2, -1))
+    for b, n in long.items():
+        j = np.arange(n)
+        k_, v_ = (x[torch.from_numpy(table[b, j // 16]).cuda(), 0, torch.from_numpy(j % 16).cuda()].cpu().numpy()
+                  for x in (cache.K, cache.V))
+        qb = q[b].cpu().numpy()[None]
+        want = attend64(qb, k_, v_, [n - 1], np.ones(n, bool), SCALE, 0.0, None)
+        check(got[b][None].cpu().numpy(), want, tolerance(qb, k_, v_, SCALE), f"seq {b}")

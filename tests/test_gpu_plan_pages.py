@@ -155,3 +155,12 @@ def test_another_stream():
     want = plan(table, free, n_free, lens, np.full(30, 20), 16, 600)
     for k in NAMES:
         assert np.array_equal(getattr(got, k).cpu().numpy(), want[k]), k
+
+
+def test_the_widest_batch():
+    r = np.random.default_rng(3)
+    batch = 65535
+    table, free, n_free, lens = _state(r, batch, 40, 16, 5000, empty=0.2)
+    counts = np.where(r.random(batch) < 0.1, -lens, 1)
+    _check(table, free, n_free, lens, counts, 16, batch)
+    _check(table, free, n_free, lens, counts, 16, 4000)

@@ -84,7 +84,8 @@ def test_pools_past_31_bits_of_rows_are_refused():
     (dict(lens=FAKE + 2), pk.ERR_INVALID), (dict(offsets=0), pk.ERR_INVALID), (dict(counts=FAKE + 2), pk.ERR_INVALID),
     (dict(slopes=FAKE + 1), pk.ERR_INVALID), (dict(width=0), pk.ERR_INVALID), (dict(width=2 ** 30), pk.ERR_INVALID),
     (dict(qs=1000), pk.ERR_INVALID), (dict(scale=float("inf")), pk.ERR_INVALID), (dict(cap=-1.0), pk.ERR_INVALID),
-    (dict(cap=float("nan")), pk.ERR_INVALID), (dict(most=0), pk.ERR_INVALID), (dict(t=-1), pk.ERR_INVALID),
+    (dict(cap=float("nan")), pk.ERR_INVALID), (dict(cap=1e-7), pk.ERR_INVALID), (dict(cap=1e31), pk.ERR_INVALID),
+    (dict(cap=float("inf")), pk.ERR_INVALID), (dict(most=0), pk.ERR_INVALID), (dict(t=-1), pk.ERR_INVALID),
     (dict(t=2 ** 24 + 1), pk.ERR_UNSUPPORTED), (dict(batch=0), pk.ERR_INVALID), (dict(batch=65536), pk.ERR_UNSUPPORTED),
     (dict(ws=0), pk.ERR_WORKSPACE), (dict(ws=FAKE + 128), pk.ERR_WORKSPACE), (dict(ws_bytes=1000), pk.ERR_WORKSPACE),
     (dict(pages=None), pk.ERR_INVALID), (dict(pages=_pages(n=0)), pk.ERR_INVALID), (dict(pages=_pages(K=FAKE + 4)), pk.ERR_INVALID)])
@@ -109,7 +110,7 @@ def test_no_tokens_do_nothing():
 def test_workspace_sizes_grow_with_the_call():
     cfg = _cfg()
     sizes = [pk.paged_workspace_size(cfg, b, b * m, m) for b, m in ((1, 1), (8, 4), (8, 8), (8, 9), (64, 100), (64, 10000))]
-    assert sizes == sorted(sizes) and sizes[0] >= 256 and sizes[-1] < 140 << 20 and all(x % 256 == 0 for x in sizes)
+    assert sizes == sorted(sizes) and sizes[0] >= 256 and sizes[-1] < 80 << 20 and all(x % 256 == 0 for x in sizes)
     assert pk.paged_workspace_size(cfg, 0, 4, 1) == pk.paged_workspace_size(cfg, 1, -1, 1) == 0
     assert pk.paged_workspace_size(cfg, 3, 0) == 256 and pk.paged_workspace_size(cfg, 1, 4, 0) == 0
 
