@@ -25,7 +25,7 @@
 // blocks that the chip holds as the longest tile of rows has, a block takes a tile, the longest of a
 // sequence first.  Else the tiles, one behind the other, are cut into as many stretches of equal work
 // as the chip holds blocks, wherever the cuts fall, and a second kernel joins the softmax states of
-// the tiles that were cut (at most three halves of a tile a block more through memory). 
+// the tiles that were cut (at most three halves of a tile a block more through memory).
 
 #include <hip/hip_fp16.h>
 
@@ -55,7 +55,6 @@ constexpr int kPmRows = 128;    // rows of a tile
 constexpr int kPmKeys = 64;     // keys of a tile
 constexpr int kPmAhead = 4;     // operands read ahead
 constexpr int kPmFewRows = 16;  // rows of a sequence that is walked as few
-constexpr int kPmJoinRows = 8;  // rows of a joining block at a time
 
 struct FewRows {
     int g;
@@ -86,7 +85,7 @@ __device__ __forceinline__ int tile_keys(const PagedArgs& a, const PagedSeq& s, 
 struct PromptPlace {
     int b, head, tile, key;
 };
-__device__ __forceinline__ PromptPlace read_lane(const PromptPlace& p, int lane) {
+__device__ __forceinline__ PromptPlace read_place(const PromptPlace& p, int lane) {
     return PromptPlace{__builtin_amdgcn_readlane(p.b, lane), __builtin_amdgcn_readlane(p.head, lane),
                        __builtin_amdgcn_readlane(p.tile, lane), __builtin_amdgcn_readlane(p.key, lane)};
 }
@@ -127,7 +126,7 @@ struct PromptRecord {
 constexpr size_t kPmRecordBytes = (kPgBlocks * sizeof(PromptRecord) + 255) / 256 * 256;
 struct PromptSpace {
     PromptRecord* record;  // [kPgBlocks]
-    float* part;           // [2 kPgBlocks][kPmRows][D]
+    float* part;           // [2 kPgBlocks][wave][D / 8][lane][4]: as the waves hold their outputs
     float2* state;         // [2 kPgBlocks][kPmRows]
     __device__ __forceinline__ explicit PromptSpace(const PagedArgs& a) {
         char* p = FewSpace(a, kPmFewRows).end;
@@ -191,25 +190,38 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
             place = PromptPlace{found, in % a.hkv, PromptCut(a, s).tiles - 1 - in / a.hkv, 0};
         }
         const int owner = (int)__builtin_ctzll(who);
-        out.begin = out.end = read_lane(place, owner);
+        out.begin = out.end = read_place(place, owner);
         ++out.end.tile;
         out.seq = read_lane(s, owner);
         return out;
     }
     if (block >= kPgBlocks) return out;
-#pragma unroll 1
-    for (int e = 1; e >= 0; --e) {
+    // Where the stretch begins and where it ends, by two lanes at once.
+    const bool odd_lane = threadIdx.x & 1;
+    int place_b = a.batch;
+    int64_t place_in = 0;
+    PagedSeq place_s{}, begin_s{};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
         const int64_t id = line_block(block) + e, x = id * step + min(id, rest);
         const uint64_t who = __ballot(before <= x && x < before + work);
         if (who == 0) continue;  // the end of the line
-        if (before <= x && x < before + work) {
-            find(x, before, [](const PromptCut& c) { return c.cost(c.tiles); });
-            place = prompt_place(a, found, s, PromptCut(a, s), x - found_at);
-        }
         const int owner = (int)__builtin_ctzll(who);
-        (e ? out.end : out.begin) = read_lane(place, owner);
-        out.seq = read_lane(s, owner);
+        if (before <= x && x < before + work) find(x, before, [](const PromptCut& c) { return c.cost(c.tiles); });
+        const PagedSeq q = read_lane(s, owner);
+        const int b = __builtin_amdgcn_readlane(found, owner);
+        const int64_t in = x - read_lane(found_at, owner);
+        if (e == 0) begin_s = q;
+        if (odd_lane == (e == 1)) {
+            place_b = b;
+            place_in = in;
+            place_s = q;
+        }
     }
+    if (place_b < a.batch) place = prompt_place(a, place_b, place_s, PromptCut(a, place_s), place_in);
+    out.begin = read_place(place, 0);
+    out.end = read_place(place, 1);
+    out.seq = begin_s;
     return out;
 }
 
@@ -317,6 +329,14 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
     const int tkey = 4 * half + ((lane & 15) >> 2);
     const int tchunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 
+    int entry = 0;
+    uint64_t there = 0, next = 0;  // keys of this tile and of the next that have pages
+    auto load_first = [&]() {
+        if (tile0 >= tile1) return;
+        load(place(tile0, entry_of(tile0), there), sk0, sv0);
+        if (tile0 + 1 < tile1) entry = entry_of(tile0 + 1);
+    };
+    load_first();
     if (tid == 0) again = 0;  // seen at the first barrier
     const u4v* qr = reinterpret_cast<const u4v*>(static_cast<const __half*>(a.q) +
                                                  (int64_t)(seq.begin + tok) * a.q_stride + qhead * kD);
@@ -324,8 +344,6 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
 #pragma unroll
     for (int c = 0; c < 8; ++c) qf[c] = query_part(qr[2 * c + half], flip);
 
-    int entry = 0;
-    uint64_t there = 0, next = 0;  // keys of this tile and of the next that have pages
     // Tile `tile`, whose keys lie in ck and cv; loads the next into nk and nv.
     auto take = [&](int tile, const u4v* ck, const u4v* cv, u4v* nk, u4v* nv) __attribute__((always_inline)) {
         if (tile + 1 < tile1) {
@@ -447,12 +465,9 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        if (tile0 < tile1) {
-            load(place(tile0, entry_of(tile0), there), sk0, sv0);
-            if (tile0 + 1 < tile1) entry = entry_of(tile0 + 1);
-            loads_done();
-            clean(tile0, there, sv0);
-        }
+        if (careful) load_first();
+        loads_done();
+        if (careful && tile0 < tile1) clean(tile0, there, sv0);
         __syncthreads();
         for (int tile = tile0; tile < tile1; tile += 2) {
             take(tile, sk0, sv0, sk1, sv1);
@@ -505,12 +520,12 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
                             (_Float16)(o[d][i + 3] * inv)};
         } else {
             const float fix = at_r(r, nm, c2);
-            f4v* out = reinterpret_cast<f4v*>(ws.part) + (slot * kPmRows + row - row0) * (kD / 4);
+            f4v* out = reinterpret_cast<f4v*>(ws.part) + (slot * kPgWaves + wave) * 1024 + lane;
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    out[8 * d + 2 * (i / 4) + half] = f4v{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * fix;
+                    out[(4 * d + i / 4) * 64] = f4v{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * fix;
             if (half == 0) ws.state[slot * kPmRows + row - row0] = float2{left_r(r, l), l * fix};
         }
     }
@@ -532,76 +547,65 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
     if (block < kPgBlocks && threadIdx.x == 0) ws.record[line_block(block)] = record;
 }
 
-// Joins the states of the tile that block id of the line began and did not end: 32 lanes a row, 4 dims
-// a lane, 4 rows at a time, a quarter of the tile a block.
-constexpr int kPmJoinBlocks = 4, kPmJoinTurns = kPmRows / kPmJoinBlocks / kPmJoinRows;
-__device__ __forceinline__ void tile_join(const PagedArgs& a, int shaped, int id, int quarter) {
+// Joins the states of the tile that block id of the line began and did not end, 32 dims a block, every
+// lane what a lane of its number held.
+constexpr int kPmJoinBlocks = kD / 32;
+__device__ __forceinline__ void tile_join(const PagedArgs& a, int shaped, int id, int d) {
     __shared__ int slots[kPgBlocks];
     const PromptSpace ws(a);
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const PromptRecord rec = ws.record[id];
     if (rec.b < 0) return;
     // The block that ends the tile is the first behind with that mark; each between, and it, may have a state.
     int states = 1;
     if (tid == 0) slots[0] = 2 * id + 1;
     for (int i = id + 1; i < kPgBlocks; i += 64) {  // every wave alike
-        const int at = i + (tid & 63), first = at < kPgBlocks ? ws.record[at].first : 0;
+        const int at = i + lane, first = at < kPgBlocks ? ws.record[at].first : 0;
         const uint64_t ends = __ballot(first & kEnds);
         const uint64_t mine = __ballot(first & kMiddle) & (ends ? (2ull << __builtin_ctzll(ends)) - 1 : ~0ull);
-        if (mine >> (tid & 63) & 1) slots[states + __builtin_popcountll(mine & ((1ull << (tid & 63)) - 1))] = 2 * at;
+        if (mine >> lane & 1) slots[states + __builtin_popcountll(mine & ((1ull << lane) - 1))] = 2 * at;
         states += __builtin_popcountll(mine);
         if (ends) break;
     }
     __syncthreads();
     const PagedSeq seq = paged_seq(a, rec.b);
-    const int d4 = tid & 31, M = seq.count * a.g;
-    const int row0 = quarter * kPmJoinTurns * kPmJoinRows + (tid >> 5);  // then every kPmJoinRows-th
+    const int row = rec.tile * kPmRows + 32 * wave + (lane & 31);
+    if (row >= seq.count * a.g) return;
     const float c2 = shaped ? 1.f : score_factor(a.scale);
-    float top[kPmJoinTurns], l[kPmJoinTurns];
-    f4v acc[kPmJoinTurns];
+    float top = -__builtin_huge_valf(), l = 0.f;
+    f4v acc[4];
 #pragma unroll
-    for (int j = 0; j < kPmJoinTurns; ++j) {
-        top[j] = -__builtin_huge_valf();
-        l[j] = 0.f;
-        acc[j] = f4v{0.f, 0.f, 0.f, 0.f};
-    }
-    // Rows behind the last hold what was there; they are not written.
+    for (int j = 0; j < 4; ++j) acc[j] = f4v{0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < states; ++i) {
-        float2 st[kPmJoinTurns];
-        f4v v[kPmJoinTurns];
+        const int64_t slot = slots[i];
+        const float2 st = ws.state[slot * kPmRows + 32 * wave + (lane & 31)];
+        const f4v* part = reinterpret_cast<const f4v*>(ws.part) + (slot * kPgWaves + wave) * 1024 + 4 * d * 64 + lane;
+        f4v v[4];
 #pragma unroll
-        for (int j = 0; j < kPmJoinTurns; ++j) {
-            const int64_t at = (int64_t)slots[i] * kPmRows + row0 + j * kPmJoinRows;
-            st[j] = ws.state[at];
-            v[j] = reinterpret_cast<const f4v*>(ws.part)[at * (kD / 4) + d4];
-        }
+        for (int j = 0; j < 4; ++j) v[j] = part[j * 64];
+        // A share that saw no key that counts left zeros, or values that are not finite.
+        const bool none = st.x == -__builtin_huge_valf();
+        const float to = fmaxf(top, st.x);
+        const float c0 = none ? 1.f : rescale(top, to, c2), c1 = none ? 1.f : rescale(st.x, to, c2);
+        l = l * c0 + (none ? 0.f : st.y * c1);
 #pragma unroll
-        for (int j = 0; j < kPmJoinTurns; ++j) {
-            if (st[j].x == -__builtin_huge_valf()) {  // saw no key that counts: zeros, or values that are not finite
-                acc[j] += v[j];
-                continue;
-            }
-            const float to = fmaxf(top[j], st[j].x);
-            const float c0 = rescale(top[j], to, c2), c1 = rescale(st[j].x, to, c2);
-            l[j] = l[j] * c0 + st[j].y * c1;
-            acc[j] = acc[j] * c0 + v[j] * c1;
-            top[j] = to;
-        }
+        for (int j = 0; j < 4; ++j) acc[j] = acc[j] * c0 + v[j] * c1;
+        top = to;
     }
+    const float inv = l > 0.f ? 1.f / l : l;
+    h4v* out = static_cast<h4v*>(a.out) +
+               ((int64_t)(seq.begin + row / a.g) * a.hkv * a.g + rec.head * a.g + row % a.g) * (kD / 4) + 8 * d + (lane >> 5);
 #pragma unroll
-    for (int j = 0; j < kPmJoinTurns; ++j) {
-        const int at = rec.tile * kPmRows + row0 + j * kPmJoinRows;
-        if (at >= M) break;
-        const f4v o = acc[j] * (l[j] > 0.f ? 1.f / l[j] : l[j]);
-        static_cast<h4v*>(a.out)[((int64_t)(seq.begin + at / a.g) * a.hkv * a.g + rec.head * a.g + at % a.g) * (kD / 4) + d4] =
-            h4v{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
+    for (int j = 0; j < 4; ++j) {
+        const f4v o = acc[j] * inv;
+        out[2 * j] = h4v{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
     }
 }
 
-// Both joins in one launch: a block for every quarter of a tile that may be cut, then one for every row
-// of the sequences of few.
+// Both joins in one launch: four blocks for every tile that may be cut, then one for every row of the
+// sequences of few.
 __global__ __launch_bounds__(32 * kPjGroups) void paged_prompt_join_kernel(PagedArgs a, int shaped) {
-    static_assert(kPjGroups == kPmJoinRows, "blocks of both take as many threads");
+    static_assert(32 * kPjGroups == kPgThreads, "blocks of both take as many threads");
     const int id = (int)blockIdx.x - kPgBlocks * kPmJoinBlocks;
     if (id < 0)
         tile_join(a, shaped, (int)blockIdx.x / kPmJoinBlocks, (int)blockIdx.x % kPmJoinBlocks);
