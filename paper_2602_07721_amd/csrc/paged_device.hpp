@@ -195,7 +195,8 @@ struct FewLine {
 
 // Parts (64 KB of K and V) from which on all that is read cannot stay in the caches until it is read
 // again: it is then read past them.  A step of 4.3 GB takes 637 us so and 715 through the caches, one of
-// 95 MB, read before, 34 and 30.5.
+// 95 MB, read before, 34 and 30.5.  Not so the keys of 32 rows, of which a load takes 32 bytes of 32 lines:
+// 8 tokens of each of 8 sequences of 131072 rows take 652 us with keys through the caches, 805 past them.
 constexpr int64_t kStreamParts = (192 << 20) / (kPfKeys * 4 * kD);
 
 // What a block leaves for the joining kernel: the head that its stretch began and did not end (b < 0:
@@ -277,8 +278,10 @@ __device__ __forceinline__ FewRecord few_walk(const PagedArgs& a, const FewSpace
             const int r = __builtin_amdgcn_ds_bpermute(Rows::key(h, lane) << 2, at);
             const _Float16* k = static_cast<const _Float16*>(a.K) + (int64_t)r * kD;
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c)
-                kreg[h * kSteps + c] = read(reinterpret_cast<const u4v*>(k + Rows::template dim<false>(c, lane)));
+            for (int c = 0; c < kSteps; ++c) {
+                const u4v* part = reinterpret_cast<const u4v*>(k + Rows::template dim<false>(c, lane));
+                kreg[h * kSteps + c] = R == 32 ? *part : read(part);
+            }
         }
         if (st + kPgWaves < last) entry = entry_of(b, st + kPgWaves, len);
     };
