@@ -21,11 +21,12 @@
 // the others' many loads: 5 us for 64 keys that take 1.3 otherwise.
 //
 // How the work is shared out, which every wave finds for itself from sums over the lengths, so a
-// captured call stays right when lengths change: where there is twice as much of it for each of the
-// blocks that the chip holds as the longest tile of rows has, a block takes a tile, the longest of a
-// sequence first.  Else the tiles, one behind the other, are cut into as many stretches of equal work
-// as the chip holds blocks, wherever the cuts fall, and a second kernel joins the softmax states of
-// the tiles that were cut (at most three halves of a tile a block more through memory).
+// captured call stays right when lengths change: a block takes a tile, the longest of a sequence first,
+// or, where that would leave many of them idle at the end, the tiles, one behind the other, are cut into as
+// many stretches of equal work as the chip holds blocks, wherever the cuts fall, and a second kernel joins
+// the softmax states of the tiles that were cut (at most three halves of a tile a block more through
+// memory).  4096 tokens over themselves, 32 heads, take 168 us by tiles and 187 cut; 512 over 32768 745
+// and 310.
 
 #include <hip/hip_fp16.h>
 
@@ -39,7 +40,7 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 
 // 16 bytes a lane from memory straight into LDS, lane i's behind lane i - 1's.  The builtin for 64-bit
 // addresses makes the compiler wait for every LDS read at once as long as one is under way, where here
-// reads are waited for one by one (562 us for 605: 8192 tokens, 32 heads).  What it writes is seen after
+// reads are waited for one by one (565 us for 605: 8192 tokens, 32 heads).  What it writes is seen after
 // loads_done() and a barrier; the compiler's own waits count it in as they are in order.
 __device__ __forceinline__ void load_lds(const void* from, void* to) {
     const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)to);
@@ -145,7 +146,7 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
     const LaneSeqs mine(a);
     const PromptPlace none{a.batch, 0, 0, 0};
     PromptStretch out{none, none, PagedSeq{}};
-    int64_t work = 0, tokens = 0, items = 0, most = 0, all, all_tokens, all_items;
+    int64_t work = 0, tokens = 0, items = 0, most = 0, least = 0, all, all_tokens, all_items;
     PagedSeq s{};
     mine.each_of(a, [&](int b, const PagedSeq& q) {
         s = q;
@@ -155,6 +156,7 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
         work += c.cost(c.tiles) * a.hkv;
         items += (int64_t)c.tiles * a.hkv;
         most = max(most, c.base + (int64_t)kPmRows * c.tiles);
+        least = max(least, c.base + kPmRows);
     });
     const int64_t before = wave_sum_before(work, &all);
     const int64_t first_item = wave_sum_before(items, &all_items);
@@ -178,7 +180,19 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
     };
     PromptPlace place = none;
     const int64_t step = quotient(all, kPgBlocks), rest = all - step * kPgBlocks;
-    if (!__any(most > step / 2)) {
+    // Equal stretches cost a sixteenth more than tiles, and what takes as long as 9 tiles of keys: partial
+    // outputs and their join.  So a tile a block, if neither the longest tile, 3/4 of its cost as blocks
+    // that are alone on a CU are faster, nor the last round of tiles takes that much longer: whether it is
+    // not full, by the shortest tiles, or a sequence begins with its longest there.  Of 39 calls that were
+    // timed both ways one is 10% behind the faster way, the others at most 3%; tiles are up to 2.4 times
+    // slower than cuts, cuts 37% slower than tiles.
+    const int64_t more = step / 16 + 9 * kPmKeys * a.g, last = all_items - kPgBlocks;
+    const int64_t idle = (kPgBlocks - all_items % kPgBlocks) % kPgBlocks;
+    const bool late = mine.each > 1 || first_item >= max(last, (int64_t)1);
+    const bool cut = most - most / 4 > step + more ||
+                     (items > 0 && first_item + items > last &&
+                      (least * idle > more * kPgBlocks || (late && most - most / 4 > work / kPgBlocks + more)));
+    if (!__any(cut)) {
         const int64_t id = block;
         const uint64_t who = __ballot(first_item <= id && id < first_item + items);
         if (who == 0) return out;

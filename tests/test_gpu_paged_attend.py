@@ -169,6 +169,34 @@ def test_wide_batches_of_chunks():
     _run(lens, counts, 2, 2, 16, seed=4)
 
 
+# Tiles of rows whose keys several blocks share: few of them, over many keys.
+@pytest.mark.parametrize("lens,counts,hkv,g", [([6000], [40], 2, 4), ([5000, 30, 7001], [64, 1, 33], 1, 3),
+                                               ([3000, 2500, 2000], [300, 290, 1], 2, 2), ([12000], [130], 1, 16)])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (20.0, False), (0.0, True), (5.0, True)])
+def test_tiles_that_blocks_share(lens, counts, hkv, g, cap, bias):
+    _run(lens, counts, hkv, g, 16, cap=cap, bias=bias, seed=len(lens))
+    lost = [(b, j) for b, n in enumerate(lens) for j in ([0, 3] + list(range(n // 32, n // 32 + 9)) if n > 1000 else [])]
+    _run(lens, counts, hkv, g, 16, cap=cap, bias=bias, lost=lost, seed=7)
+
+
+def test_tiles_that_blocks_share_in_wide_batches():
+    # Several sequences a lane, of which few are long.
+    r = np.random.default_rng(5)
+    lens = [int(x) for x in r.integers(1, 300, 200)]
+    counts = [int(min(x, y)) for x, y in zip(r.integers(0, 40, 200), lens)]
+    for b in (0, 1, 77, 199):
+        lens[b], counts[b] = 9000 + b, 35
+    _run(lens, counts, 1, 2, 16, seed=6)
+
+
+# More tiles of rows than blocks that the chip holds at once: the last round of them full, or not, or begun by another
+# sequence (of equal tiles or not).
+@pytest.mark.parametrize("lens,counts,hkv", [([2048], [2048], 8), ([2100], [2100], 8), ([1500, 1200], [1500, 1200], 8),
+                                             ([3000], [2100], 8), ([700, 2000, 900], [600, 1100, 450], 8)])
+def test_many_tiles(lens, counts, hkv):
+    _run(lens, counts, hkv, 4, 64, seed=3, heads=[0, hkv - 1])
+
+
 @pytest.mark.parametrize("cap,bias", [(20.0, False), (1.0, False), (0.0, True), (30.0, True), (1e4, False)])
 @pytest.mark.parametrize("lens,counts,g", [([500, 33], [1, 1], 4), ([500, 33], [9, 2], 3), ([700, 90], [150, 1], 4)])
 def test_shaped_scores(cap, bias, lens, counts, g):
