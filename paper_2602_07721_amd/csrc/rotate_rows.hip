@@ -28,7 +28,8 @@ typedef int int4v __attribute__((ext_vector_type(4)));
 
 constexpr int kRrThreads = 256, kRrGroups = kRrThreads / 16;
 constexpr int kRrAhead = 4;       // rows whose loads a group has in flight
-constexpr int kRrMostHeads = 8;  // heads of a group
+constexpr int kRrMostHeads = 8;   // heads of a group
+constexpr int kRrFewGroups = 2048;
 
 enum { kNoPairs = 0, kHalves = 1, kNeighbours = 2 };
 
@@ -42,7 +43,7 @@ struct RowGroups {
 };
 
 template <int PAIRS>
-__global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, int heads, bool past) {
+__global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, int heads) {
     const RowGroups gr(a, heads);
     const int c = threadIdx.x & 15;  // dims 8 c .. 8 c + 7 of a row
     // All of q's groups, then k's, then v's: a wave's are of one kind mostly.
@@ -141,9 +142,7 @@ __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, i
             }
             const int h = h0 + u * (int)per;
             if (h >= all) continue;
-            int4v* at = to + (int64_t)h * step * (kD / 8);
-            if (past) __builtin_nontemporal_store(y[u], at);
-            else *at = y[u];
+            to[(int64_t)h * step * (kD / 8)] = y[u];
         }
     }
 }
@@ -151,16 +150,13 @@ __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, i
 }  // namespace
 
 hipError_t launch_rotate_rows(const RotateArgs& a, hipStream_t s) {
-    // As many heads a group as make its sines worth it, but no fewer groups than fill the chip.
-    int heads = kRrMostHeads;
-    while (heads > kRrAhead && RowGroups(a, heads).all(a) < 256 * 8 * kRrGroups) heads /= 2;
+    // 8 heads share a group's sines, in few groups 4, which one group loads at once: 4096 tokens of 32 + 16
+    // heads take 21.0 us with 8 and 27.1 with 4, 32 tokens 7.4 and 6.4, 500 about the same.
+    const int heads = RowGroups(a, kRrMostHeads).all(a) < kRrFewGroups ? kRrAhead : kRrMostHeads;
     const int64_t blocks = (RowGroups(a, heads).all(a) + kRrGroups - 1) / kRrGroups;
-    // Outputs that no cache holds until they are read go past them: 16384 tokens of 48 heads 98.5 -> 92.6 us.
-    const bool past = (int64_t)a.t * (a.hkv * a.g + 2 * a.hkv) * kD * 2 > (64 << 20);
     const ProfEvents pe = prof_begin("rotate_rows");
     auto go = [&](auto kernel) {
-        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRrThreads), 0, s, pe.start, pe.stop, 0, a, heads,
-                              past);
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRrThreads), 0, s, pe.start, pe.stop, 0, a, heads);
     };
     if (a.rot == 0) go(rotate_rows_kernel<kNoPairs>);
     else if (!a.pairs) go(rotate_rows_kernel<kHalves>);
