@@ -228,7 +228,7 @@ hipError_t launch_plan_pages(const PlanArgs& a, hipStream_t s) {
     auto go = [&](auto kernel, int threads) {
         hipExtLaunchKernelGGL(kernel, dim3(1), dim3(threads), 0, s, pe.start, pe.stop, 0, a);
     };
-    // Fewer waves meet at a barrier sooner.
+    // Fewer waves meet at a barrier sooner: 64 sequences 6.1 us by 256 threads, 6.8 by 1024; 256 5.2 and 6.2.
     a.batch <= kPlanFew && a.t <= 4 * kPlanFew ? go(plan_pages_kernel<kPlanFew>, kPlanFew)
                                                : go(plan_pages_kernel<kPlanMost>, kPlanMost);
     const hipError_t e = hipGetLastError();
