@@ -20,6 +20,8 @@ namespace pariskv {
 
 namespace {
 
+// 30 tokens over up to 20011 rows take 221 us with 16 rows and 227 with 32, 40 with biases over up to 4096,
+// 7 heads on a KV head, 31 and 36.
 __host__ __device__ inline int few_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }
 
 struct Everyone {
@@ -50,6 +52,8 @@ size_t paged_plan(PagedArgs& a) {
 
 hipError_t launch_paged_attend(const PagedArgs& a, hipStream_t s) {
     const int64_t rows = (int64_t)a.most * a.g;
+    // 8 tokens of 4 heads a KV head, here and as tiles of rows: of a sequence of 20011 rows 30 and 39 us, of 8
+    // of 131072 651 and 800, of 30 of up to 2011 52 and 55, of up to 20011 285 and 266.
     if (rows > 32) return launch_paged_prompt(a, s);
     const int shape = (a.cap > 0.f ? kCappedScores : 0) | (a.slopes ? kBiasedScores : 0);
     ProfEvents pe = prof_begin("paged_attend");

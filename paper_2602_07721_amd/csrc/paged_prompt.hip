@@ -18,7 +18,8 @@
 // Sequences of at most 16 rows, single tokens mostly, are walked as paged_attend.hip does it instead, by
 // blocks of their own, the first: bound by HBM, they all run at once, and the tiles' blocks follow in the
 // place of those that are done.  Side by side with them from the start, tiles wait for their keys behind
-// the others' many loads: 5 us for 64 keys that take 1.3 otherwise.
+// the others' many loads: 5 us for 64 keys that take 1.3 otherwise.  30 sequences of 3 tokens, 12 rows, take
+// 225 us so and 250 as tiles, single tokens 229 and 239.
 //
 // How the work is shared out, which every wave finds for itself from sums over the lengths, so a
 // captured call stays right when lengths change: a block takes a tile, the longest of a sequence first,
