@@ -551,10 +551,7 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
         place_now.tile = 0;
         if (++place_now.head == a.hkv) {
             place_now.head = 0;
-            do {
-                if (++place_now.b >= a.batch) break;
-                seq = scalar_seq(a, place_now.b);
-            } while (PromptCut(a, seq).tiles == 0);
+            place_now.b = next_seq(a, place_now.b + 1, seq, [&](const PagedSeq& s) { return PromptCut(a, s).tiles > 0; });
         }
     }
     __syncthreads();  // LDS is read

@@ -104,6 +104,19 @@ def test_sequences_without_tokens_and_without_rows():
     _run([0, 0, 0], [0, 0, 0], 2, 2, 16, most=40)
 
 
+@pytest.mark.parametrize("batch,step", [(40, 7), (300, 64), (300, 65), (1000, 333)])
+def test_batches_of_mostly_empty_places(batch, step):
+    # Every step-th place has a sequence; of those between some have rows, but no new tokens.
+    lens = [3 * (b % 5) for b in range(batch)]
+    for m in (1, 40):
+        counts = [0] * batch
+        for b in range(step // 2, batch, step):
+            lens[b], counts[b] = 700 + b, m
+        _run(lens, counts, 2, 2, 16, seed=m)
+        counts[step // 2] = 1
+        _run(lens, counts, 2, 2, 16, seed=m, most=40)
+
+
 @pytest.mark.parametrize("most", [4, 100])
 def test_tokens_that_attend_nothing_give_zeros(most):
     # No row at all, and more tokens than rows: those at positions below 0 see nothing.
