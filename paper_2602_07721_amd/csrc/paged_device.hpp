@@ -472,8 +472,8 @@ __device__ __forceinline__ void few_stretch(const PagedArgs& a, int id, Pick&& p
 }
 
 // Joins the states of row r of the head that block id began and did not end: 8 groups of 32 lanes take
-// every eighth block, 4 dims a lane.
-constexpr int kPjGroups = 8;
+// every eighth block, 4 dims a lane, the states of kPjAhead blocks on their way at a time.
+constexpr int kPjGroups = 8, kPjAhead = 8;
 __device__ __forceinline__ void few_join(const PagedArgs& a, int rows, float c2, int id, int r) {
     __shared__ f4v so[kPjGroups][32];
     __shared__ float sr[kPjGroups], sl[kPjGroups];
@@ -487,17 +487,27 @@ __device__ __forceinline__ void few_join(const PagedArgs& a, int rows, float c2,
     bool odd = false;
     float top = -__builtin_huge_valf(), l = 0.f;
     f4v acc{0.f, 0.f, 0.f, 0.f};
-    for (int i = id + sub; i <= rec.last; i += kPjGroups) {
-        const int64_t at = (int64_t)(2 * i + (i == id ? 1 : 0)) * rows + r;
-        const float2 st = ws.state[at];
-        const f4v v = reinterpret_cast<const f4v*>(ws.part)[at * (kD / 4) + d4];
-        if (st.x == -__builtin_huge_valf()) continue;  // saw no key
-        odd |= __builtin_signbit(st.y);
-        const float to = fmaxf(top, st.x);
-        const float c0 = rescale(top, to, c2), c1 = rescale(st.x, to, c2);
-        l = l * c0 + __builtin_fabsf(st.y) * c1;
-        acc = acc * c0 + v * c1;
-        top = to;
+    for (int i0 = id + sub; i0 <= rec.last; i0 += kPjGroups * kPjAhead) {
+        float2 st[kPjAhead];
+        f4v v[kPjAhead];
+#pragma unroll
+        for (int u = 0; u < kPjAhead; ++u) {
+            const int i = i0 + u * kPjGroups;
+            if (i > rec.last) continue;
+            const int64_t at = (int64_t)(2 * i + (i == id ? 1 : 0)) * rows + r;
+            st[u] = ws.state[at];
+            v[u] = reinterpret_cast<const f4v*>(ws.part)[at * (kD / 4) + d4];
+        }
+#pragma unroll
+        for (int u = 0; u < kPjAhead; ++u) {
+            if (i0 + u * kPjGroups > rec.last || st[u].x == -__builtin_huge_valf()) continue;  // saw no key
+            odd |= __builtin_signbit(st[u].y);
+            const float to = fmaxf(top, st[u].x);
+            const float c0 = rescale(top, to, c2), c1 = rescale(st[u].x, to, c2);
+            l = l * c0 + __builtin_fabsf(st[u].y) * c1;
+            acc = acc * c0 + v[u] * c1;
+            top = to;
+        }
     }
     so[sub][d4] = acc;
     if (d4 == 0) {

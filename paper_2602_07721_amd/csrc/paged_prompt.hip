@@ -559,19 +559,48 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
     if (block < kPgBlocks && threadIdx.x == 0) ws.record[line_block(block)] = record;
 }
 
-// Joins the states of the tile that block id of the line began and did not end, 32 dims a block, every
-// lane what a lane of its number held.
-constexpr int kPmJoinBlocks = kD / 32;
+// Adds a share's state of a row, reference and sum, and some dims of its output to those so far.  One that saw
+// no key that counts left zeros, or values that are not finite.
+template <int N>
+__device__ __forceinline__ void add_state(float2 st, const f4v (&v)[N], float c2, float& top, float& l, f4v (&acc)[N]) {
+    const bool none = st.x == -__builtin_huge_valf();
+    const float to = fmaxf(top, st.x);
+    const float c0 = none ? 1.f : rescale(top, to, c2), c1 = none ? 1.f : rescale(st.x, to, c2);
+    l = l * c0 + (none ? 0.f : st.y * c1);
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = acc[j] * c0 + v[j] * c1;
+    top = to;
+}
+
+// Joins the states of the tiles that blocks of the line began and did not end: joining block (id, d) the
+// dims 32 d on of the tile that block id began, every lane what a lane of its number held.  Where at least
+// kPmManyStates blocks had a tile's keys, the joining blocks of the first so many, which have no tile of their
+// own, share it: each 8 dims of 32 rows, its waves every fourth state (16 tokens of 8 heads over 131072 rows,
+// 512 states: 195 us by the first alone).
+constexpr int kPmJoinBlocks = kD / 32, kPmManyStates = 16, kPmJoinAhead = 8;
+static_assert(kPmManyStates * kPmJoinBlocks == kPmRows / 32 * (kD / 8), "one part each");
 __device__ __forceinline__ void tile_join(const PagedArgs& a, int shaped, int id, int d) {
     __shared__ int slots[kPgBlocks];
+    __shared__ f4v so[kPgWaves][64][1];
+    __shared__ float2 ss[kPgWaves][32];
     const PromptSpace ws(a);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const PromptRecord rec = ws.record[id];
-    if (rec.b < 0) return;
+    // The tile begun last by a block up to this one, kPmManyStates - 1 before it at most, and whether as many
+    // blocks behind that one have nothing but its keys.
+    const int near = id - (kPmManyStates - 1) + lane;
+    const PromptRecord none{-1, 0, 0, 0}, about = near >= 0 && near < kPgBlocks ? ws.record[near] : none;
+    const uint64_t begun = __ballot(about.b >= 0) & ((1ull << kPmManyStates) - 1);
+    const uint64_t inside = __ballot(about.first == kMiddle);
+    if (begun == 0) return;
+    const int at_begin = 63 - __builtin_clzll(begun), begin = id - (kPmManyStates - 1) + at_begin;
+    constexpr uint64_t kOthers = (1ull << (kPmManyStates - 1)) - 1;
+    const bool many = (inside >> (at_begin + 1) & kOthers) == kOthers;
+    if (begin < id && !many) return;
+    const PromptRecord rec = ws.record[begin];
     // The block that ends the tile is the first behind with that mark; each between, and it, may have a state.
     int states = 1;
-    if (tid == 0) slots[0] = 2 * id + 1;
-    for (int i = id + 1; i < kPgBlocks; i += 64) {  // every wave alike
+    if (tid == 0) slots[0] = 2 * begin + 1;
+    for (int i = begin + 1; i < kPgBlocks; i += 64) {  // every wave alike
         const int at = i + lane, first = at < kPgBlocks ? ws.record[at].first : 0;
         const uint64_t ends = __ballot(first & kEnds);
         const uint64_t mine = __ballot(first & kMiddle) & (ends ? (2ull << __builtin_ctzll(ends)) - 1 : ~0ull);
@@ -581,10 +610,46 @@ __device__ __forceinline__ void tile_join(const PagedArgs& a, int shaped, int id
     }
     __syncthreads();
     const PagedSeq seq = paged_seq(a, rec.b);
-    const int row = rec.tile * kPmRows + 32 * wave + (lane & 31);
-    if (row >= seq.count * a.g) return;
     const float c2 = shaped ? 1.f : score_factor(a.scale);
+    const int M = seq.count * a.g;
+    h4v* const outs = static_cast<h4v*>(a.out);
+    // Where the 4 dims 8 c + 4 half on of row `row` lie.
+    auto place = [&](int row, int c) {
+        return ((int64_t)(seq.begin + row / a.g) * a.hkv * a.g + rec.head * a.g + row % a.g) * (kD / 4) + 2 * c + (lane >> 5);
+    };
+    auto rounded = [](f4v o) { return h4v{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]}; };
     float top = -__builtin_huge_valf(), l = 0.f;
+    if (many) {
+        const int part = (id - begin) * kPmJoinBlocks + d, w = part / (kD / 8), c = part % (kD / 8);
+        const int row = rec.tile * kPmRows + 32 * w + (lane & 31);
+        f4v acc[1] = {f4v{0.f, 0.f, 0.f, 0.f}};
+        for (int i0 = wave; i0 < states; i0 += kPgWaves * kPmJoinAhead) {
+            float2 st[kPmJoinAhead];
+            f4v v[kPmJoinAhead][1];
+#pragma unroll
+            for (int u = 0; u < kPmJoinAhead; ++u) {
+                const int i = i0 + kPgWaves * u;
+                const int64_t slot = slots[min(i, states - 1)];
+                st[u] = ws.state[slot * kPmRows + 32 * w + (lane & 31)];
+                v[u][0] = reinterpret_cast<const f4v*>(ws.part)[(slot * kPgWaves + w) * 1024 + c * 64 + lane];
+            }
+#pragma unroll
+            for (int u = 0; u < kPmJoinAhead; ++u) {
+                if (i0 + kPgWaves * u >= states) break;
+                add_state(st[u], v[u], c2, top, l, acc);
+            }
+        }
+        so[wave][lane][0] = acc[0];
+        if (lane < 32) ss[wave][lane] = float2{top, l};
+        __syncthreads();
+        if (wave != 0 || row >= M) return;
+#pragma unroll
+        for (int x = 1; x < kPgWaves; ++x) add_state(ss[x][lane & 31], so[x][lane], c2, top, l, acc);
+        outs[place(row, c)] = rounded(acc[0] * (l > 0.f ? 1.f / l : l));
+        return;
+    }
+    const int row = rec.tile * kPmRows + 32 * wave + (lane & 31);
+    if (row >= M) return;
     f4v acc[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[j] = f4v{0.f, 0.f, 0.f, 0.f};
@@ -595,23 +660,11 @@ __device__ __forceinline__ void tile_join(const PagedArgs& a, int shaped, int id
         f4v v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = part[j * 64];
-        // A share that saw no key that counts left zeros, or values that are not finite.
-        const bool none = st.x == -__builtin_huge_valf();
-        const float to = fmaxf(top, st.x);
-        const float c0 = none ? 1.f : rescale(top, to, c2), c1 = none ? 1.f : rescale(st.x, to, c2);
-        l = l * c0 + (none ? 0.f : st.y * c1);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = acc[j] * c0 + v[j] * c1;
-        top = to;
+        add_state(st, v, c2, top, l, acc);
     }
     const float inv = l > 0.f ? 1.f / l : l;
-    h4v* out = static_cast<h4v*>(a.out) +
-               ((int64_t)(seq.begin + row / a.g) * a.hkv * a.g + rec.head * a.g + row % a.g) * (kD / 4) + 8 * d + (lane >> 5);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const f4v o = acc[j] * inv;
-        out[2 * j] = h4v{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
-    }
+    for (int j = 0; j < 4; ++j) outs[place(row, 4 * d + j)] = rounded(acc[j] * inv);
 }
 
 // Both joins in one launch: four blocks for every tile that may be cut, then one for every row of the

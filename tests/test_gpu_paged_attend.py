@@ -192,6 +192,19 @@ def test_tiles_that_blocks_share(lens, counts, hkv, g, cap, bias):
     _run(lens, counts, hkv, g, 16, cap=cap, bias=bias, lost=lost, seed=7)
 
 
+@pytest.mark.parametrize("lens,counts", [([8000], [1200]), ([9000, 6000], [300, 700])])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_tiles_that_few_blocks_share(lens, counts, cap):
+    _run(lens, counts, 2, 4, 16, cap=cap, seed=9, heads=[1], lost=[(0, j) for j in range(40, 60)])
+
+
+@pytest.mark.parametrize("n,m,hkv,g", [(30000, 1, 1, 4), (30000, 4, 1, 8), (70000, 20, 1, 4), (33000, 3, 2, 16)])
+def test_one_long_sequence(n, m, hkv, g):
+    # All blocks share the keys of a head or two.
+    _run([n], [m], hkv, g, 16, seed=m)
+    _run([n], [m], hkv, g, 16, seed=m, lost=[(0, j) for j in range(200, 900)])
+
+
 def test_tiles_that_blocks_share_in_wide_batches():
     # Several sequences a lane, of which few are long.
     r = np.random.default_rng(5)
