@@ -31,7 +31,7 @@ struct Everyone {
 template <int R, int SHAPE>
 __global__ __launch_bounds__(kPgThreads, 2) void paged_few_kernel(PagedArgs a) {
     __shared__ __attribute__((aligned(16))) unsigned char lds[kPgWaves * few_wave_lds(R)];
-    few_stretch<R, SHAPE>(a, a.blocks == kPgBlocks ? line_block(blockIdx.x) : (int)blockIdx.x, Everyone(),
+    few_stretch<R, SHAPE>(a, a.blocks == kPgBlocks ? line_block(blockIdx.x, kPgBlocks) : (int)blockIdx.x, Everyone(),
                              [&](int w) { return lds + w * few_wave_lds(R); });
 }
 

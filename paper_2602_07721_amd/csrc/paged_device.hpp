@@ -169,9 +169,9 @@ struct LaneSeqs {
     }
 };
 
-// Which stretch of a line a block takes: consecutive blocks go to the 8 XCDs in turn, and each XCD
-// takes one length of the line, whose neighbours read the same keys.
-__device__ __forceinline__ int line_block(uint32_t block) { return (int)(block % 8 * (kPgBlocks / 8) + block / 8); }
+// Which of a line's stretches, a multiple of 8, a block takes: consecutive blocks go to the 8 XCDs in turn,
+// and each XCD takes one length of the line, whose neighbours read the same keys.
+__device__ __forceinline__ int line_block(uint32_t block, int blocks) { return (int)(block % 8 * (blocks / 8) + block / 8); }
 
 // The quotient of numbers that mostly fit 32 bits.
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {

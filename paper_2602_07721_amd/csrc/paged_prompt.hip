@@ -24,10 +24,10 @@
 // How the work is shared out, which every wave finds for itself from sums over the lengths, so a
 // captured call stays right when lengths change: a block takes a tile, the longest of a sequence first,
 // or, where that would leave many of them idle at the end, the tiles, one behind the other, are cut into as
-// many stretches of equal work as the chip holds blocks, wherever the cuts fall, and a second kernel joins
-// the softmax states of the tiles that were cut (at most three halves of a tile a block more through
-// memory).  4096 tokens over themselves, 32 heads, take 168 us by tiles and 187 cut; 512 over 32768 745
-// and 310.
+// many stretches of equal work as the chip holds blocks (fewer if they were short), wherever the cuts fall,
+// and a second kernel joins the softmax states of the tiles that were cut (at most two halves of tiles a
+// block through memory).  4096 tokens over themselves, 32 heads, take 165 us by tiles and 184 cut; 512 over
+// 32768 800 and 310.
 
 #include <hip/hip_fp16.h>
 
@@ -138,15 +138,21 @@ struct PromptSpace {
     }
 };
 
-// The stretch of a block, from one place up to another, and the sequence that it begins in.
+// The stretch of a block, from one place up to another, the sequence that it begins in, and which of the
+// line it is.
 struct PromptStretch {
     PromptPlace begin, end;
     PagedSeq seq;
+    int id;
 };
+// Stretches that a tile is cut into at most, and tiles of keys of a stretch at least, on average: more stretches
+// take longer to join than they save.  16 tokens of 8 heads take 56 us over 131072 rows and 26 over 8000, with 512
+// stretches 80 and 55; 32 tokens of 8 x 4 heads over 3000 28 and 51.
+constexpr int kPmShares = 128, kPmLeast = 4;
 __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint32_t block) {
     const LaneSeqs mine(a);
     const PromptPlace none{a.batch, 0, 0, 0};
-    PromptStretch out{none, none, PagedSeq{}};
+    PromptStretch out{none, none, PagedSeq{}, (int)block};
     int64_t work = 0, tokens = 0, items = 0, most = 0, least = 0, all, all_tokens, all_items;
     PagedSeq s{};
     mine.each_of(a, [&](int b, const PagedSeq& q) {
@@ -180,13 +186,13 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
         });
     };
     PromptPlace place = none;
-    const int64_t step = quotient(all, kPgBlocks), rest = all - step * kPgBlocks;
+    const int64_t step = quotient(all, kPgBlocks);
     // Equal stretches cost a sixteenth more than tiles, and what takes as long as 9 tiles of keys: partial
     // outputs and their join.  So a tile a block, if neither the longest tile, 3/4 of its cost as blocks
     // that are alone on a CU are faster, nor the last round of tiles takes that much longer: whether it is
-    // not full, by the shortest tiles, or a sequence begins with its longest there.  Of 39 calls that were
-    // timed both ways one is 10% behind the faster way, the others at most 3%; tiles are up to 2.4 times
-    // slower than cuts, cuts 37% slower than tiles.
+    // not full, by the shortest tiles, or a sequence begins with its longest there.  Of 44 calls that were
+    // timed both ways one is 11% behind the faster way, the others at most 4%; tiles take up to 6 times as long
+    // as cuts, cuts up to 23% longer than tiles.
     const int64_t more = step / 16 + 9 * kPmKeys * a.g, last = all_items - kPgBlocks;
     const int64_t idle = (kPgBlocks - all_items % kPgBlocks) % kPgBlocks;
     const bool late = mine.each > 1 || first_item >= max(last, (int64_t)1);
@@ -210,7 +216,11 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
         out.seq = read_lane(s, owner);
         return out;
     }
-    if (block >= kPgBlocks) return out;
+    const int64_t shares = quotient(all, kPmLeast * kPmKeys * a.g) & ~7ll;
+    const int blocks = (int)min(min(kPmShares * all_items, max(shares, (int64_t)8)), (int64_t)kPgBlocks);
+    if (block >= blocks) return out;
+    out.id = line_block(block, blocks);
+    const int64_t each = quotient(all, blocks), rest = all - each * blocks;
     // Where the stretch begins and where it ends, by two lanes at once.
     const bool odd_lane = threadIdx.x & 1;
     int place_b = a.batch;
@@ -218,7 +228,7 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
     PagedSeq place_s{}, begin_s{};
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int64_t id = line_block(block) + e, x = id * step + min(id, rest);
+        const int64_t id = out.id + e, x = id * each + min(id, rest);
         const uint64_t who = __ballot(before <= x && x < before + work);
         if (who == 0) continue;  // the end of the line
         const int owner = (int)__builtin_ctzll(who);
@@ -248,7 +258,7 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
     static_assert(few_wave_lds(kPmFewRows) <= (int)sizeof sk0, "a wave's share of few rows takes one of them");
     __shared__ int again;  // whether a wave has outputs that are not finite
     if (blockIdx.x < kPgBlocks) {
-        few_stretch<kPmFewRows, SHAPE>(a, line_block(blockIdx.x), FewRows{a.g}, [&](int w) {
+        few_stretch<kPmFewRows, SHAPE>(a, line_block(blockIdx.x, kPgBlocks), FewRows{a.g}, [&](int w) {
             return reinterpret_cast<unsigned char*>(w == 0 ? sk0 : w == 1 ? sk1 : w == 2 ? sv0 : sv1);
         });
         return;
@@ -266,7 +276,7 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
     const bool last_one = b == end.b && head == end.head && place_now.tile == end.tile;
     const int tile0 = place_now.key, tile1 = last_one ? end.key : keys;
     const bool whole = tile0 == 0 && tile1 == keys;
-    const int64_t slot = 2 * line_block(block) + (tile0 > 0 ? 0 : 1);
+    const int64_t slot = 2 * stretch.id + (tile0 > 0 ? 0 : 1);
     if (!whole) {
         if (tile0 > 0) record.first = kMiddle | (tile1 == keys ? kEnds : 0);
         else record = PromptRecord{b, head, place_now.tile, record.first};
@@ -556,7 +566,7 @@ __global__ __launch_bounds__(kPgThreads, 2) void paged_prompt_kernel(PagedArgs a
     }
     __syncthreads();  // LDS is read
     }
-    if (block < kPgBlocks && threadIdx.x == 0) ws.record[line_block(block)] = record;
+    if (block < kPgBlocks && threadIdx.x == 0) ws.record[stretch.id] = record;
 }
 
 // Adds a share's state of a row, reference and sum, and some dims of its output to those so far.  One that saw
