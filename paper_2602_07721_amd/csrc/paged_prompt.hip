@@ -153,22 +153,24 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
     const LaneSeqs mine(a);
     const PromptPlace none{a.batch, 0, 0, 0};
     PromptStretch out{none, none, PagedSeq{}, (int)block};
-    int64_t work = 0, tokens = 0, items = 0, most = 0, least = 0, all, all_tokens, all_items;
+    int64_t work = 0, most = 0, least = 0, all;
+    int tokens = 0, items = 0;  // tokens up to t + 1; with at most t, no more tiles than blocks were launched
     PagedSeq s{};
     mine.each_of(a, [&](int b, const PagedSeq& q) {
         s = q;
         const PromptCut c(a, s);
-        tokens += s.count;
+        tokens = min(tokens + s.count, a.t + 1);
         if (c.tiles == 0) return;
         work += c.cost(c.tiles) * a.hkv;
-        items += (int64_t)c.tiles * a.hkv;
+        items = (int)((uint32_t)items + (uint32_t)c.tiles * (uint32_t)a.hkv);
         most = max(most, c.base + (int64_t)kPmRows * c.tiles);
         least = max(least, c.base + kPmRows);
     });
     const int64_t before = wave_sum_before(work, &all);
-    const int64_t first_item = wave_sum_before(items, &all_items);
-    wave_sum_before(tokens, &all_tokens);
-    if (all == 0 || all_tokens > a.t) return out;  // offsets that do not rise
+    if (all == 0 || __builtin_amdgcn_readlane((int)wave_incl_sum((uint32_t)tokens), 63) > a.t)
+        return out;  // the second: offsets that do not rise
+    const int items_to = (int)wave_incl_sum((uint32_t)items), first_item = items_to - items;
+    const int all_items = __builtin_amdgcn_readlane(items_to, 63);
     // The sequence of this lane's that has place x of a line: the last that begins there or before.
     int found = mine.b0;
     int64_t found_at = 0;
@@ -190,20 +192,20 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
     // Equal stretches cost a sixteenth more than tiles, and what takes as long as 9 tiles of keys: partial
     // outputs and their join.  So a tile a block, if neither the longest tile, 3/4 of its cost as blocks
     // that are alone on a CU are faster, nor the last round of tiles takes that much longer: whether it is
-    // not full, by the shortest tiles, or a sequence begins with its longest there.  Of 44 calls that were
-    // timed both ways one is 11% behind the faster way, the others at most 4%; tiles take up to 6 times as long
-    // as cuts, cuts up to 23% longer than tiles.
-    const int64_t more = step / 16 + 9 * kPmKeys * a.g, last = all_items - kPgBlocks;
-    const int64_t idle = (kPgBlocks - all_items % kPgBlocks) % kPgBlocks;
-    const bool late = mine.each > 1 || first_item >= max(last, (int64_t)1);
+    // not full, by half of the shortest tiles' cost, or a sequence begins there, its longest tiles first.
+    // Of 98 calls that were timed both ways the taken one is 1.3% behind the faster on average, 13% at worst; tiles
+    // take up to 6 times as long as cuts, cuts up to 28% longer than tiles.
+    const int64_t more = step / 16 + 9 * kPmKeys * a.g;
+    const int last = all_items - kPgBlocks, idle = -all_items & (kPgBlocks - 1);
+    const bool late = first_item + (mine.each > 1 ? items : 1) > max(last, kPgBlocks);
     const bool cut = most - most / 4 > step + more ||
-                     (items > 0 && first_item + items > last &&
-                      (least * idle > more * kPgBlocks || (late && most - most / 4 > work / kPgBlocks + more)));
+                     (items > 0 && items_to > last &&
+                      (least / 2 * idle > more * kPgBlocks || (late && most - most / 4 > (all - before) / kPgBlocks + more)));
     if (!__any(cut)) {
-        const int64_t id = block;
-        const uint64_t who = __ballot(first_item <= id && id < first_item + items);
+        const int id = (int)block;
+        const uint64_t who = __ballot(first_item <= id && id < items_to);
         if (who == 0) return out;
-        if (first_item <= id && id < first_item + items) {
+        if (first_item <= id && id < items_to) {
             find(id, first_item, [](const PromptCut& c) { return (int64_t)c.tiles; });
             // Consecutive blocks go to the 8 XCDs in turn, and so do the KV heads: those that read the
             // same keys share an L2.
@@ -217,7 +219,7 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
         return out;
     }
     const int64_t shares = quotient(all, kPmLeast * kPmKeys * a.g) & ~7ll;
-    const int blocks = (int)min(min(kPmShares * all_items, max(shares, (int64_t)8)), (int64_t)kPgBlocks);
+    const int blocks = (int)min(min((int64_t)kPmShares * all_items, max(shares, (int64_t)8)), (int64_t)kPgBlocks);
     if (block >= blocks) return out;
     out.id = line_block(block, blocks);
     const int64_t each = quotient(all, blocks), rest = all - each * blocks;
