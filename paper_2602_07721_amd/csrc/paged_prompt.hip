@@ -193,8 +193,8 @@ __device__ __forceinline__ PromptStretch prompt_stretch(const PagedArgs& a, uint
     // outputs and their join.  So a tile a block, if neither the longest tile, 3/4 of its cost as blocks
     // that are alone on a CU are faster, nor the last round of tiles takes that much longer: whether it is
     // not full, by half of the shortest tiles' cost, or a sequence begins there, its longest tiles first.
-    // Of 98 calls that were timed both ways the taken one is 1.3% behind the faster on average, 13% at worst; tiles
-    // take up to 6 times as long as cuts, cuts up to 28% longer than tiles.
+    // Of 98 calls that were timed both ways the taken one is 1.3% behind the faster on average, 13% at worst;
+    // tiles take up to 6 times as long as cuts, cuts up to 28% longer than tiles.
     const int64_t more = step / 16 + 9 * kPmKeys * a.g;
     const int last = all_items - kPgBlocks, idle = -all_items & (kPgBlocks - 1);
     const bool late = first_item + (mine.each > 1 ? items : 1) > max(last, kPgBlocks);
