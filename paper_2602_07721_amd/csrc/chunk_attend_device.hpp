@@ -341,6 +341,12 @@ struct ChunkRows<16> {
         }
     }
 
+    // Adds the values of a row of V that are not finite to this lane's outputs.
+    __device__ __forceinline__ void add_odd_values(const h4v* v) {
+#pragma unroll
+        for (int d = 0; d < 8; ++d) add_odd(o[d], v[4 * d + lg]);
+    }
+
     // Leaves the state in ca_state_bytes(16) of LDS; the sums' signs say `odd`.
     __device__ __forceinline__ void leave(unsigned char* to, int lane, bool odd) const {
         float* so = reinterpret_cast<float*>(to);
@@ -429,6 +435,18 @@ struct ChunkRows<32> {
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo, o[d], 0, 0, 0);
             }
         }
+    }
+
+    __device__ __forceinline__ void add_odd_values(const h4v* v) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f4v part{0.f, 0.f, 0.f, 0.f};
+                add_odd(part, v[8 * d + 2 * j + half]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][4 * j + i] += part[i];
+            }
     }
 
     __device__ __forceinline__ void leave(unsigned char* to, int lane, bool odd) const {

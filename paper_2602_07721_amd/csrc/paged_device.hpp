@@ -89,17 +89,6 @@ struct ScoreShape {
     }
 };
 
-// Values of V that are not finite, of the keys that a row at position p sees, dims 4 d4 on.
-__device__ __forceinline__ f4v paged_odd_part(const PagedArgs& a, int b, int head, int p, int len, int d4) {
-    f4v sum{0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j <= min(p, len - 1); ++j) {
-        const int entry = page_entry(a, b, j);
-        if ((uint32_t)entry >= (uint32_t)a.n_pages) continue;
-        add_odd(sum, static_cast<const h4v*>(a.V)[(int64_t)page_row(a, entry, head, j) * (kD / 4) + d4]);
-    }
-    return sum;
-}
-
 // Sum over the lanes before this one and over all, of values of 0 to 2^57: their bits in three parts
 // whose sums fit 32, which are moved between lanes in registers.
 __device__ __forceinline__ int64_t wave_sum_before(int64_t v, int64_t* all) {
@@ -238,6 +227,12 @@ constexpr int few_wave_lds(int rows) {
     return kCaKeys * kD * 2 > ca_state_bytes(rows) ? kCaKeys * kD * 2 : ca_state_bytes(rows);
 }
 
+// What the sum and the outputs of a state at r are multiplied by when they are joined at `to` >= r.  One that saw
+// no key that counts has a sum of 0, and outputs of 0 or values that are not finite: they stay what they are.
+__device__ __forceinline__ float state_factor(float r, float to, float c2) {
+    return r == -__builtin_huge_valf() ? 1.f : rescale(r, to, c2);
+}
+
 // What a block takes of a head at a time: parts [part0, part1) of the keys of its M = count g rows.
 struct FewSegment {
     int b, head, part0, part1, parts;
@@ -250,8 +245,12 @@ struct FewSegment {
 
 // Walks segments from g, at place x of the line, up to `end`.  lds(w): few_wave_lds(R) bytes of wave w,
 // 16-byte aligned.  A head's outputs where its parts are all here, else states: row r's outputs, its
-// reference and sum, negative where paged_odd_part has something to add.  A wave's next step, of this
-// segment or of the next, is on its way while one is computed on and while segments end.
+// reference and sum.  A wave's next step, of this segment or of the next, is on its way while one is
+// computed on and while segments end.
+//
+// Values of V that are not finite are taken out of a step that not every row sees whole.  The rows that
+// see them get them from memory when the segment ends: of the steps from the first to the last that held
+// some (131067 rows of one head, 4 rows: 29.4 us; with an infinity in the last 30.6, in the last 27 39.5).
 template <int R, int SHAPE, bool STREAM, class Parts, class Lds>
 __device__ __forceinline__ FewRecord few_walk(const PagedArgs& a, const FewSpace& ws, const FewLine& line, int id,
                                               FewSegment g, int64_t x, int64_t end, Parts&& parts_of, Lds&& lds) {
@@ -336,7 +335,7 @@ __device__ __forceinline__ FewRecord few_walk(const PagedArgs& a, const FewSpace
         const int row = min(Rows::row(lane), M - 1), p = len - g.seq.count + row / a.g;
         const ScoreShape<SHAPE> shape(a, g.head * a.g + row % a.g);
         Rows rows(SHAPE ? 1.f : score_factor(a.scale), lane);
-        bool odd = false;  // whether some V there had values that are not finite
+        int odd_first = 0, odd_last = -1;  // the steps whose V had values that are not finite taken out
         int st = g.first() + wave;
         const bool idle = st >= last;  // no step of this segment
         for (; st < last; st += kPgWaves) {
@@ -350,7 +349,8 @@ __device__ __forceinline__ FewRecord few_walk(const PagedArgs& a, const FewSpace
 #pragma unroll 1
                 for (int i = 0; i < 8; ++i) note_odd(reinterpret_cast<const u4v*>(vt)[64 * i + lane], m);
                 if (__any(m & kOddBits)) {
-                    odd = true;
+                    if (odd_last < 0) odd_first = st;
+                    odd_last = st;
                     clean_v(vt, lane);
                 }
             }
@@ -374,8 +374,32 @@ __device__ __forceinline__ FewRecord few_walk(const PagedArgs& a, const FewSpace
         if (idle && next_st < next_last) fetch(n.b, n.head, n.seq.len, next_st, next_last, next_entry);
         if (more) load_q(n);
 
+#pragma unroll 1
+        for (int odd = odd_first; odd <= odd_last; odd += kPgWaves) {
+            const int key = key_row(odd, len), e = page_entry(a, g.b, key);
+            const bool good = (uint32_t)e < (uint32_t)a.n_pages;
+            const int at = good ? page_row(a, e, g.head, key) : 0;
+            const uint32_t w = bits_to(min(p, len - 1) - odd * kCaKeys) & (uint32_t)__ballot(good);
+            if (__all(w == ~0u)) continue;  // the products had them
+            uint32_t keys = 0;  // with such values
+#pragma unroll 4
+            for (int i = 0; i < 8; ++i) {
+                const int r = __builtin_amdgcn_ds_bpermute((4 * i + vrow) << 2, at);
+                uint32_t m = 0u;
+                note_odd(*(reinterpret_cast<const u4v*>(static_cast<const _Float16*>(a.V) + (int64_t)r * kD) + vchunk), m);
+                const uint64_t who = __ballot(m & kOddBits);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) keys |= (who >> (16 * j) & 0xffff) != 0 ? 1u << (4 * i + j) : 0u;
+            }
+#pragma unroll 1
+            for (; keys != 0; keys &= keys - 1) {
+                const int k = __builtin_ctz(keys);
+                const h4v* v = static_cast<const h4v*>(a.V) + (int64_t)__builtin_amdgcn_readlane(at, k) * (kD / 4);
+                if (w >> k & 1) rows.add_odd_values(v);
+            }
+        }
         wave_lds_order();
-        rows.leave(vt, lane, odd);
+        rows.leave(vt, lane, false);
         __syncthreads();
         // Joins the waves' states, 32 lanes a row, 4 dims a lane.
         const bool whole = g.part0 == 0 && g.part1 == g.parts;
@@ -385,31 +409,24 @@ __device__ __forceinline__ FewRecord few_walk(const PagedArgs& a, const FewSpace
         const int d4 = tid & 31;
         for (int r = tid >> 5; r < M; r += kPgThreads / 32) {
             float top = -__builtin_huge_valf(), l = 0.f;
-            bool some = false;
             f4v acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kPgWaves; ++w) top = fmaxf(top, reinterpret_cast<const float*>(lds(w))[R * kCaRow + r]);
 #pragma unroll
             for (int w = 0; w < kPgWaves; ++w) {
                 const float* of = reinterpret_cast<const float*>(lds(w));
-                top = fmaxf(top, of[R * kCaRow + r]);
-                some |= __builtin_signbit(of[R * (kCaRow + 1) + r]);
+                const float c = state_factor(of[R * kCaRow + r], top, c2);
+                l += c * of[R * (kCaRow + 1) + r];
+                acc += c * *reinterpret_cast<const f4v*>(of + r * kCaRow + 4 * d4);
             }
-            if (top > -__builtin_huge_valf())
-#pragma unroll
-                for (int w = 0; w < kPgWaves; ++w) {
-                    const float* of = reinterpret_cast<const float*>(lds(w));
-                    const float c = rescale(of[R * kCaRow + r], top, c2);
-                    l += c * __builtin_fabsf(of[R * (kCaRow + 1) + r]);
-                    acc += c * *reinterpret_cast<const f4v*>(of + r * kCaRow + 4 * d4);
-                }
             if (whole) {
                 const int tok = r / a.g;
                 acc *= l > 0.f ? 1.f / l : l;
-                if (some) acc += paged_odd_part(a, g.b, g.head, len - g.seq.count + tok, len, d4);
                 static_cast<h4v*>(a.out)[((int64_t)(g.seq.begin + tok) * a.hkv * a.g + g.head * a.g + r % a.g) * (kD / 4) + d4] =
                     h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
             } else {
                 reinterpret_cast<f4v*>(ws.part)[(slot * R + r) * (kD / 4) + d4] = acc;
-                if (d4 == 0) ws.state[slot * R + r] = float2{top, some ? -l : l};
+                if (d4 == 0) ws.state[slot * R + r] = float2{top, l};
             }
         }
         if (!more) return record;
@@ -484,7 +501,6 @@ __device__ __forceinline__ void few_join(const PagedArgs& a, int rows, float c2,
     const PagedSeq seq = paged_seq(a, b);
     if (r >= seq.count * a.g) return;
     const int d4 = threadIdx.x & 31, sub = threadIdx.x >> 5;
-    bool odd = false;
     float top = -__builtin_huge_valf(), l = 0.f;
     f4v acc{0.f, 0.f, 0.f, 0.f};
     for (int i0 = id + sub; i0 <= rec.last; i0 += kPjGroups * kPjAhead) {
@@ -500,11 +516,10 @@ __device__ __forceinline__ void few_join(const PagedArgs& a, int rows, float c2,
         }
 #pragma unroll
         for (int u = 0; u < kPjAhead; ++u) {
-            if (i0 + u * kPjGroups > rec.last || st[u].x == -__builtin_huge_valf()) continue;  // saw no key
-            odd |= __builtin_signbit(st[u].y);
+            if (i0 + u * kPjGroups > rec.last) continue;
             const float to = fmaxf(top, st[u].x);
-            const float c0 = rescale(top, to, c2), c1 = rescale(st[u].x, to, c2);
-            l = l * c0 + __builtin_fabsf(st[u].y) * c1;
+            const float c0 = state_factor(top, to, c2), c1 = state_factor(st[u].x, to, c2);
+            l = l * c0 + st[u].y * c1;
             acc = acc * c0 + v[u] * c1;
             top = to;
         }
@@ -512,29 +527,23 @@ __device__ __forceinline__ void few_join(const PagedArgs& a, int rows, float c2,
     so[sub][d4] = acc;
     if (d4 == 0) {
         sr[sub] = top;
-        sl[sub] = odd ? -l : l;
+        sl[sub] = l;
     }
     __syncthreads();
     if (sub != 0) return;
     top = -__builtin_huge_valf();
     l = 0.f;
     acc = f4v{0.f, 0.f, 0.f, 0.f};
-    odd = false;
+#pragma unroll
+    for (int i = 0; i < kPjGroups; ++i) top = fmaxf(top, sr[i]);
 #pragma unroll
     for (int i = 0; i < kPjGroups; ++i) {
-        top = fmaxf(top, sr[i]);
-        odd |= __builtin_signbit(sl[i]);
+        const float c = state_factor(sr[i], top, c2);
+        l += c * sl[i];
+        acc += c * so[i][d4];
     }
-    if (top > -__builtin_huge_valf())
-#pragma unroll
-        for (int i = 0; i < kPjGroups; ++i) {
-            const float c = rescale(sr[i], top, c2);
-            l += c * __builtin_fabsf(sl[i]);
-            acc += c * so[i][d4];
-        }
     acc *= l > 0.f ? 1.f / l : l;
     const int tok = r / a.g;
-    if (odd) acc += paged_odd_part(a, b, head, seq.len - seq.count + tok, seq.len, d4);
     static_cast<h4v*>(a.out)[((int64_t)(seq.begin + tok) * a.hkv * a.g + head * a.g + r % a.g) * (kD / 4) + d4] =
         h4v{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
 }
