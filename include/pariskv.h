@@ -700,7 +700,8 @@ size_t pariskv_paged_workspace(const pariskv_config* cfg, int32_t batch, int64_t
  * the weights of sequences with more than 16 rows (tokens times q_per_kv) are rounded
  * to float16, and summed so.  Before it is rounded itself an output is then within
  * 2^-11 of the largest |v| that its token sees, otherwise within 2^-20; twice the
- * scores' float32 rounding (2^-21 softcap with one) and 2^-33 a row come on top.  A
+ * scores' float32 rounding (with a softcap up to 64, 2^-21 of it; with a larger one,
+ * 2^-18 of the capped score) and 2^-33 a row come on top.  A
  * row's values, whatever they are, reach only the tokens that attend it, whose dim is
  * then infinite or NaN.  The same call gives the same bits again.
  * t = 0 does nothing.

@@ -55,16 +55,15 @@ hipError_t launch_paged_attend(const PagedArgs& a, hipStream_t s) {
     // 8 tokens of 4 heads a KV head, here and as tiles of rows: of a sequence of 20011 rows 30 and 39 us, of 8
     // of 131072 651 and 800, of 30 of up to 2011 52 and 55, of up to 20011 285 and 266.
     if (rows > 32) return launch_paged_prompt(a, s);
-    const int shape = (a.cap > 0.f ? kCappedScores : 0) | (a.slopes ? kBiasedScores : 0);
+    const int shape = score_shape(a);
     ProfEvents pe = prof_begin("paged_attend");
     auto go = [&](auto kernel) {
         hipExtLaunchKernelGGL(kernel, dim3((unsigned)a.blocks), dim3(kPgThreads), 0, s, pe.start, pe.stop, 0, a);
     };
-    auto by_rows = [&](auto k16, auto k32) { few_rows(rows) == 16 ? go(k16) : go(k32); };
-    if (shape == kPlainScores) by_rows(paged_few_kernel<16, 0>, paged_few_kernel<32, 0>);
-    else if (shape == kCappedScores) by_rows(paged_few_kernel<16, 1>, paged_few_kernel<32, 1>);
-    else if (shape == kBiasedScores) by_rows(paged_few_kernel<16, 2>, paged_few_kernel<32, 2>);
-    else by_rows(paged_few_kernel<16, 3>, paged_few_kernel<32, 3>);
+    by_shape(shape, [&](auto x) {
+        constexpr int kShape = decltype(x)::value;
+        few_rows(rows) == 16 ? go(paged_few_kernel<16, kShape>) : go(paged_few_kernel<32, kShape>);
+    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.blocks == 1) return e;
     pe = prof_begin("paged_join");

@@ -33,8 +33,24 @@ __device__ __forceinline__ int page_row(const PagedArgs& a, int entry, int head,
     return (entry * a.hkv + head) * size + (row - (int)a.page((uint32_t)row) * size);
 }
 
-// What is done to scores before their softmax.
-enum { kPlainScores = 0, kCappedScores = 1, kBiasedScores = 2 };
+// What is done to scores before their softmax.  Caps above kWaveCap have forms of their own.
+enum { kPlainScores = 0, kCappedScores = 1, kBiasedScores = 2, kLargeCap = 4 };
+constexpr float kWaveCap = 64.f;
+inline int score_shape(const PagedArgs& a) {
+    return (a.cap > 0.f ? kCappedScores : 0) | (a.slopes ? kBiasedScores : 0) | (a.cap > kWaveCap ? kLargeCap : 0);
+}
+// f(std::integral_constant of the shape)
+template <class F>
+void by_shape(int shape, F&& f) {
+    switch (shape) {
+        case 1: return f(std::integral_constant<int, 1>());
+        case 2: return f(std::integral_constant<int, 2>());
+        case 3: return f(std::integral_constant<int, 3>());
+        case 5: return f(std::integral_constant<int, 5>());
+        case 7: return f(std::integral_constant<int, 7>());
+        default: return f(std::integral_constant<int, 0>());
+    }
+}
 
 // With a shape, scores are in powers of two: s' = cap log2(e) tanh(scale s / cap), or the plain
 // product, plus slope log2(e) times the distance.
@@ -51,12 +67,24 @@ struct ScoreShape {
     // Of a lane's N scores, which the functions give for their numbers: the score, and how far its key is
     // behind the token (negative).
     //
-    // Where all of a wave's |u| are below 0.2, a series, within 2^-24 of tanh(u), in five instructions of
-    // the vector unit; else tanh(u) = 1 - 2 / (2^(2 log2(e) u) + 1), within 2^-23 of 1, with two that take
-    // four times as long.  8192 tokens, 32 heads, cap 30: 867 us with both for every score.
+    // Where all of a wave's |u| are below 0.2, a series, within 2^-22 of itself, in five instructions of
+    // the vector unit; else tanh(u) = 1 - 2 / (2^(2 log2(e) u) + 1), within 2^-21 of 1, with two that take
+    // four times as long.  8192 tokens, 32 heads, cap 30: 716 to 760 us so, 867 with the second for every score.
+    // So a wave's other scores, those of keys that a row does not see among them, decide on 2^-21 of the cap:
+    // up to a cap of 64 at most 2^-15 of a weight.  Above it each score takes its own of the two (917 us where 716 are taken so).
     template <int N, class Score, class Distance>
     __device__ __forceinline__ void operator()(Score&& score, Distance&& distance) const {
         if constexpr ((SHAPE & kCappedScores) != 0) {
+            auto near = [&](float u) {
+                const float u2 = u * u;
+                float x = __builtin_fmaf(u2, cap * -0.053968254f, cap * 0.13333334f);
+                x = __builtin_fmaf(u2, x, cap * -0.33333334f);
+                return u * __builtin_fmaf(u2, x, cap);
+            };
+            auto far = [&](float u) {
+                const float e = __builtin_amdgcn_exp2f(u * 2.8853900817779268f);
+                return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(e + 1.f), cap);
+            };
             float top = 0.f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -65,17 +93,12 @@ struct ScoreShape {
             }
             if (__all(top < 0.2f)) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float u = score(i), u2 = u * u;
-                    float x = __builtin_fmaf(u2, cap * -0.053968254f, cap * 0.13333334f);
-                    x = __builtin_fmaf(u2, x, cap * -0.33333334f);
-                    score(i) = u * __builtin_fmaf(u2, x, cap);
-                }
+                for (int i = 0; i < N; ++i) score(i) = near(score(i));
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(score(i) * 2.8853900817779268f);
-                    score(i) = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(e + 1.f), cap);
+                    const float u = score(i);
+                    score(i) = (SHAPE & kLargeCap) != 0 && __builtin_fabsf(u) < 0.2f ? near(u) : far(u);
                 }
             }
         } else {

@@ -697,7 +697,7 @@ size_t paged_prompt_bytes(const PagedArgs& a) {
 }
 
 hipError_t launch_paged_prompt(const PagedArgs& a, hipStream_t s) {
-    const int shape = (a.cap > 0.f ? kCappedScores : 0) | (a.slopes ? kBiasedScores : 0);
+    const int shape = score_shape(a);
     // At most so many tiles of rows.
     const int64_t some = a.batch < a.t ? a.batch : a.t;
     const int64_t tiles = ((int64_t)a.t * a.g / kPmRows + some) * a.hkv;
@@ -706,10 +706,7 @@ hipError_t launch_paged_prompt(const PagedArgs& a, hipStream_t s) {
         hipExtLaunchKernelGGL(kernel, dim3((unsigned)(kPgBlocks + (tiles > kPgBlocks ? tiles : kPgBlocks))), dim3(kPgThreads), 0, s,
                               pe.start, pe.stop, 0, a);
     };
-    if (shape == kPlainScores) go(paged_prompt_kernel<0>);
-    else if (shape == kCappedScores) go(paged_prompt_kernel<1>);
-    else if (shape == kBiasedScores) go(paged_prompt_kernel<2>);
-    else go(paged_prompt_kernel<3>);
+    by_shape(shape, [&](auto x) { go(paged_prompt_kernel<decltype(x)::value>); });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     pe = prof_begin("paged_join");
