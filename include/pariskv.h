@@ -626,7 +626,8 @@ typedef struct pariskv_page_step {
                            sequences (granted or not); at most t                  */
     int32_t* granted;   /* [batch] counts[b], or 0 (see below); may be counts     */
     int32_t* slots;     /* [t] where each token's row belongs; -1 for tokens that
-                           were not granted and behind the last                   */
+                           were not granted, behind the last, and in pages that
+                           are none (below 0, or with slots past 2^31 - 1)        */
     int32_t* positions; /* [t] its row in its sequence; -1 likewise               */
 } pariskv_page_step;
 

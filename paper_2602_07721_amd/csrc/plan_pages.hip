@@ -80,6 +80,12 @@ __device__ __forceinline__ Ask ask_of(const PlanArgs& a, int b) {
     return k;
 }
 
+// The slot of row `in` of a page; -1 for a page below 0 and for a slot past 31 bits, which would wrap to another page's.
+__device__ __forceinline__ int slot_of(const PlanArgs& a, int page, int in) {
+    const int64_t slot = (int64_t)page * a.page.d + in;
+    return page >= 0 && slot <= INT32_MAX ? (int)slot : -1;
+}
+
 // Slot and position of token i: its sequence is the last whose offset is not behind it.
 template <class Offset>
 __device__ __forceinline__ void fill_token(const PlanArgs& a, int i, Offset&& offset) {
@@ -100,7 +106,7 @@ __device__ __forceinline__ void fill_token(const PlanArgs& a, int i, Offset&& of
         if (at < n) {
             pos = a.new_lens[lo] - n + at;
             const uint32_t j = a.page((uint32_t)pos);
-            slot = a.table[lo * a.width + j] * (int)a.page.d + (pos - (int)(j * a.page.d));
+            slot = slot_of(a, a.table[lo * a.width + j], pos - (int)(j * a.page.d));
         }
     }
     a.slots[i] = slot;
@@ -179,7 +185,7 @@ __global__ __launch_bounds__(THREADS) void plan_pages_kernel(PlanArgs a) {
             // A decode step's token: its page is at hand, or the last one held.
             if (place && k.fresh == 1 && end <= (uint32_t)a.t) {
                 if (ok && takes == 0) page = row[k.held - 1];
-                a.slots[end - 1] = ok ? page * (int)a.page.d + (int)(k.len - a.page(k.len) * a.page.d) : -1;
+                a.slots[end - 1] = ok ? slot_of(a, page, (int)(k.len - a.page(k.len) * a.page.d)) : -1;
                 a.positions[end - 1] = ok ? (int)k.len : -1;
             }
             far |= k.fresh > 1;
