@@ -40,9 +40,12 @@ __device__ __forceinline__ h8v join_h4(s4v a, s4v b) {
 __device__ __forceinline__ h8v query_part(u4v v, uint32_t flip) {
     return as_h8(v ^ flip);
 }
-// A score's factor in powers of two.  A scale of 0 weighs every score alike, as this does.
+// A score's factor in powers of two.  A scale of 0 weighs every score alike, as this does.  Scores times the
+// largest finite factor are alike, or so far apart that a larger one weighs them no other way; an infinite
+// one would make NaNs of products that are 0.
+constexpr float kMostFactor = 0x1.fffffep127f;
 __device__ __forceinline__ float score_factor(float scale) {
-    return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f);
+    return fminf(fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f), kMostFactor);
 }
 
 // A row's weights are P = 2^(c2 (s - r) + kUp): s its scores, c2 their factor, and r one of them, near

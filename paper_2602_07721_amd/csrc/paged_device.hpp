@@ -60,9 +60,14 @@ struct ScoreShape {
     __device__ __forceinline__ ScoreShape(const PagedArgs& a, int head) {
         constexpr float kLog2e = 1.4426950408889634f;
         const float scale = fabsf(a.scale);
-        unit = SHAPE & kCappedScores ? scale / a.cap : scale * kLog2e;
+        // Finite, as score_factor's.
+        unit = fminf(SHAPE & kCappedScores ? scale / a.cap : scale * kLog2e, kMostFactor);
         cap = SHAPE & kCappedScores ? a.cap * kLog2e : 0.f;
-        slope = SHAPE & kBiasedScores ? a.slopes[head] * kLog2e : 0.f;
+        slope = 0.f;
+        if constexpr ((SHAPE & kBiasedScores) != 0) {
+            const float x = a.slopes[head];
+            slope = __builtin_fabsf(x) <= kMostFactor ? fminf(fmaxf(x * kLog2e, -kMostFactor), kMostFactor) : x;
+        }
     }
     // Of a lane's N scores, which the functions give for their numbers: the score, and how far its key is
     // behind the token (negative).

@@ -74,3 +74,44 @@ def test_caps_on_both_sides_of_the_change_of_form(cap, m, g, bias):
     k, v = (x[:, 0] for x in pool.rows[0])
     want = attend64(q, k, v, np.arange(n - m, n), np.ones(n, bool), SCALE, cap, slopes)
     check(got, want, tolerance(q, k, v, SCALE, cap, slopes), f"cap {cap}")
+
+
+@pytest.mark.parametrize("m,g", [(1, 4), (8, 4), (60, 2)])
+@pytest.mark.parametrize("scale,cap,slope", [(3e38, 0.0, None), (-3e38, 0.0, None), (3e38, 0.0, 0.5), (1e37, 2.0 ** -20, None),
+                                             (1e37, 2.0 ** -20, 0.25), (SCALE, 0.0, 3e38)])
+def test_factors_past_the_largest_float32(m, g, scale, cap, slope):
+    # Finite scales, slopes and scores, whose factors log2(e) scale, scale / softcap and log2(e) slope are not.  Products
+    # of query and key are 2^-20 times whole numbers, so without a cap scores are alike or so far apart that all weight
+    # lies on the largest; with it they are -cap, 0 and cap.  What is left is the roundings of weights and outputs.
+    n = 90
+    print(f"[paged] scale {scale} cap {cap} slope {slope} {m} tokens g {g}", flush=True)
+    r = np.random.default_rng(m)
+    pool = Pool(r, 1, [n], 16)
+    for j in range(n):
+        k = np.zeros(D, np.float16)
+        k[0] = r.integers(-3, 4) / 1024
+        _set_key(pool, 0, j, k)
+    q = np.zeros((m, g, D), np.float16)
+    q[:, :, 0] = r.choice([-1, 1], (m, g)) / 1024
+    slopes = None if slope is None else np.full(g, slope, np.float32)
+    got = _run(pool, q, [0, m], 1, g, cap, slopes, scale=scale)
+    k, v = (x[:, 0] for x in pool.rows[0])
+    want = attend64(q, k, v, np.arange(n - m, n), np.ones(n, bool), scale, cap, slopes)
+    rel = 2.0 ** -10 + 2.0 ** -19 + (2 * 2.0 ** -21 * cap if cap else 0.0)
+    if cap and slope:  # biases to slope n, rounded with their sum: see tolerance()
+        rel += 2 * 2.0 ** -23 * (2 * cap + 40 + cap)
+    check(got, want, rel * np.abs(v.astype(np.float64)).max(), f"scale {scale}")
+
+
+@pytest.mark.parametrize("m", [1, 40])
+def test_dense_forms_take_the_same_scales(m):
+    r = np.random.default_rng(m)
+    n, g = 90, 4
+    K = np.zeros((1, 1, n, D), np.float16)
+    K[..., 0] = r.integers(-3, 4, n) / 1024
+    V = r.standard_normal((1, 1, n, D)).astype(np.float16)
+    q = np.zeros((1, g, m, D), np.float16)
+    q[..., 0] = r.choice([-1, 1], (g, m)) / 1024
+    got = pk.sink_window_attend(config(1, g), gpu(q), gpu(K), gpu(V), n - m, 0, n, 3e38).cpu().numpy()
+    want = attend64(q[0].transpose(1, 0, 2), K[0, 0], V[0, 0], np.arange(n - m, n), np.ones(n, bool), 3e38, 0.0, None)
+    check(got[0].transpose(1, 0, 2), want, (2.0 ** -10 + 2.0 ** -19) * np.abs(V.astype(np.float64)).max(), f"{m} tokens")
