@@ -653,8 +653,9 @@ int pariskv_plan_pages(const pariskv_page_step* step, void* stream);
  *              nothing is done (its row of q_out too is left as it was).  Slots
  *              must differ: of equal ones any token's row may stay, or parts
  *   freqs      device float [rot_dim / 2], radians a position: pair i turns by
- *              positions * freqs[i], whole turns taken off in 64 bits (exact to
- *              float32's rounding while that is below 2^31)
+ *              positions * freqs[i], whole turns taken off in two numbers of 64
+ *              bits (what is left is exact to float32's rounding while the angle
+ *              is below 2^31, its sine and cosine to 2^-22)
  *   rot_dim    dims that are rotated, the first ones: a multiple of 16 up to D
  *   pairs      0: dims i and i + rot_dim / 2 are pair i; 1: dims 2 i and 2 i + 1
  *   q_weight, k_weight  device float [D], or NULL: no norm

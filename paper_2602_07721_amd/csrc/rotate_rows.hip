@@ -4,9 +4,9 @@
 //   y = x w / sqrt(mean(x^2) + eps)
 //   (a, b) -> (a cos - b sin, b cos + a sin)   for the pairs of the first `rot` dims
 //
-// Everything in float32, rounded once.  An angle is position * frequency in 64 bits, less its whole
-// turns, before it is rounded to float32: 4 million positions on, float32 would be off by a quarter
-// radian.
+// Everything in float32, rounded once.  An angle is position * frequency in two numbers of 64 bits, less
+// its whole turns, before it is rounded to float32: 4 million positions on, float32 would be off by a
+// quarter radian; near 2^31 radians one number of 64 bits is off by up to 2^-21.9.
 //
 // Bound by HBM: 512 bytes a row of q, k and v.  16 lanes take some heads of one kind of a token, 16 bytes
 // a lane, 4 rows at a time and the next 4 on their way: the norm's sum is four lane moves, a pair's other
@@ -41,6 +41,14 @@ struct RowGroups {
         : q((a.hkv * a.g + n - 1) / n), kv((a.hkv + n - 1) / n) {}
     __host__ __device__ int64_t all(const RotateArgs& a) const { return (int64_t)a.t * (q + 2 * kv); }
 };
+
+// p f / (2 pi) less the nearest whole number, from -1/2 to 1/2: what the product and 1 / (2 pi) leave in 64
+// bits is added at the end.
+__device__ __forceinline__ float turns_of(double p, double f) {
+    constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;  // 1 / (2 pi)
+    const double angle = p * f, whole = rint(angle * kTurn);
+    return (float)(fma(angle, kTurn, -whole) + fma(angle, kTurnRest, fma(p, f, -angle) * kTurn));
+}
 
 template <int PAIRS>
 __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, int heads) {
@@ -89,9 +97,8 @@ __global__ __launch_bounds__(kRrThreads) void rotate_rows_kernel(RotateArgs a, i
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (PAIRS == kHalves || i % 2 == 0) {
-                const double turn = p * (double)a.freqs[f0 + (PAIRS == kHalves ? i : i / 2)] * 0.15915494309189535;
                 // In turns; within 2^-22.9 of sine and cosine over 2^24 values of half a turn either way.
-                const float x = (float)(turn - rint(turn));
+                const float x = turns_of(p, a.freqs[f0 + (PAIRS == kHalves ? i : i / 2)]);
                 si = __builtin_amdgcn_sinf(x);
                 co = __builtin_amdgcn_cosf(x);
             }
