@@ -909,6 +909,12 @@ def _require_on(devices, specs, stream):
         _require_here(stream, *(t for t, *_ in specs))
 
 
+def _fit(x, bits=32):
+    """A whole number, or the nearest one that `bits` bits hold, which the library judges (ctypes would wrap it)."""
+    most = 2 ** (bits - 1) - 1
+    return max(-most - 1, min(int(x), most))
+
+
 class PagedCache:
     """A pool of pages (see ``pariskv_pages``): K, V [n_pages][Hkv][page_size][D] float16 on the GPU."""
 
@@ -985,7 +991,7 @@ def plan_pages(table, free, n_free, lens, counts, page_size, t=None, plan=None, 
              (plan.slots, "plan.slots", i32, (n,), False), (plan.positions, "plan.positions", i32, (n,), False))
     (tp, fp, np_, lp, cp, *outs), devices = _tensors(specs)
     _require_on(devices, specs, stream)
-    step = _PageStep(tp, width, fp, free.shape[0], int(page_size), np_, lp, cp, batch, n, *outs)
+    step = _PageStep(tp, width, fp, free.shape[0], _fit(page_size), np_, lp, cp, _fit(batch), n, *outs)
     _check(lib().pariskv_plan_pages(ctypes.byref(step), _stream(stream)))
     return plan
 
@@ -1039,13 +1045,14 @@ def rotate_rows(cfg, cache, q, k, v, positions, slots, freqs=None, q_weight=None
     devices.update((q.get_device(), k.get_device(), v.get_device()))
     _require_on(devices, ((q, "q"), (k, "k"), (v, "v")) + specs, stream)
     _check(lib().pariskv_rotate_rows(cfg.c(), ctypes.byref(_Pages(Kp, Vp, n_pages, size)), qp, qs, kp, ks, vp, vs, t, pp, sp,
-                                     fp, 2 * half, bool(pairs), qw, kw, eps, op, _stream(stream)))
+                                     fp, _fit(2 * half), bool(pairs), qw, kw, eps, op, _stream(stream)))
     return q_out
 
 
 def paged_workspace_size(cfg, batch, t, max_tokens=None):
     """Bytes of a workspace for paged_attend with these sizes and all smaller ones (0 on invalid sizes)."""
-    return int(lib().pariskv_paged_workspace(cfg.c(), int(batch), int(t), max(1, int(t)) if max_tokens is None else int(max_tokens)))
+    most = max(1, int(t)) if max_tokens is None else max_tokens
+    return int(lib().pariskv_paged_workspace(cfg.c(), _fit(batch), _fit(t, 64), _fit(most, 64)))
 
 
 def paged_attend(cfg, q, cache, table, lens, offsets, scale, counts=None, max_tokens=None, softcap=0.0, slopes=None,
@@ -1063,7 +1070,7 @@ def paged_attend(cfg, q, cache, table, lens, offsets, scale, counts=None, max_to
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise ValueError("table must be a [batch][width] int32 tensor")
     batch, width = table.shape
-    most = max(1, t) if max_tokens is None else int(max_tokens)
+    most = max(1, t) if max_tokens is None else _fit(max_tokens, 64)
     if out is None:
         out = _new(q.shape, half, q.device, stream)
     if workspace is None:
