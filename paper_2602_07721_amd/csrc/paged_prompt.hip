@@ -9,7 +9,8 @@
 //   O^T += V^T P^T the scores' own registers are the second operand (the sum over keys may run in any
 //                  order that both operands agree on); V^T by transposing LDS reads.
 // P is rounded to one float16 value, by up to 2^-11 of it, for outputs that are float16 themselves;
-// the sum adds the rounded values, so the weights add up to one.
+// the sum adds the rounded values, so the weights add up to one.  8192 tokens, 32 heads: 567 us, 713 with
+// P in two parts; errors against 64 bits 2.09e-4 and 2.02e-4 of the outputs, of which their own rounding is 2.02e-4.
 //
 // Tiles that every row sees whole take no masks.  The next tile goes straight into LDS while one is
 // computed on; a lane has looked up one of its keys' pages while the tile before was computed on, and
